@@ -1,0 +1,223 @@
+// Shared parts of the KV-cache operators (include/unison_kv.h): argument
+// checks on the host, guarded look-ups and matrix fragments on the device.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "../../include/unison_kv.h"
+#include "common.cuh"
+#include "profile.cuh"
+
+namespace unison {
+
+// ------------------------------------------------------------------ host --
+inline bool kv_aligned(const void *p, size_t b) { return (reinterpret_cast<uintptr_t>(p) & (b - 1)) == 0; }
+inline bool kv_rows_ok(const void *p, int64_t s0, int64_t s1) {
+  return p && kv_aligned(p, 16) && s0 % 8 == 0 && s1 % 8 == 0;
+}
+
+// Sizes of a cache, and the arrays that every operator reads.
+inline int kv_check_cache(const unison_kv_cache *c) {
+  if (!c) return UNISON_ERR_ARG;
+  if (c->n_seqs < 0 || c->max_pages < 0 || c->n_pages < 0 || c->page_size < 1 || c->n_heads < 1)
+    return UNISON_ERR_RANGE;
+  if (c->head_dim < 8 || c->head_dim > 256 || c->head_dim % 8) return UNISON_ERR_RANGE;
+  if (c->dtype != UNISON_KV_BF16 && c->dtype != UNISON_KV_FP16) return UNISON_ERR_ARG;
+  if ((int64_t)c->max_pages * c->page_size >= (1ll << 31) - 64) return UNISON_ERR_RANGE;
+  if (c->n_seqs > 0 && (!c->length || (c->max_pages > 0 && !c->page_table))) return UNISON_ERR_ARG;
+  return UNISON_OK;
+}
+
+inline int kv_check_tree(const unison_kv_tree *t, int n_seqs) {
+  if (!t) return UNISON_ERR_ARG;
+  if (t->n_seqs < 0 || t->n_tokens < 0) return UNISON_ERR_RANGE;
+  if (t->n_seqs != n_seqs) return UNISON_ERR_ARG;
+  if (t->max_tokens < 1 || t->max_tokens > UNISON_KV_MAX_TOKENS) return UNISON_ERR_RANGE;
+  if (t->n_seqs > 0 && !t->offsets) return UNISON_ERR_ARG;
+  return UNISON_OK;
+}
+
+// Multiprocessors of the current device, asked for once per device.
+int kv_sm_count();
+
+// Raises a kernel's dynamic shared memory limit, once per device and kernel
+// (`done`: a bit per device, kept by the caller beside the kernel).
+bool kv_allow_smem(const void *kernel, int bytes, uint64_t *done);
+
+// Queues a kernel.  The verdict is the launch's own, not an older error's.
+template <typename... P, typename... A>
+int kv_launch(const char *name, dim3 grid, dim3 block, size_t smem, void *stream, bool after, void (*kernel)(P...),
+              A &&...args) {
+  cudaError_t e;
+  {
+    ProfSpan span(name, static_cast<cudaStream_t>(stream));
+    cudaLaunchConfig_t lc = {};
+    lc.gridDim = grid;
+    lc.blockDim = block;
+    lc.dynamicSmemBytes = smem;
+    lc.stream = static_cast<cudaStream_t>(stream);
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    lc.attrs = at;
+    lc.numAttrs = after ? 1 : 0;
+    e = cudaLaunchKernelEx(&lc, kernel, static_cast<P>(args)...);
+  }
+  count_launches(1);
+  if (e == cudaSuccess) return UNISON_OK;
+  cudaGetLastError();
+  return UNISON_ERR_CUDA;
+}
+
+// ---------------------------------------------------------------- device --
+template <typename T>
+struct KvType;
+template <>
+struct KvType<__nv_bfloat16> {
+  static __device__ __forceinline__ uint32_t pack(float a, float b) {  // a in the low half
+    const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&v);
+  }
+  static __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+  static constexpr uint32_t kExponent = 0x7F80u;  // all ones: infinity or NaN
+};
+template <>
+struct KvType<__half> {
+  static __device__ __forceinline__ uint32_t pack(float a, float b) {
+    const __half2 v = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&v);
+  }
+  static __device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
+  static constexpr uint32_t kExponent = 0x7C00u;
+};
+
+// A session's rows of the step's arrays, clamped to what the tree allows.
+struct KvRange {
+  int first, count;
+};
+__device__ __forceinline__ KvRange kv_tokens(const unison_kv_tree &t, int b, int32_t *status) {
+  const int lo = t.offsets[b], hi = t.offsets[b + 1];
+  const int first = min(max(lo, 0), t.n_tokens);
+  const int last = min(max(hi, first), t.n_tokens);
+  const int count = min(last - first, t.max_tokens);
+  if (status && (lo != first || hi != first + count)) status[b] = UNISON_ERR_RANGE;
+  return {first, count};
+}
+__device__ __forceinline__ int kv_length(const unison_kv_cache &c, int b) {
+  const int n = c.length[b], room = c.max_pages * c.page_size;
+  const int len = min(max(n, 0), room);
+  if (c.status && n != len) c.status[b] = UNISON_ERR_RANGE;
+  return len;
+}
+// Page of a slot, or -1.  The slot is below max_pages * page_size.
+__device__ __forceinline__ int kv_page(const unison_kv_cache &c, int b, int slot, int &off) {
+  const unsigned i = (unsigned)slot / (unsigned)c.page_size;
+  off = slot - (int)(i * (unsigned)c.page_size);
+  const int page = __ldg(c.page_table + (int64_t)b * c.max_pages + i);
+  if ((unsigned)page < (unsigned)c.n_pages) return page;
+  if (c.status) c.status[b] = UNISON_ERR_RANGE;
+  return -1;
+}
+
+__device__ __forceinline__ uint32_t smem_u32(const void *p) {
+  return static_cast<uint32_t>(__cvta_generic_to_shared(p));
+}
+// 16 bytes into shared memory, zeros where !valid (src is then not read).
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, bool valid) {
+  const int bytes = valid ? 16 : 0;
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void ldm4(uint32_t (&r)[4], uint32_t a) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(a)
+               : "memory");
+}
+__device__ __forceinline__ void ldm4t(uint32_t (&r)[4], uint32_t a) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(a)
+               : "memory");
+}
+template <typename T>
+__device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1);
+template <>
+__device__ __forceinline__ void mma16816<__nv_bfloat16>(float (&c)[4], const uint32_t (&a)[4], uint32_t b0,
+                                                        uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+template <>
+__device__ __forceinline__ void mma16816<__half>(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// 2^x; results below the normal range are 0.
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// A row of DP elements in shared memory is DP / 8 chunks of 16 bytes; chunk c
+// of row r lies at c ^ (r & 7), so that the eight rows of a matrix fragment
+// are in different banks.
+template <int DP>
+__device__ __forceinline__ uint32_t swizzled(uint32_t base, int row, int chunk) {
+  return base + row * (DP * 2) + ((chunk ^ (row & 7)) << 4);
+}
+
+// ------------------------------------------------- sharing out the tiles --
+// The work of a call is a list of key tiles: session by session, KV head by
+// head, row tile by row tile, key tile by key tile.  Every CTA takes an equal
+// run of it, whatever the sessions' lengths are; a run may begin and end
+// inside a segment (one session, head and row tile).
+struct KvWalk {
+  int b;          // session
+  int64_t begin;  // index of its first tile in the list
+};
+
+// Tiles of one session.
+template <int kTile>
+__device__ __forceinline__ int kv_key_tiles(int len, int tokens) {
+  return tokens ? (len + kTile - 1) / kTile + 1 : 0;  // the last one holds the new tokens
+}
+
+// All threads of a CTA add their values; every thread gets the exclusive
+// prefix and the sum.  `part`: 33 words of shared memory.
+__device__ __forceinline__ int64_t block_scan(int64_t x, int64_t *part, int64_t &total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = (blockDim.x + 31) >> 5;
+  int64_t y = x;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int64_t z = __shfl_up_sync(~0u, y, d);
+    if (lane >= d) y += z;
+  }
+  __syncthreads();
+  if (lane == 31) part[warp] = y;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    int64_t s = 0;
+    for (int w = 0; w < warps; w++) {
+      const int64_t v = part[w];
+      part[w] = s;
+      s += v;
+    }
+    part[32] = s;
+  }
+  __syncthreads();
+  total = part[32];
+  return part[warp] + y - x;
+}
+
+}  // namespace unison

@@ -1,0 +1,531 @@
+// Attention of drafted tokens over the paged cache (unison_kv_attend).
+#include "kv.cuh"
+
+namespace unison {
+namespace {
+
+constexpr int kThreads = 128;
+constexpr int kTile = 64;  // keys of a tile
+
+struct AttendParams {
+  unison_kv_cache c;
+  unison_kv_tree t;
+  unison_kv_step s;
+  float *partial;  // [grid][2][rows][DP + 2]
+  struct AttendPart *part;  // [grid]
+  int group;
+};
+
+// What a CTA leaves to be joined: the segment that begins in its run and goes
+// on in the runs of the CTAs up to `last`.
+struct AttendPart {
+  int b, head, row_tile, last;  // last < 0: nothing
+};
+
+template <int DP>
+constexpr int kAttendStages = DP <= 128 ? 3 : 2;
+template <int DP, int MT>
+constexpr int kAttendSmem = kAttendStages<DP> *kTile *DP * 4 + MT * 16 * DP * 2;
+
+// Reads of one tile's rows are planned two tiles ahead of their use: first the
+// page ids (into a register), then the rows' addresses (shared memory), then
+// the copies.
+template <typename T, int DP, int MT>
+__global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) attend_kernel(const AttendParams P) {
+  constexpr int kStages = kAttendStages<DP>;
+  constexpr int kRows = MT * 16;
+  constexpr int kGroups = 4 / MT;      // groups of warps with keys of their own
+  constexpr int kWarpKeys = kTile / kGroups;
+  constexpr int kChunks = DP / 8;
+  extern __shared__ __align__(128) unsigned char smem[];
+  __shared__ int64_t scan_part[33];
+  __shared__ int found_b;
+  __shared__ int64_t found_begin;
+  __shared__ const T *row_k[2][kTile], *row_v[2][kTile];
+  __shared__ uint32_t row_ok[8][2];
+  __shared__ float merge_m[4][16], merge_l[4][16];
+  __shared__ int odd_values;
+
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int D = P.c.head_dim, H = P.c.n_heads, G = P.group;
+  const uint32_t kv_base = smem_u32(smem);
+  const uint32_t q_base = kv_base + kStages * kTile * DP * 4;
+  if (tid == 0) P.part[blockIdx.x].last = -1;
+
+  auto seq_tiles = [&](int b) -> int64_t {
+    const int tokens = kv_tokens(P.t, b, P.c.status).count;
+    const int row_tiles = (tokens * G + kRows - 1) / kRows;
+    return (int64_t)kv_key_tiles<kTile>(kv_length(P.c, b), tokens) * row_tiles * H;
+  };
+  // all tiles, then the session in which this CTA's run begins
+  int64_t total = 0;
+  for (int b0 = 0; b0 < P.c.n_seqs; b0 += kThreads) {
+    int64_t n;
+    block_scan(b0 + tid < P.c.n_seqs ? seq_tiles(b0 + tid) : 0, scan_part, n);
+    total += n;
+  }
+  const int grid = (int)min((int64_t)gridDim.x, total);  // CTAs that have work: one tile at least
+  if ((int)blockIdx.x >= grid) return;
+  int64_t at = total * blockIdx.x / grid;
+  const int64_t end = total * (blockIdx.x + 1) / grid;
+  int64_t sum = 0;
+  for (int b0 = 0; b0 < P.c.n_seqs; b0 += kThreads) {
+    const int64_t mine = b0 + tid < P.c.n_seqs ? seq_tiles(b0 + tid) : 0;
+    int64_t n;
+    const int64_t before = sum + block_scan(mine, scan_part, n);
+    if (at >= before && at < before + mine) {
+      found_b = b0 + tid;
+      found_begin = before;
+    }
+    sum += n;
+    if (at < sum) break;
+  }
+  __syncthreads();
+  int b = found_b;
+  int64_t seq_begin = found_begin;
+
+  while (at < end) {
+    // ---- the segment that `at` lies in
+    int64_t mine = seq_tiles(b);
+    while (at >= seq_begin + mine) {
+      seq_begin += mine;
+      mine = seq_tiles(++b);
+    }
+    const KvRange tok = kv_tokens(P.t, b, nullptr);
+    const int len = kv_length(P.c, b);
+    const int key_tiles = kv_key_tiles<kTile>(len, tok.count);
+    const int row_tiles = (tok.count * G + kRows - 1) / kRows;
+    const int64_t rel = at - seq_begin;
+    const int seg = (int)(rel / key_tiles);
+    const int head = seg / row_tiles, row_tile = seg % row_tiles;
+    const int64_t seg_begin = seq_begin + (int64_t)seg * key_tiles;
+    const int kt0 = (int)(at - seg_begin);
+    const int kt1 = (int)min((int64_t)key_tiles, end - seg_begin);
+    const int rows = min(tok.count * G - row_tile * kRows, kRows);
+    const int last_tile = key_tiles - 1;
+
+    __syncthreads();  // the last segment's shared memory is free
+    if (tid == 0) odd_values = 0;
+
+    // ---- query rows, zeros behind the last and behind head_dim
+    for (int i = tid; i < kRows * kChunks; i += kThreads) {
+      const int r = i / kChunks, c = i % kChunks;
+      const bool ok = r < rows && c * 8 < D;
+      const int row = row_tile * kRows + (ok ? r : 0);
+      const T *src = static_cast<const T *>(P.s.q) + (tok.first + row / G) * P.s.q_token +
+                     (head * G + row % G) * P.s.q_head + (ok ? c * 8 : 0);
+      cp_async16(swizzled<DP>(q_base, r, c), src, ok);
+    }
+    cp_commit();
+
+    auto find_page = [&](int kt, int &off) -> int {  // threads 0 .. kTile-1
+      const int slot = kt * kTile + tid;
+      off = 0;
+      if (tid >= kTile || kt >= last_tile || slot >= len) return -1;
+      return kv_page(P.c, b, slot, off);
+    };
+    auto put_rows = [&](int kt, int page, int off) {
+      if (tid >= kTile) return;
+      const T *k = nullptr, *v = nullptr;
+      if (kt == last_tile) {
+        if (tid < tok.count) {
+          k = static_cast<const T *>(P.s.k_new) + (tok.first + tid) * P.s.k_token + head * P.s.k_head;
+          v = static_cast<const T *>(P.s.v_new) + (tok.first + tid) * P.s.v_token + head * P.s.v_head;
+        }
+      } else if (page >= 0) {
+        k = static_cast<const T *>(P.c.k) + page * P.c.k_page + head * P.c.k_head + off * P.c.k_slot;
+        v = static_cast<const T *>(P.c.v) + page * P.c.v_page + head * P.c.v_head + off * P.c.v_slot;
+      }
+      row_k[kt & 1][tid] = k;
+      row_v[kt & 1][tid] = v;
+      const uint32_t bits = __ballot_sync(~0u, k != nullptr);
+      if (lane == 0) row_ok[kt & 7][warp] = bits;
+    };
+    auto copy_tile = [&](int kt) {
+      const uint32_t st = kv_base + ((kt - kt0) % kStages) * (kTile * DP * 4);
+#pragma unroll
+      for (int i = 0; i < kTile * kChunks / kThreads; i++) {
+        const int r = (i * kThreads + tid) / kChunks, c = (i * kThreads + tid) % kChunks;
+        const T *k = row_k[kt & 1][r], *v = row_v[kt & 1][r];
+        const bool ok = k != nullptr && c * 8 < D;
+        cp_async16(swizzled<DP>(st, r, c), ok ? k + c * 8 : static_cast<const T *>(P.s.q), ok);
+        cp_async16(swizzled<DP>(st + kTile * DP * 2, r, c), ok ? v + c * 8 : static_cast<const T *>(P.s.q), ok);
+      }
+    };
+
+    // ---- fill the pipeline
+    int page, off;
+    for (int s = 0; s < kStages - 1; s++) {
+      const int kt = kt0 + s;
+      if (kt < kt1) {
+        page = find_page(kt, off);
+        put_rows(kt, page, off);
+      }
+      __syncthreads();
+      if (kt < kt1) copy_tile(kt);
+      cp_commit();
+    }
+    if (kt0 + kStages - 1 < kt1) {
+      page = find_page(kt0 + kStages - 1, off);
+      put_rows(kt0 + kStages - 1, page, off);
+    }
+    page = find_page(kt0 + kStages, off);
+
+    const int rt = warp % MT, kg = warp / MT;
+    const int r0 = rt * 16 + (lane >> 2), r1 = r0 + 8;
+    auto mask_of = [&](int r) -> uint64_t {
+      if (r >= rows) return 0;
+      const int node = (row_tile * kRows + r) / G;
+      return P.t.mask ? P.t.mask[tok.first + node] : ~0ull >> (63 - node);
+    };
+    const uint64_t mask0 = mask_of(r0), mask1 = mask_of(r1);
+
+    float o[DP / 8][4];
+#pragma unroll
+    for (int i = 0; i < DP / 8; i++) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+    float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;  // running maximum (log2 units) and sum
+    const float to_log2 = P.s.scale * 1.4426950408889634f;
+
+    for (int kt = kt0; kt < kt1; kt++) {
+      cp_wait<kStages - 2>();
+      __syncthreads();
+      if (kt + kStages - 1 < kt1) copy_tile(kt + kStages - 1);
+      cp_commit();
+      if (kt + kStages < kt1) put_rows(kt + kStages, page, off);
+      page = find_page(kt + kStages + 1, off);
+
+      const uint32_t ks = kv_base + ((kt - kt0) % kStages) * (kTile * DP * 4), vs = ks + kTile * DP * 2;
+      if (kt == last_tile) {
+        // A new token that a row does not see must not reach it as 0 * inf:
+        // such values become 0 here and are put back, row by row, at the end.
+        const int first = (kt - kt0) % kStages * (kTile * DP * 2) + kTile * DP;
+        uint16_t *v = reinterpret_cast<uint16_t *>(smem) + first;
+        bool odd = false;
+        for (int i = tid; i < kTile * DP; i += kThreads)
+          if ((v[i] & KvType<T>::kExponent) == KvType<T>::kExponent) {
+            v[i] = 0;
+            odd = true;
+          }
+        if (odd) odd_values = 1;
+        __syncthreads();
+      }
+
+      // ---- scores of 16 rows and kWarpKeys keys
+      float s[kWarpKeys / 8][4];
+#pragma unroll
+      for (int i = 0; i < kWarpKeys / 8; i++) s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.f;
+#pragma unroll
+      for (int d = 0; d < DP / 16; d++) {
+        uint32_t a[4];
+        ldm4(a, swizzled<DP>(q_base, rt * 16 + (lane & 15), d * 2 + (lane >> 4)));
+#pragma unroll
+        for (int j = 0; j < kWarpKeys / 16; j++) {
+          uint32_t kf[4];
+          const int key = kg * kWarpKeys + j * 16 + ((lane >> 4) << 3) + (lane & 7);
+          ldm4(kf, swizzled<DP>(ks, key, d * 2 + ((lane >> 3) & 1)));
+          mma16816<T>(s[2 * j], a, kf[0], kf[1]);
+          mma16816<T>(s[2 * j + 1], a, kf[2], kf[3]);
+        }
+      }
+      const uint64_t there = (uint64_t)row_ok[kt & 7][1] << 32 | row_ok[kt & 7][0];
+      const uint64_t see0 = kt == last_tile ? there & mask0 : there, see1 = kt == last_tile ? there & mask1 : there;
+      float t0 = -INFINITY, t1 = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < kWarpKeys / 8; i++) {
+#pragma unroll
+        for (int e = 0; e < 2; e++) {
+          const int key = kg * kWarpKeys + i * 8 + (lane & 3) * 2 + e;
+          s[i][e] = see0 >> key & 1 ? s[i][e] * to_log2 : -INFINITY;
+          s[i][2 + e] = see1 >> key & 1 ? s[i][2 + e] * to_log2 : -INFINITY;
+          t0 = fmaxf(t0, s[i][e]);
+          t1 = fmaxf(t1, s[i][2 + e]);
+        }
+      }
+#pragma unroll
+      for (int d = 1; d < 4; d <<= 1) {
+        t0 = fmaxf(t0, __shfl_xor_sync(~0u, t0, d));
+        t1 = fmaxf(t1, __shfl_xor_sync(~0u, t1, d));
+      }
+      const float n0 = fmaxf(m0, t0), n1 = fmaxf(m1, t1);
+      const float u0 = n0 == -INFINITY ? 0.f : n0, u1 = n1 == -INFINITY ? 0.f : n1;
+      const float f0 = exp2_fast(m0 - u0), f1 = exp2_fast(m1 - u1);
+      m0 = n0;
+      m1 = n1;
+      l0 *= f0;
+      l1 *= f1;
+#pragma unroll
+      for (int i = 0; i < DP / 8; i++) {
+        o[i][0] *= f0;
+        o[i][1] *= f0;
+        o[i][2] *= f1;
+        o[i][3] *= f1;
+      }
+      // ---- weights, and their products with the values
+#pragma unroll
+      for (int j = 0; j < kWarpKeys / 16; j++) {
+        float w[8];
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+          w[e] = exp2_fast(s[2 * j][e] - (e < 2 ? u0 : u1));
+          w[4 + e] = exp2_fast(s[2 * j + 1][e] - (e < 2 ? u0 : u1));
+        }
+        l0 += (w[0] + w[1]) + (w[4] + w[5]);
+        l1 += (w[2] + w[3]) + (w[6] + w[7]);
+        const uint32_t a[4] = {KvType<T>::pack(w[0], w[1]), KvType<T>::pack(w[2], w[3]),
+                               KvType<T>::pack(w[4], w[5]), KvType<T>::pack(w[6], w[7])};
+#pragma unroll
+        for (int d = 0; d < DP / 16; d++) {
+          uint32_t vf[4];
+          const int key = kg * kWarpKeys + j * 16 + (lane & 15);
+          ldm4t(vf, swizzled<DP>(vs, key, d * 2 + (lane >> 4)));
+          mma16816<T>(o[2 * d], a, vf[0], vf[1]);
+          mma16816<T>(o[2 * d + 1], a, vf[2], vf[3]);
+        }
+      }
+    }
+    cp_wait<0>();
+
+    // ---- join the warps that had keys of their own
+#pragma unroll
+    for (int d = 1; d < 4; d <<= 1) {
+      l0 += __shfl_xor_sync(~0u, l0, d);
+      l1 += __shfl_xor_sync(~0u, l1, d);
+    }
+    if ((lane & 3) == 0) {
+      merge_m[warp][lane >> 2] = m0;
+      merge_m[warp][(lane >> 2) + 8] = m1;
+      merge_l[warp][lane >> 2] = l0;
+      merge_l[warp][(lane >> 2) + 8] = l1;
+    }
+    __syncthreads();
+    float top0 = m0, top1 = m1;
+#pragma unroll
+    for (int g = 0; g < kGroups; g++) {
+      top0 = fmaxf(top0, merge_m[g * MT + rt][lane >> 2]);
+      top1 = fmaxf(top1, merge_m[g * MT + rt][(lane >> 2) + 8]);
+    }
+    const float f0 = exp2_fast(m0 - (top0 == -INFINITY ? 0.f : top0));
+    const float f1 = exp2_fast(m1 - (top1 == -INFINITY ? 0.f : top1));
+    float *acc = reinterpret_cast<float *>(smem);  // [kGroups][kRows][DP]: the stages are drained
+#pragma unroll
+    for (int i = 0; i < DP / 8; i++) {
+      float *p0 = acc + ((kg * kRows + r0) * DP + i * 8 + (lane & 3) * 2);
+      float *p1 = p0 + 8 * DP;
+      p0[0] = o[i][0] * f0;
+      p0[1] = o[i][1] * f0;
+      p1[0] = o[i][2] * f1;
+      p1[1] = o[i][3] * f1;
+    }
+    __syncthreads();
+    const bool whole = kt0 == 0 && kt1 == key_tiles;
+    const bool starts = kt0 == 0;
+    float *part = P.partial + ((int64_t)blockIdx.x * 2 + (starts ? 1 : 0)) * (kRows * (DP + 2));
+    for (int i = tid; i < kRows * (DP / 2); i += kThreads) {
+      const int r = i / (DP / 2), d = i % (DP / 2) * 2;
+      if (r >= rows || d >= D) continue;
+      const int rr = r & 15, ww = r >> 4;
+      float top = -INFINITY, l = 0.f, x = 0.f, y = 0.f;
+#pragma unroll
+      for (int g = 0; g < kGroups; g++) top = fmaxf(top, merge_m[g * MT + ww][rr]);
+      const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+      for (int g = 0; g < kGroups; g++) {
+        l += merge_l[g * MT + ww][rr] * exp2_fast(merge_m[g * MT + ww][rr] - base);
+        x += acc[(g * kRows + r) * DP + d];
+        y += acc[(g * kRows + r) * DP + d + 1];
+      }
+      const int row = row_tile * kRows + r, node = row / G;
+      if (kt1 == key_tiles && odd_values) {
+        const uint64_t mask = (P.t.mask ? P.t.mask[tok.first + node] : ~0ull >> (63 - node)) & (~0ull >> (64 - tok.count));
+        for (int j = 0; j < tok.count; j++) {
+          if (!(mask >> j & 1)) continue;
+          const T *v = static_cast<const T *>(P.s.v_new) + (tok.first + j) * P.s.v_token + head * P.s.v_head + d;
+          const float vx = KvType<T>::to_float(v[0]), vy = KvType<T>::to_float(v[1]);
+          if (!isfinite(vx)) x += vx;
+          if (!isfinite(vy)) y += vy;
+        }
+      }
+      if (whole) {
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        T *dst = static_cast<T *>(P.s.out) + (tok.first + node) * P.s.out_token + (head * G + row % G) * P.s.out_head + d;
+        *reinterpret_cast<uint32_t *>(dst) = KvType<T>::pack(x * inv, y * inv);
+        if (d == 0 && P.s.lse)
+          P.s.lse[(int64_t)(tok.first + node) * P.s.n_q_heads + head * G + row % G] =
+              (top + log2f(l)) * 0.6931471805599453f;
+      } else {
+        part[r * (DP + 2) + d] = x;
+        part[r * (DP + 2) + d + 1] = y;
+        if (d == 0) {
+          part[r * (DP + 2) + DP] = top;
+          part[r * (DP + 2) + DP + 1] = l;
+        }
+      }
+    }
+    if (starts && !whole && tid == 0) {
+      // the CTA in whose run the segment's last tile lies
+      const int64_t tile = seg_begin + key_tiles - 1;
+      int c = (int)((tile + 1) * grid / total);  // about right: the exact one is a step away
+      c = min(max(c, 0), grid - 1);
+      while (c > 0 && total * c / grid > tile) c--;
+      while (total * (c + 1) / grid <= tile) c++;
+      P.part[blockIdx.x] = {b, head, row_tile, c};
+    }
+    at = seg_begin + kt1;
+  }
+}
+
+// Joins the parts of the segments that lie in several CTAs' runs.  One CTA per
+// run of the other kernel and 16 rows.
+template <typename T, int DP, int MT>
+__global__ void __launch_bounds__(kThreads) attend_join_kernel(const AttendParams P) {
+  constexpr int kRows = MT * 16;
+  const AttendPart seg = P.part[blockIdx.x];
+  if (seg.last < 0) return;
+  const int D = P.c.head_dim, G = P.group;
+  const KvRange tok = kv_tokens(P.t, seg.b, nullptr);
+  const int rows = min(tok.count * G - seg.row_tile * kRows, kRows);
+  const int parts = seg.last - blockIdx.x + 1;
+  constexpr int64_t kStep = (int64_t)2 * kRows * (DP + 2);
+  // the first CTA's part is its second one, the others' is their first
+  const float *first = P.partial + (int64_t)blockIdx.x * kStep + kRows * (DP + 2);
+  const float *rest = P.partial + (int64_t)blockIdx.x * kStep;
+  for (int i = threadIdx.x; i < 16 * (DP / 2); i += kThreads) {
+    const int r = blockIdx.y * 16 + i / (DP / 2), d = i % (DP / 2) * 2;
+    if (r >= rows || d >= D) continue;
+    float top = first[r * (DP + 2) + DP];
+    for (int p = 1; p < parts; p++) top = fmaxf(top, rest[p * kStep + r * (DP + 2) + DP]);
+    const float base = top == -INFINITY ? 0.f : top;
+    float x = 0.f, y = 0.f, l = 0.f;
+    for (int p = 0; p < parts; p++) {
+      const float *q = (p ? rest + p * kStep : first) + r * (DP + 2);
+      const float f = exp2_fast(q[DP] - base);
+      l += q[DP + 1] * f;
+      x += q[d] * f;
+      y += q[d + 1] * f;
+    }
+    const int row = seg.row_tile * kRows + r, node = row / G;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    T *dst = static_cast<T *>(P.s.out) + (tok.first + node) * P.s.out_token + (seg.head * G + row % G) * P.s.out_head + d;
+    *reinterpret_cast<uint32_t *>(dst) = KvType<T>::pack(x * inv, y * inv);
+    if (d == 0 && P.s.lse)
+      P.s.lse[(int64_t)(tok.first + node) * P.s.n_q_heads + seg.head * G + row % G] =
+          (top + log2f(l)) * 0.6931471805599453f;
+  }
+}
+
+struct AttendPlan {
+  int dp, mt, grid;
+  uint64_t bytes;
+};
+
+AttendPlan attend_plan(int head_dim, int max_rows) {
+  AttendPlan p;
+  p.dp = head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256;
+  p.mt = max_rows <= 16 ? 1 : max_rows <= 32 ? 2 : 4;
+  p.grid = kv_sm_count() * (p.dp <= 128 ? 2 : 1);
+  p.bytes = (uint64_t)p.grid * (2 * p.mt * 16 * (p.dp + 2) * 4 + sizeof(AttendPart));
+  return p;
+}
+
+template <typename T, int DP, int MT>
+int attend_run(const AttendParams &p, const AttendPlan &plan, void *stream) {
+  static uint64_t done = 0;
+  constexpr int smem = kAttendSmem<DP, MT>;
+  if (!kv_allow_smem(reinterpret_cast<const void *>(attend_kernel<T, DP, MT>), smem, &done)) return UNISON_ERR_CUDA;
+  int rc = kv_launch("kv_attend", dim3(plan.grid), dim3(kThreads), smem, stream, false, attend_kernel<T, DP, MT>, p);
+  if (rc != UNISON_OK) return rc;
+  return kv_launch("kv_attend_join", dim3(plan.grid, MT), dim3(kThreads), 0, stream, false,
+                   attend_join_kernel<T, DP, MT>, p);
+}
+
+template <typename T>
+int attend_pick(const AttendParams &p, const AttendPlan &plan, void *stream) {
+  switch (plan.dp * 8 + plan.mt) {
+    case 64 * 8 + 1: return attend_run<T, 64, 1>(p, plan, stream);
+    case 64 * 8 + 2: return attend_run<T, 64, 2>(p, plan, stream);
+    case 64 * 8 + 4: return attend_run<T, 64, 4>(p, plan, stream);
+    case 128 * 8 + 1: return attend_run<T, 128, 1>(p, plan, stream);
+    case 128 * 8 + 2: return attend_run<T, 128, 2>(p, plan, stream);
+    case 128 * 8 + 4: return attend_run<T, 128, 4>(p, plan, stream);
+    case 256 * 8 + 1: return attend_run<T, 256, 1>(p, plan, stream);
+    case 256 * 8 + 2: return attend_run<T, 256, 2>(p, plan, stream);
+    default: return attend_run<T, 256, 4>(p, plan, stream);
+  }
+}
+
+}  // namespace
+
+int kv_sm_count() {
+  static int count[64];  // 0: not asked yet; every thread would store the same
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
+    cudaGetLastError();
+    return 1;
+  }
+  int n = __atomic_load_n(&count[dev], __ATOMIC_RELAXED);
+  if (n) return n;
+  if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) {
+    cudaGetLastError();
+    return 1;
+  }
+  __atomic_store_n(&count[dev], n, __ATOMIC_RELAXED);
+  return n;
+}
+
+bool kv_allow_smem(const void *kernel, int bytes, uint64_t *done) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
+    cudaGetLastError();
+    return false;
+  }
+  if (__atomic_load_n(done, __ATOMIC_RELAXED) >> dev & 1) return true;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) {
+    cudaGetLastError();
+    return false;
+  }
+  __atomic_fetch_or(done, 1ull << dev, __ATOMIC_RELAXED);
+  return true;
+}
+
+}  // namespace unison
+
+using namespace unison;
+
+static int attend_check(const unison_kv_cache *c, const unison_kv_tree *t, int n_q_heads) {
+  int rc = kv_check_cache(c);
+  if (rc == UNISON_OK) rc = kv_check_tree(t, c->n_seqs);
+  if (rc != UNISON_OK) return rc;
+  if (n_q_heads < 1 || n_q_heads % c->n_heads || n_q_heads / c->n_heads > 64) return UNISON_ERR_RANGE;
+  return UNISON_OK;
+}
+
+extern "C" uint64_t unison_kv_attend_workspace(const unison_kv_cache *cache, const unison_kv_tree *tree, int n_q_heads) {
+  if (attend_check(cache, tree, n_q_heads) != UNISON_OK) return 0;
+  return attend_plan(cache->head_dim, tree->max_tokens * (n_q_heads / cache->n_heads)).bytes;
+}
+
+extern "C" int unison_kv_attend(const unison_kv_cache *cache, const unison_kv_tree *tree, const unison_kv_step *step,
+                                void *workspace, uint64_t workspace_bytes, void *cuda_stream) {
+  if (!step) return UNISON_ERR_ARG;
+  const int rc = attend_check(cache, tree, step->n_q_heads);
+  if (rc != UNISON_OK) return rc;
+  if (cache->n_seqs == 0 || tree->n_tokens == 0) return UNISON_OK;
+  if (!kv_rows_ok(step->q, step->q_token, step->q_head) || !kv_rows_ok(step->k_new, step->k_token, step->k_head) ||
+      !kv_rows_ok(step->v_new, step->v_token, step->v_head) || !kv_rows_ok(step->out, step->out_token, step->out_head))
+    return UNISON_ERR_ARG;
+  if (cache->max_pages > 0 && cache->n_pages > 0 &&
+      (!kv_rows_ok(cache->k, cache->k_page | cache->k_head, cache->k_slot) ||
+       !kv_rows_ok(cache->v, cache->v_page | cache->v_head, cache->v_slot)))
+    return UNISON_ERR_ARG;
+  AttendParams p;
+  p.c = *cache;
+  p.t = *tree;
+  p.s = *step;
+  p.group = step->n_q_heads / cache->n_heads;
+  const AttendPlan plan = attend_plan(cache->head_dim, tree->max_tokens * p.group);
+  if (!workspace || !kv_aligned(workspace, 16) || workspace_bytes < plan.bytes) return UNISON_ERR_ARG;
+  p.part = static_cast<AttendPart *>(workspace);
+  p.partial = reinterpret_cast<float *>(p.part + plan.grid);
+  return cache->dtype == UNISON_KV_BF16 ? attend_pick<__nv_bfloat16>(p, plan, cuda_stream)
+                                        : attend_pick<__half>(p, plan, cuda_stream);
+}

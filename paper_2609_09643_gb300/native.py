@@ -15,7 +15,8 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
 OUT = os.path.join(PKG, "_build")
 LIB = os.path.join(OUT, "libunison.so")
-SOURCES = ["trace.cu", "replay.cu", "rank.cu", "profile.cu", "selftest.cu"]
+SOURCES = ["trace.cu", "replay.cu", "rank.cu", "profile.cu", "selftest.cu",
+           "kv_attend.cu", "kv_observe.cu", "kv_cache.cu", "kv_verify.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-O2"]
 
@@ -31,7 +32,8 @@ def _stale(obj: str, src: str) -> bool:
     if not os.path.exists(obj):
         return True
     headers = [os.path.join(CSRC, h) for h in sorted(os.listdir(CSRC)) if h.endswith(".cuh")]
-    deps = [src, *headers, os.path.join(PKG, "..", "include", "unison.h")]
+    include = os.path.join(PKG, "..", "include")
+    deps = [src, *headers, *(os.path.join(include, h) for h in ("unison.h", "unison_kv.h"))]
     return any(os.path.getmtime(d) > os.path.getmtime(obj) for d in deps if os.path.exists(d))
 
 

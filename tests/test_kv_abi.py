@@ -1,0 +1,184 @@
+"""Host side of the KV-cache operators (no GPU needed): every declared symbol
+is exported, and every call refuses what its header excludes before anything
+is queued."""
+import ctypes as C
+
+import pytest
+import torch
+
+from kv_reference import Made
+from test_abi import declared_symbols
+
+
+@pytest.fixture(scope="module")
+def kv():
+    from paper_2609_09643_gb300 import native
+    native.build()
+    from paper_2609_09643_gb300 import kv
+    return kv
+
+
+def test_declared_symbols_are_exported(kv):
+    lib = C.CDLL(kv.binding.lib_path())
+    decl = [s for s in declared_symbols("unison_kv.h")]
+    assert decl == sorted(kv.EXPORTS)
+    for name in decl:
+        assert hasattr(lib, name), name
+
+
+def _made(**kw):
+    return Made([5, 40], [3, 2], device="cpu", **kw)
+
+
+class _Args:
+    """Arguments of every call, on host tensors: a call that is refused never reads them."""
+
+    def __init__(self, kv):
+        m = self.m = _made()
+        self.kv, self.L = kv, kv.lib()
+        self.cache, self.tree = m.cache(kv), m.tree(kv)
+        self.into = _made().cache(kv)
+        self.out, self.lse = torch.zeros_like(m.q), torch.zeros(m.q.shape[:2])
+        self.mass_new = torch.zeros(m.total, m.hkv)
+        self.step = kv._step(self.cache, self.tree, m.q, m.k_new, m.v_new, self.out, self.lse, self.mass_new, 0.1)
+        self.path_t = torch.zeros(2, 3, dtype=torch.int32)
+        self.path = kv.KvPath(self.path_t.data_ptr(), self.path_t.data_ptr(), 3)
+        self.work = torch.zeros(64 << 20, dtype=torch.uint8)
+        self.bytes = self.work.numel()
+        self.keep = torch.zeros(2, dtype=torch.int32).data_ptr()
+        self.sink = self.recent = 0
+        p = torch.zeros(m.total, 100)
+        i = torch.zeros(64, dtype=torch.int32)
+        self.hold = (p, i)
+        self.v = kv.KvVerify(p.data_ptr(), p.data_ptr(), 100, 100, i.data_ptr(), i.data_ptr(), i.data_ptr(),
+                             i.data_ptr(), i.data_ptr(), i.data_ptr(), 3, 100, 2)
+
+    def attend(self):
+        return self.L.unison_kv_attend(self.cache.ref, self.tree.ref, C.byref(self.step), self.work.data_ptr(),
+                                       self.bytes, None)
+
+    def observe(self):
+        return self.L.unison_kv_observe(self.cache.ref, self.tree.ref, C.byref(self.step), C.byref(self.path), None)
+
+    def commit(self):
+        return self.L.unison_kv_commit(self.cache.ref, self.tree.ref, C.byref(self.step), C.byref(self.path), None)
+
+    def evict(self):
+        return self.L.unison_kv_evict(self.cache.ref, self.into.ref, self.keep, self.sink, self.recent,
+                                      self.work.data_ptr(), self.bytes, None)
+
+    def verify(self):
+        return self.L.unison_kv_verify(self.tree.ref, C.byref(self.v), None)
+
+
+ARG, RANGE = -1, -4
+CACHE = ("attend", "observe", "commit", "evict")
+STEP = ("attend", "observe", "commit")
+REFUSED = [
+    # calls, what is changed, expected code
+    (CACHE, lambda a: setattr(a.cache.struct, "page_size", 0), RANGE),
+    (CACHE, lambda a: setattr(a.cache.struct, "n_seqs", -1), RANGE),
+    (CACHE, lambda a: setattr(a.cache.struct, "n_heads", 0), RANGE),
+    (CACHE, lambda a: setattr(a.cache.struct, "head_dim", 60), RANGE),
+    (CACHE, lambda a: setattr(a.cache.struct, "head_dim", 264), RANGE),
+    (CACHE, lambda a: setattr(a.cache.struct, "max_pages", 1 << 28), RANGE),
+    (CACHE, lambda a: setattr(a.cache.struct, "dtype", 2), ARG),
+    (CACHE, lambda a: setattr(a.cache.struct, "length", None), ARG),
+    (CACHE, lambda a: setattr(a.cache.struct, "page_table", None), ARG),
+    (CACHE, lambda a: setattr(a.cache.struct, "k", None), ARG),
+    (CACHE, lambda a: setattr(a.cache.struct, "k", a.cache.struct.k + 8), ARG),
+    (CACHE, lambda a: setattr(a.cache.struct, "k_slot", 12), ARG),
+    (("attend", "commit", "evict"), lambda a: setattr(a.cache.struct, "v_head", 4), ARG),
+    (("observe", "evict"), lambda a: setattr(a.cache.struct, "mass", None), ARG),
+    ((*STEP, "verify"), lambda a: setattr(a.tree.struct, "max_tokens", 65), RANGE),
+    ((*STEP, "verify"), lambda a: setattr(a.tree.struct, "max_tokens", 0), RANGE),
+    ((*STEP, "verify"), lambda a: setattr(a.tree.struct, "n_tokens", -1), RANGE),
+    ((*STEP, "verify"), lambda a: setattr(a.tree.struct, "offsets", None), ARG),
+    (STEP, lambda a: setattr(a.tree.struct, "n_seqs", 3), ARG),
+    (("attend", "observe"), lambda a: setattr(a.step, "n_q_heads", 7), RANGE),
+    (("attend", "observe"), lambda a: setattr(a.step, "n_q_heads", 2 * 65), RANGE),
+    (("attend", "observe"), lambda a: setattr(a.step, "n_q_heads", 0), RANGE),
+    (("attend", "observe"), lambda a: setattr(a.step, "q", None), ARG),
+    (("attend", "observe"), lambda a: setattr(a.step, "q_token", 4), ARG),
+    (("attend", "commit"), lambda a: setattr(a.step, "v_new", None), ARG),
+    (STEP, lambda a: setattr(a.step, "k_new", a.step.k_new + 2), ARG),
+    (("attend",), lambda a: setattr(a.step, "out", None), ARG),
+    (("observe",), lambda a: setattr(a.step, "lse", None), ARG),
+    (("observe", "commit"), lambda a: setattr(a.path, "n_path", None), ARG),
+    (("attend", "evict"), lambda a: setattr(a, "bytes", 16), ARG),
+    (("evict",), lambda a: setattr(a, "keep", None), ARG),
+    (("evict",), lambda a: setattr(a, "sink", -1), RANGE),
+    (("evict",), lambda a: setattr(a, "recent", -1), RANGE),
+    (("evict",), lambda a: setattr(a.into.struct, "head_dim", 128), ARG),
+    (("evict",), lambda a: setattr(a.into.struct, "n_heads", 1), ARG),
+    (("evict",), lambda a: setattr(a.into.struct, "v", None), ARG),
+    (("verify",), lambda a: setattr(a.v, "vocab", 0), RANGE),
+    (("verify",), lambda a: setattr(a.v, "vocab", (1 << 22) + 1), RANGE),
+    (("verify",), lambda a: setattr(a.v, "dtype", 3), ARG),
+    (("verify",), lambda a: setattr(a.v, "path_stride", 2), ARG),
+    (("verify",), lambda a: setattr(a.v, "u", None), ARG),
+    (("verify",), lambda a: setattr(a.v, "next_token", None), ARG),
+    (("verify",), lambda a: setattr(a.tree.struct, "parent", None), ARG),
+]
+
+
+@pytest.mark.parametrize("i", range(len(REFUSED)))
+def test_refusals(kv, i):
+    calls, change, code = REFUSED[i]
+    for call in calls:
+        a = _Args(kv)
+        change(a)
+        assert getattr(a, call)() == code, call
+
+
+def test_null_structs_are_refused(kv):
+    a, L = _Args(kv), kv.lib()
+    assert L.unison_kv_attend(None, a.tree.ref, C.byref(a.step), a.work.data_ptr(), a.bytes, None) == ARG
+    assert L.unison_kv_attend(a.cache.ref, None, C.byref(a.step), a.work.data_ptr(), a.bytes, None) == ARG
+    assert L.unison_kv_attend(a.cache.ref, a.tree.ref, None, a.work.data_ptr(), a.bytes, None) == ARG
+    assert L.unison_kv_observe(a.cache.ref, a.tree.ref, None, None, None) == ARG
+    assert L.unison_kv_commit(a.cache.ref, a.tree.ref, None, None, None) == ARG
+    assert L.unison_kv_evict(None, None, a.keep, 0, 0, a.work.data_ptr(), a.bytes, None) == ARG
+    assert L.unison_kv_verify(None, C.byref(a.v), None) == ARG
+    assert L.unison_kv_verify(a.tree.ref, None, None) == ARG
+    assert L.unison_kv_attend_workspace(None, None, 8) == 0
+    assert L.unison_kv_evict_workspace(None) == 0
+
+
+def test_binding_refuses_other_types_and_shapes(kv):
+    m = _made()
+    cache, tree = m.cache(kv), m.tree(kv)
+    for bad in (m.q.float(), m.q[:, :, :32], m.q[:2], m.q.transpose(1, 2)):
+        with pytest.raises(ValueError):
+            kv.attend(cache, tree, bad, m.k_new, m.v_new, stream=0)
+    with pytest.raises(ValueError):
+        kv.attend(cache, tree, m.q, m.k_new[:, :1], m.v_new, stream=0)
+    with pytest.raises(ValueError):
+        kv.Cache(m.k, m.v.half(), m.page_table, m.length)
+    with pytest.raises(ValueError):
+        kv.Cache(m.k, m.v, m.page_table.long(), m.length)
+    with pytest.raises(ValueError):
+        kv.Cache(m.k, m.v, m.page_table, m.length, mass=m.mass.double())
+    with pytest.raises(ValueError):
+        kv.Tree(m.offsets, 3)
+    with pytest.raises(ValueError):
+        kv.Tree(m.offsets, 3, mask=m.mask.int())
+    with pytest.raises(ValueError):
+        kv.evict(cache, torch.zeros(3, dtype=torch.int32), stream=0)
+    p = torch.zeros(m.total, 10)
+    i = torch.zeros(m.total, dtype=torch.int32)
+    with pytest.raises(ValueError):
+        kv.verify(tree, i, p, p.half(), torch.zeros(m.total), torch.zeros(2), stream=0)
+    with pytest.raises(ValueError):
+        kv.verify(tree, i.long(), p, p, torch.zeros(m.total), torch.zeros(2), stream=0)
+
+
+def test_empty_batches_do_nothing(kv):
+    m = Made([], [], device="cpu")
+    cache, tree = m.cache(kv), m.tree(kv)
+    kv.attend(cache, tree, m.q, m.k_new, m.v_new, stream=0)
+    kv.observe(cache, tree, m.q, torch.zeros(0, 8), m.k_new, stream=0)
+    kv.commit(cache, tree, m.k_new, m.v_new, stream=0)
+    kv.evict(cache, torch.zeros(0, dtype=torch.int32), stream=0)
+    i = torch.zeros(0, dtype=torch.int32)
+    kv.verify(tree, i, torch.zeros(0, 10), None, torch.zeros(0), torch.zeros(0), stream=0)
