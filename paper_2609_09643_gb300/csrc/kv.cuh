@@ -47,9 +47,10 @@ int kv_sm_count();
 // (`done`: a bit per device, kept by the caller beside the kernel).
 bool kv_allow_smem(const void *kernel, int bytes, uint64_t *done);
 
-// Queues a kernel.  The verdict is the launch's own, not an older error's.
+// Queues a kernel of clusters of `cluster` CTAs.  The verdict is the launch's
+// own, not an older error's.
 template <typename... P, typename... A>
-int kv_launch(const char *name, dim3 grid, dim3 block, size_t smem, void *stream, bool after, void (*kernel)(P...),
+int kv_launch(const char *name, dim3 grid, dim3 block, size_t smem, void *stream, int cluster, void (*kernel)(P...),
               A &&...args) {
   cudaError_t e;
   {
@@ -60,10 +61,12 @@ int kv_launch(const char *name, dim3 grid, dim3 block, size_t smem, void *stream
     lc.dynamicSmemBytes = smem;
     lc.stream = static_cast<cudaStream_t>(stream);
     cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = cluster;
+    at[0].val.clusterDim.y = 1;
+    at[0].val.clusterDim.z = 1;
     lc.attrs = at;
-    lc.numAttrs = after ? 1 : 0;
+    lc.numAttrs = cluster > 1 ? 1 : 0;
     e = cudaLaunchKernelEx(&lc, kernel, static_cast<P>(args)...);
   }
   count_launches(1);

@@ -432,9 +432,9 @@ int attend_run(const AttendParams &p, const AttendPlan &plan, void *stream) {
   static uint64_t done = 0;
   constexpr int smem = kAttendSmem<DP, MT>;
   if (!kv_allow_smem(reinterpret_cast<const void *>(attend_kernel<T, DP, MT>), smem, &done)) return UNISON_ERR_CUDA;
-  int rc = kv_launch("kv_attend", dim3(plan.grid), dim3(kThreads), smem, stream, false, attend_kernel<T, DP, MT>, p);
+  int rc = kv_launch("kv_attend", dim3(plan.grid), dim3(kThreads), smem, stream, 1, attend_kernel<T, DP, MT>, p);
   if (rc != UNISON_OK) return rc;
-  return kv_launch("kv_attend_join", dim3(plan.grid, MT), dim3(kThreads), 0, stream, false,
+  return kv_launch("kv_attend_join", dim3(plan.grid, MT), dim3(kThreads), 0, stream, 1,
                    attend_join_kernel<T, DP, MT>, p);
 }
 

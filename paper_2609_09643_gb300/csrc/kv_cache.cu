@@ -1,5 +1,7 @@
 // Changes of the paged cache: accepted tokens into it (unison_kv_commit), the
 // least attended ones out of it (unison_kv_evict).
+#include <cooperative_groups.h>
+
 #include "kv.cuh"
 
 namespace unison {
@@ -64,11 +66,17 @@ struct EvictParams {
   const int32_t *keep;
   int32_t sink, recent;
   bool in_place;
-  int32_t *from, *into;  // [sessions * heads][slots of a session] moves
-  int32_t *count;        // [sessions * heads]
+  int hold;        // keys that a CTA of the selection has room for
+  int per_seg;     // CTAs that move one segment's slots
+  int32_t *moves;  // [segments][slots of a session]: sources, and from the middle on targets (in place)
+  int32_t *count;  // [segments]
 };
 
-constexpr int kSelect = 1024;
+constexpr int kSelect = 512;
+constexpr int kWarps = kSelect / 32;
+constexpr int kMaxCluster = 8;
+constexpr int kBins = 2048;         // digits of 11, 11 and 10 bits
+constexpr int kMostHeld = 50 << 10;  // keys in a CTA's shared memory
 
 // Order of a slot among its session's: protected slots above all, then larger
 // mass (the bits of a float, turned so that unsigned order is the numbers'
@@ -78,9 +86,9 @@ __device__ __forceinline__ uint32_t slot_key(const EvictParams &P, int b, int h,
   const int page = kv_page(P.c, b, slot, off);
   if (page < 0) return 0;
   const int64_t m = page * P.c.m_page + h * P.c.m_head + off * P.c.m_slot;
+  const float x = P.c.mass[m] + 0.f;
   const int pos = P.c.pos ? P.c.pos[m] : slot;
   if (pos < P.sink || (int64_t)pos >= (int64_t)next - P.recent) return ~0u;
-  const float x = P.c.mass[m] + 0.f;
   if (isnan(x)) return 0;
   const uint32_t u = __float_as_uint(x);
   return u >> 31 ? ~u : u | 0x80000000u;
@@ -99,110 +107,205 @@ __device__ __forceinline__ int kept_count(const EvictParams &P, int b, int len) 
   return n;
 }
 
-// One CTA per session and head lists the moves.  The key of the last slot that
-// stays is found digit by digit (four counts of 256), then one pass in slot
-// order ranks the slots with that very key and pairs sources with targets.
+// Lists the moves of one segment (session and head); a cluster of CTAs shares
+// its slots, in order.  Every key is read once and kept in shared memory.  The
+// key of the last slot that stays is found digit by digit: each CTA counts its
+// own keys, adds up the counts of all (through distributed shared memory) and
+// finds the same digit.  Then one pass in slot order ranks the slots that have
+// that very key, one counts and one writes the moves.
 __global__ void __launch_bounds__(kSelect) evict_select_kernel(const EvictParams P) {
-  __shared__ uint32_t hist[256];
-  __shared__ uint32_t prefix, rest;
-  __shared__ int64_t part[33];
-  const int tid = threadIdx.x;
-  const int b = blockIdx.x / P.c.n_heads, h = blockIdx.x % P.c.n_heads;
+  namespace cg = cooperative_groups;
+  extern __shared__ uint32_t keys[];  // [hold]
+  __shared__ __align__(16) uint32_t hist[2][kBins];
+  __shared__ uint32_t digit, above, inside;
+  __shared__ int64_t part[33], cta_sum[2][kMaxCluster];
+  cg::cluster_group cluster = cg::this_cluster();
+  const int ctas = cluster.num_blocks(), rank = cluster.block_rank();
+  const int seg = blockIdx.x / ctas, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int b = seg / P.c.n_heads, h = seg % P.c.n_heads;
   const int len = kv_length(P.c, b);
   const int n = kept_count(P, b, len);
   const int next = P.c.pos && P.c.next_pos ? P.c.next_pos[b] : len;
   const int64_t room = (int64_t)P.c.max_pages * P.c.page_size;
-  int32_t *from = P.from + blockIdx.x * room, *into = P.into + blockIdx.x * room;
-  if (n == 0 || (P.in_place && n == len)) {
-    if (tid == 0) P.count[blockIdx.x] = 0;
+  int32_t *from = P.moves + seg * room, *into = from + room / 2;
+  if (n == 0 || (P.in_place && n == len)) {  // all CTAs of the cluster
+    if (rank == 0 && tid == 0) P.count[seg] = 0;
     return;
   }
+  // this CTA's run of the slots, and this warp's
+  const int run = ((len + ctas * kSelect - 1) / (ctas * kSelect)) * kSelect;
+  const int64_t first64 = (int64_t)rank * run;
+  const int first = (int)min(first64, (int64_t)len), last = (int)min(first64 + run, (int64_t)len);
+  auto key_of = [&](int s) { return s - first < P.hold ? keys[s - first] : slot_key(P, b, h, s, next); };
+
   uint32_t last_key = 0;  // of the slots that stay
-  int ties = 0;           // slots with that key that stay, the lowest first
+  uint32_t ties = 0;      // slots with that key that stay, the lowest first
   if (n < len) {
-    if (tid == 0) prefix = 0, rest = n;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      if (tid < 256) hist[tid] = 0;
-      __syncthreads();
-      const uint32_t have = prefix;
-      for (int s = tid; s < len; s += kSelect) {
-        const uint32_t k = slot_key(P, b, h, s, next);
-        if (shift == 24 || k >> (shift + 8) == have) atomicAdd(&hist[k >> shift & 255], 1u);
+    const int held = min(last - first, P.hold);
+#pragma unroll 4
+    for (int i = tid; i < held; i += kSelect) keys[i] = slot_key(P, b, h, first + i, next);
+    for (int i = tid; i < kBins; i += kSelect) hist[0][i] = 0;
+    __syncthreads();
+    uint32_t rest = n;
+    int shift = 21, bits = 11;
+    for (int pass = 0;; pass++) {
+      uint32_t *mine = hist[pass & 1];
+      for (int s = first + tid; s < last; s += kSelect) {
+        const uint32_t k = key_of(s);
+        if (pass == 0 || k >> (shift + bits) == last_key) atomicAdd(&mine[k >> shift & ((1u << bits) - 1)], 1u);
+      }
+      cluster.sync();
+      // four bins a thread, from the top: thread 0 has the highest
+      const int bin = kBins - 4 - 4 * tid;
+      uint4 sum = {0, 0, 0, 0};
+      for (int c = 0; c < ctas; c++) {
+        const uint4 x = *reinterpret_cast<const uint4 *>(cluster.map_shared_rank(mine, c) + bin);
+        sum.x += x.x, sum.y += x.y, sum.z += x.z, sum.w += x.w;
+      }
+      for (int i = tid; i < kBins; i += kSelect) hist[~pass & 1][i] = 0;  // of the last pass: read by all
+      int64_t all;
+      uint32_t over = (uint32_t)block_scan(sum.x + sum.y + sum.z + sum.w, part, all);
+      const uint32_t of[4] = {sum.w, sum.z, sum.y, sum.x};
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        if (over < rest && rest <= over + of[i]) {
+          digit = bin + 3 - i;
+          above = over;
+          inside = of[i];
+        }
+        over += of[i];
       }
       __syncthreads();
-      if (tid == 0) {
-        uint32_t left = rest;
-        int d = 255;
-        while (d > 0 && hist[d] < left) left -= hist[d--];
-        rest = left;
-        prefix = have << 8 | d;
+      last_key = last_key << bits | digit;
+      rest -= above;
+      if (rest == inside) {  // all with these digits stay
+        last_key = (last_key << shift) - 1;
+        break;
       }
-      __syncthreads();
-    }
-    last_key = prefix;
-    ties = (int)rest;
-  }
-  int64_t ties_seen = 0, free_seen = 0, moved = 0;
-  for (int s0 = 0; s0 < len; s0 += kSelect) {
-    const int s = s0 + tid;
-    const uint32_t k = s < len ? slot_key(P, b, h, s, next) : 0;
-    bool stays = s < len;
-    int64_t all;
-    if (n < len) {
-      const bool tie = s < len && k == last_key;
-      const int64_t rank = ties_seen + block_scan(tie, part, all);
-      ties_seen += all;
-      stays = s < len && (k > last_key || (tie && rank < ties));
-    }
-    if (P.in_place) {
-      const bool target = s < n && !stays, source = s >= n && stays;
-      const int64_t r = block_scan((int64_t)target << 32 | source, part, all);
-      if (target) into[free_seen + (r >> 32)] = s;
-      if (source) from[moved + (r & 0xFFFFFFFF)] = s;
-      free_seen += all >> 32;
-      moved += all & 0xFFFFFFFF;
-    } else {
-      const int64_t r = block_scan(stays, part, all);
-      if (stays) from[moved + r] = s;
-      moved += all;
+      if (shift == 0) {
+        ties = rest;
+        break;
+      }
+      bits = shift > 10 ? 11 : 10;
+      shift -= bits;
+      __syncthreads();  // digit, above, inside are read
     }
   }
-  if (tid == 0) P.count[blockIdx.x] = (int)(P.in_place ? min(moved, free_seen) : moved);
+
+  // The exclusive prefix over all CTAs' threads, in order, of a value that lane 0 of every warp gives.
+  int exchanges = 0;
+  auto prefix = [&](int64_t x, int64_t &all) -> int64_t {
+    const int64_t in_cta = block_scan(lane == 0 ? x : 0, part, all);
+    const int64_t before_warp = __shfl_sync(~0u, in_cta, 0);
+    if (ctas == 1) return before_warp;
+    const int slot = exchanges++ & 1;
+    if (tid < ctas) *cluster.map_shared_rank(&cta_sum[slot][rank], tid) = all;
+    cluster.sync();
+    int64_t before = 0;
+    all = 0;
+    for (int c = 0; c < ctas; c++) {
+      if (c < rank) before += cta_sum[slot][c];
+      all += cta_sum[slot][c];
+    }
+    return before + before_warp;
+  };
+  if (ctas > 1 && n == len) cluster.sync();  // every CTA has begun: its shared memory may be written to
+  const int warp_run = run / kWarps;
+  const int begin = min(first + warp * warp_run, last), end = min(begin + warp_run, last);
+  int64_t ties_before = 0, all;
+  if (ties) {
+    int64_t count = 0;
+    for (int s = begin + lane; s - lane < end; s += 32)
+      count += __popc(__ballot_sync(~0u, s < end && key_of(s) == last_key));
+    ties_before = prefix(count, all);
+  }
+  // Targets and sources of the moves in this warp's run, from the given ranks on.
+  auto moves = [&](bool write, int64_t targets, int64_t sources) -> int64_t {
+    int64_t tie = ties_before;
+    for (int s = begin + lane; s - lane < end; s += 32) {
+      bool stays = s < end;
+      if (n < len) {
+        const uint32_t k = s < end ? key_of(s) : 0;
+        bool same = false;
+        if (ties) {
+          same = s < end && k == last_key;
+          const uint32_t group = __ballot_sync(~0u, same);
+          same = same && tie + __popc(group & ((1u << lane) - 1)) < ties;
+          tie += __popc(group);
+        }
+        stays = s < end && (k > last_key || same);
+      }
+      const bool target = P.in_place && s < end && s < n && !stays, source = stays && (!P.in_place || s >= n);
+      const uint32_t t = __ballot_sync(~0u, target), f = __ballot_sync(~0u, source);
+      if (write && target) into[targets + __popc(t & ((1u << lane) - 1))] = s;
+      if (write && source) from[sources + __popc(f & ((1u << lane) - 1))] = s;
+      targets += __popc(t);
+      sources += __popc(f);
+    }
+    return targets << 32 | sources;
+  };
+  const int64_t before = prefix(moves(false, 0, 0), all);
+  moves(true, before >> 32, before & 0xFFFFFFFF);
+  if (rank == 0 && tid == 0) P.count[seg] = (int)(P.in_place ? min(all >> 32, all & 0xFFFFFFFF) : all & 0xFFFFFFFF);
 }
 
-// A warp moves one slot at a time: keys, values, mass and position.
+// Moves the listed slots: keys, values, mass and position.  A warp looks up 32
+// moves at once, a lane each, and then copies them row by row.
 template <typename T>
 __global__ void __launch_bounds__(256) evict_move_kernel(const EvictParams P) {
-  const int seg = blockIdx.y, lane = threadIdx.x & 31;
+  const int seg = blockIdx.x / P.per_seg, of_seg = blockIdx.x % P.per_seg, lane = threadIdx.x & 31;
   const int b = seg / P.c.n_heads, h = seg % P.c.n_heads;
   const int chunks = P.c.head_dim / 8;
   const int64_t room = (int64_t)P.c.max_pages * P.c.page_size;
-  const int32_t *from = P.from + seg * room, *into = P.into + seg * room;
+  const int32_t *from = P.moves + seg * room, *into = from + room / 2;
   const int count = P.count[seg];
-  const int warps = gridDim.x * (blockDim.x >> 5);
-  for (int i = blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5); i < count; i += warps) {
-    int off, to_off;
-    const int page = kv_page(P.c, b, from[i], off);
-    const int to_page = kv_page(P.to, b, P.in_place ? into[i] : i, to_off);
-    if (page < 0 || to_page < 0) continue;
-    const T *k = static_cast<const T *>(P.c.k) + page * P.c.k_page + h * P.c.k_head + off * P.c.k_slot;
-    const T *v = static_cast<const T *>(P.c.v) + page * P.c.v_page + h * P.c.v_head + off * P.c.v_slot;
-    T *tk = static_cast<T *>(P.to.k) + to_page * P.to.k_page + h * P.to.k_head + to_off * P.to.k_slot;
-    T *tv = static_cast<T *>(P.to.v) + to_page * P.to.v_page + h * P.to.v_head + to_off * P.to.v_slot;
-    for (int c = lane; c < 2 * chunks; c += 32) {
-      if (c < chunks)
-        reinterpret_cast<int4 *>(tk)[c] = reinterpret_cast<const int4 *>(k)[c];
-      else
-        reinterpret_cast<int4 *>(tv)[c - chunks] = reinterpret_cast<const int4 *>(v)[c - chunks];
+  const int warps = P.per_seg * (blockDim.x >> 5);
+  const int width = 2 * chunks;
+  const unsigned reciprocal = ((1u << 20) + width - 1) / width;
+  const T *k = static_cast<const T *>(P.c.k) + h * P.c.k_head, *v = static_cast<const T *>(P.c.v) + h * P.c.v_head;
+  T *to_k = static_cast<T *>(P.to.k) + h * P.to.k_head, *to_v = static_cast<T *>(P.to.v) + h * P.to.v_head;
+  for (int i0 = (of_seg * (blockDim.x >> 5) + (threadIdx.x >> 5)) * 32; i0 < count; i0 += warps * 32) {
+    int page = -1, to_page = -1, off = 0, to_off = 0;
+    if (i0 + lane < count) {
+      page = kv_page(P.c, b, from[i0 + lane], off);
+      to_page = kv_page(P.to, b, P.in_place ? into[i0 + lane] : i0 + lane, to_off);
     }
-    if (lane == 0) {
+    if (page < 0 || to_page < 0) page = to_page = -1;
+    if (page >= 0) {
       const int64_t m = page * P.c.m_page + h * P.c.m_head + off * P.c.m_slot;
       const int64_t tm = to_page * P.to.m_page + h * P.to.m_head + to_off * P.to.m_slot;
       if (P.to.mass) P.to.mass[tm] = P.c.mass[m];
       if (P.to.pos && P.c.pos) P.to.pos[tm] = P.c.pos[m];
     }
+    // 16 bytes a lane: entry e is chunk e % width of row e / width (the keys'
+    // chunks, then the values'); e < 2^11, so the division by multiplication is exact
+    constexpr int kFlight = 8;  // loads of a lane on their way at once
+    const int entries = min(count - i0, 32) * width;
+    for (int e0 = 0; e0 < entries; e0 += 32 * kFlight) {
+      int4 x[kFlight];
+      T *dst[kFlight];
+#pragma unroll
+      for (int i = 0; i < kFlight; i++) {
+        const int e = e0 + i * 32 + lane;
+        const int row = (int)((unsigned)e * reciprocal >> 20) & 31, c = e - row * width;
+        const bool key = c < chunks;
+        const int64_t p = __shfl_sync(~0u, page, row), o = __shfl_sync(~0u, off, row);
+        const int64_t tp = __shfl_sync(~0u, to_page, row), to = __shfl_sync(~0u, to_off, row);
+        dst[i] = nullptr;
+        if (e < entries && p >= 0) {
+          const T *src = key ? k + p * P.c.k_page + o * P.c.k_slot + c * 8
+                             : v + p * P.c.v_page + o * P.c.v_slot + (c - chunks) * 8;
+          dst[i] = key ? to_k + tp * P.to.k_page + to * P.to.k_slot + c * 8
+                       : to_v + tp * P.to.v_page + to * P.to.v_slot + (c - chunks) * 8;
+          x[i] = *reinterpret_cast<const int4 *>(src);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kFlight; i++)
+        if (dst[i]) *reinterpret_cast<int4 *>(dst[i]) = x[i];
+    }
   }
-  if (blockIdx.x == 0 && h == 0 && threadIdx.x == 0) {
+  if (of_seg == 0 && h == 0 && threadIdx.x == 0) {
     P.to.length[b] = kept_count(P, b, kv_length(P.c, b));
     if (!P.in_place && P.to.next_pos && P.c.next_pos) P.to.next_pos[b] = P.c.next_pos[b];
   }
@@ -210,7 +313,7 @@ __global__ void __launch_bounds__(256) evict_move_kernel(const EvictParams P) {
 
 uint64_t evict_bytes(const unison_kv_cache *c) {
   const uint64_t segs = (uint64_t)c->n_seqs * c->n_heads;
-  return segs * 4 + 2 * segs * c->max_pages * c->page_size * 4;
+  return segs * 4 + segs * c->max_pages * c->page_size * 4;
 }
 
 }  // namespace
@@ -236,7 +339,7 @@ extern "C" int unison_kv_commit(const unison_kv_cache *cache, const unison_kv_tr
   if (path && path->path && (!path->n_path || path->path_stride < 0)) return UNISON_ERR_ARG;
   const CommitParams p = {*cache, *tree, *step, path ? *path : unison_kv_path{}};
   // 16-bit types move as they are
-  return kv_launch("kv_commit", dim3(cache->n_seqs), dim3(256), 0, cuda_stream, false, commit_kernel<uint16_t>, p);
+  return kv_launch("kv_commit", dim3(cache->n_seqs), dim3(256), 0, cuda_stream, 1, commit_kernel<uint16_t>, p);
 }
 
 extern "C" uint64_t unison_kv_evict_workspace(const unison_kv_cache *cache) {
@@ -257,11 +360,12 @@ extern "C" int unison_kv_evict(const unison_kv_cache *cache, const unison_kv_cac
   }
   if (sink < 0 || recent < 0) return UNISON_ERR_RANGE;
   const uint64_t segs = (uint64_t)cache->n_seqs * cache->n_heads;
-  if (segs > 65535) return UNISON_ERR_RANGE;
+  if (segs > 1 << 22) return UNISON_ERR_RANGE;
   if (cache->n_seqs == 0) return UNISON_OK;
   if (!keep || !pools_ok(cache) || (into && !pools_ok(into))) return UNISON_ERR_ARG;
   if (cache->max_pages > 0 && cache->n_pages > 0 && !cache->mass) return UNISON_ERR_ARG;
   if (!workspace || !kv_aligned(workspace, 16) || workspace_bytes < evict_bytes(cache)) return UNISON_ERR_ARG;
+  const int64_t room = (int64_t)cache->max_pages * cache->page_size;
   EvictParams p;
   p.c = *cache;
   p.to = into ? *into : *cache;
@@ -269,12 +373,23 @@ extern "C" int unison_kv_evict(const unison_kv_cache *cache, const unison_kv_cac
   p.sink = sink;
   p.recent = recent;
   p.in_place = into == nullptr;
-  p.from = static_cast<int32_t *>(workspace);
-  p.into = p.from + segs * cache->max_pages * cache->page_size;
-  p.count = p.into + segs * cache->max_pages * cache->page_size;
-  rc = kv_launch("kv_evict_select", dim3((unsigned)segs), dim3(kSelect), 0, cuda_stream, false, evict_select_kernel, p);
+  p.moves = static_cast<int32_t *>(workspace);
+  p.count = p.moves + segs * room;
+  // CTAs per segment: as many as the segments leave room for (four CTAs on a
+  // multiprocessor), none with less than 2,048 slots.
+  const int64_t spare = (int64_t)kv_sm_count() * 4 / (int64_t)segs;
+  int ctas = 1;
+  while (ctas < kMaxCluster && ctas * 2 <= spare && (int64_t)ctas * 2048 < room) ctas *= 2;
+  p.hold = (int)min((room + ctas - 1) / ctas + kSelect, (int64_t)kMostHeld);
+  static uint64_t done = 0;
+  if (!kv_allow_smem(reinterpret_cast<const void *>(evict_select_kernel), kMostHeld * 4, &done)) return UNISON_ERR_CUDA;
+  rc = kv_launch("kv_evict_select", dim3((unsigned)(segs * ctas)), dim3(kSelect), p.hold * 4, cuda_stream, ctas,
+                 evict_select_kernel, p);
   if (rc != UNISON_OK) return rc;
-  const unsigned per_seg = (unsigned)max((uint64_t)1, ((uint64_t)kv_sm_count() * 8 + segs - 1) / segs);
-  return kv_launch("kv_evict_move", dim3(per_seg, (unsigned)segs), dim3(256), 0, cuda_stream, false,
+  // a CTA moves 256 slots at a time
+  const int64_t most = into ? min(room, (int64_t)into->max_pages * into->page_size) : room / 2;
+  const int64_t fill = ((int64_t)kv_sm_count() * 32 + segs - 1) / (int64_t)segs;
+  p.per_seg = (int)max((int64_t)1, min((most + 255) / 256, fill));
+  return kv_launch("kv_evict_move", dim3((unsigned)(segs * p.per_seg)), dim3(256), 0, cuda_stream, 1,
                    evict_move_kernel<uint16_t>, p);
 }

@@ -244,7 +244,7 @@ int observe_run(const ObserveParams &p, void *stream) {
   constexpr int smem = kObserveSmem<DP, QR>;
   if (!kv_allow_smem(reinterpret_cast<const void *>(observe_kernel<T, DP, QR>), smem, &done)) return UNISON_ERR_CUDA;
   const int per_sm = max(1, min(4, (220 << 10) / (smem + QR * 12 + 5000)));
-  return kv_launch("kv_observe", dim3(kv_sm_count() * per_sm), dim3(kThreads), smem, stream, false,
+  return kv_launch("kv_observe", dim3(kv_sm_count() * per_sm), dim3(kThreads), smem, stream, 1,
                    observe_kernel<T, DP, QR>, p);
 }
 

@@ -1,10 +1,23 @@
 // Verification of drafted tokens (unison_kv_verify).
+//
+// What a walk needs of the vocabulary rows is little until a draft is refused:
+// p and q at the drafted tokens, which one round of loads fetches for all
+// nodes at once.  Only a refusal (the sum of what is left) and the last sample
+// read whole rows.  A cluster of CTAs shares the rows of one session: CTA r
+// has a run of the vocabulary, each of its warps a run of that.  A pass over
+// the rows is one stream of loads, one exchange of the CTAs' sums and one
+// cluster barrier.
+#include <cooperative_groups.h>
+
 #include "kv.cuh"
 
 namespace unison {
 namespace {
 
-constexpr int kThreads = 1024;
+constexpr int kThreads = 512;
+constexpr int kWarps = kThreads / 32;
+constexpr int kMaxCluster = 8;
+constexpr int kUnroll = 8;                // loads in flight of a lane, from each of the two rows
 constexpr float kUnit = 1099511627776.f;  // 2^40
 
 __device__ __forceinline__ float weight(float x) { return x > 0.f ? fminf(x, 1.f) : 0.f; }
@@ -16,132 +29,176 @@ template <>
 __device__ __forceinline__ float load<float>(const float *p, int64_t i) {
   return p[i];
 }
+__device__ __forceinline__ int64_t fixed(float d) { return __float2ll_rz(__fmul_rn(d, kUnit)); }
 
-// d at one vocabulary entry after the rejections of the current node: z[0 ..
-// n-1] the sums before each of them; without q, the tokens that were taken out.
-struct Residual {
+// The refusals at the current node: z[i] the sum before refusal i, token[i]
+// the refused token.
+struct Refused {
   float z[UNISON_KV_MAX_TOKENS];
   int token[UNISON_KV_MAX_TOKENS];
-  int n;
 };
-template <typename T>
-__device__ __forceinline__ float residual(const Residual &r, const T *p, const T *q, int x, int n) {
-  float d = weight(load(p, x));
-  if (q) {
-    const float y = weight(load(q, x));
-    for (int i = 0; i < n; i++) d = fmaxf(__fsub_rn(d, __fmul_rn(r.z[i], y)), 0.f);
-  } else {
-    for (int i = 0; i < n; i++)
-      if (r.token[i] == x) d = 0.f;
+// d at entry x, whose first weight is d and whose draft weight is y, after n refusals.
+template <bool kCertain>
+__device__ __forceinline__ float residual(const Refused &r, float d, float y, int x, int n) {
+  for (int i = 0; i < n; i++) {
+    if (kCertain)
+      d = r.token[i] == x ? 0.f : d;
+    else
+      d = fmaxf(__fsub_rn(d, __fmul_rn(r.z[i], y)), 0.f);
   }
   return d;
 }
-__device__ __forceinline__ int64_t fixed(float d) { return __float2ll_rz(__fmul_rn(d, kUnit)); }
 
-// One CTA per session.  Warp w owns entries [w * span, (w + 1) * span).
-template <typename T>
+// kCertain: without q.
+template <typename T, bool kCertain>
 __global__ void __launch_bounds__(kThreads) verify_kernel(const unison_kv_tree t, const unison_kv_verify_args a) {
-  __shared__ Residual res;
-  __shared__ int64_t sums[32];
-  __shared__ int chosen;
-  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  namespace cg = cooperative_groups;
+  __shared__ Refused refused;
+  __shared__ int node_parent[UNISON_KV_MAX_TOKENS], node_token[UNISON_KV_MAX_TOKENS];
+  __shared__ float node_u[UNISON_KV_MAX_TOKENS], node_d[UNISON_KV_MAX_TOKENS], node_y[UNISON_KV_MAX_TOKENS];
+  __shared__ int64_t warp_sum[kWarps], cta_sum[2][kMaxCluster], part[33];
+  cg::cluster_group cluster = cg::this_cluster();
+  const int ctas = cluster.num_blocks(), rank = cluster.block_rank();
+  const int b = blockIdx.x / ctas, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const KvRange tok = kv_tokens(t, b, nullptr);
   int32_t *path = a.path + b * a.path_stride;
-  if (tok.count == 0) {
-    for (int i = tid; i < t.max_tokens; i += kThreads) path[i] = -1;
-    if (tid == 0) {
-      a.n_path[b] = 0;
-      a.next_token[b] = -1;
+  if (tok.count == 0) {  // all CTAs of the cluster
+    if (rank == 0) {
+      if (tid < t.max_tokens) path[tid] = -1;
+      if (tid == 0) {
+        a.n_path[b] = 0;
+        a.next_token[b] = -1;
+      }
     }
     return;
   }
   const int V = a.vocab;
-  const int span = (V + kThreads / 32 - 1) / (kThreads / 32);
-  const T *p = nullptr, *q = nullptr;
-  int cur = 0, n = 1, rejected = 0;
-  float z = 1.f;
-  auto enter = [&](int node) {
-    cur = node;
-    p = static_cast<const T *>(a.p) + (int64_t)(tok.first + node) * a.p_row;
-    q = a.q ? static_cast<const T *>(a.q) + (int64_t)(tok.first + node) * a.q_row : nullptr;
-    rejected = 0;
-    z = 1.f;
-  };
-  // the sum of the residual after n rejections, every warp's share in sums[]
-  auto total = [&](int n) -> int64_t {
+  const T *const rows_p = static_cast<const T *>(a.p) + tok.first * a.p_row;
+  const T *const rows_q = kCertain ? nullptr : static_cast<const T *>(a.q) + tok.first * a.q_row;
+  if (tid < tok.count) {
+    int parent = t.parent[tok.first + tid];
+    const int token = a.token[tok.first + tid];
+    if (tid == 0 || parent < 0 || parent >= tid || (unsigned)token >= (unsigned)V) parent = -1;  // never reached
+    node_parent[tid] = parent;
+    node_token[tid] = token;
+    node_u[tid] = a.u[tok.first + tid];
+    if (parent >= 0) {
+      node_d[tid] = weight(load(rows_p + parent * a.p_row, token));
+      node_y[tid] = kCertain ? 1.f : weight(load(rows_q + parent * a.q_row, token));
+    }
+  }
+  cluster.sync();  // every CTA has begun: its shared memory may be written to
+
+  // this warp's run of the vocabulary, in whole groups of 32 entries
+  const int span = (((V + ctas * kWarps - 1) / (ctas * kWarps)) + 31) & ~31;
+  const int64_t begin64 = (int64_t)(rank * kWarps + warp) * span;
+  const int begin = (int)min(begin64, (int64_t)V), end = (int)min(begin64 + span, (int64_t)V);
+  int passes = 0;
+  // The sum over all entries of the residual after n refusals at node `cur`.
+  auto total = [&](int cur, int n) -> int64_t {
+    const T *p = rows_p + cur * a.p_row, *q = kCertain || n == 0 ? nullptr : rows_q + cur * a.q_row;
     int64_t s = 0;
-    for (int x = warp * span + lane; x < min((warp + 1) * span, V); x += 32) s += fixed(residual(res, p, q, x, n));
+    for (int x0 = begin + lane; x0 < end; x0 += 32 * kUnroll) {
+      float d[kUnroll], y[kUnroll];
+#pragma unroll
+      for (int i = 0; i < kUnroll; i++) {
+        const int x = x0 + i * 32;
+        d[i] = x < end ? load(p, x) : 0.f;
+        y[i] = q && x < end ? load(q, x) : 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < kUnroll; i++)
+        s += fixed(residual<kCertain>(refused, weight(d[i]), weight(y[i]), x0 + i * 32, n));
+    }
 #pragma unroll
     for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(~0u, s, d);
+    if (lane == 0) warp_sum[warp] = s;
     __syncthreads();
-    if (lane == 0) sums[warp] = s;
-    __syncthreads();
+    const int slot = passes++ & 1;  // a CTA that is one pass ahead writes the other one
+    if (tid < ctas) {
+      int64_t mine = 0;
+      for (int w = 0; w < kWarps; w++) mine += warp_sum[w];
+      *cluster.map_shared_rank(&cta_sum[slot][rank], tid) = mine;
+    }
+    cluster.sync();
     int64_t all = 0;
-    for (int w = 0; w < kThreads / 32; w++) all += sums[w];
+    for (int c = 0; c < ctas; c++) all += cta_sum[slot][c];
     return all;
   };
-  enter(0);
-  if (tid == 0) path[0] = 0;
-  int64_t left = -1;  // sum of the current residual, -1: not known
+
+  int cur = 0, n = 1, count = 0;  // node, accepted nodes, refusals at this node
+  float z = 1.f;
+  int64_t left = -1;  // sum of the residual, -1: not known
+  if (rank == 0 && tid == 0) path[0] = 0;
   for (int i = 1; i < tok.count; i++) {
-    if (t.parent[tok.first + i] != cur) continue;
-    const int token = a.token[tok.first + i];
-    if ((unsigned)token >= (unsigned)V) continue;
-    const float d = residual(res, p, q, token, rejected);
-    const float y = q ? weight(load(q, token)) : 1.f;
-    const float u = a.u[tok.first + i];
-    if (__fmul_rn(__fmul_rn(u, y), z) < d) {
-      enter(i);
+    if (node_parent[i] != cur) continue;
+    const float y = node_y[i];
+    const float d = residual<kCertain>(refused, node_d[i], y, node_token[i], count);
+    if (__fmul_rn(__fmul_rn(node_u[i], y), z) < d) {
+      cur = i;
+      count = 0;
+      z = 1.f;
       left = -1;
-      if (tid == 0) path[n] = i;
+      if (rank == 0 && tid == 0) path[n] = i;
       n++;
     } else {
       __syncthreads();
       if (tid == 0) {
-        res.z[rejected] = z;
-        res.token[rejected] = token;
+        refused.z[count] = z;
+        refused.token[count] = node_token[i];
       }
       __syncthreads();
-      rejected++;
-      left = total(rejected);
+      left = total(cur, ++count);
       z = __fmul_rn((float)left, 1.f / kUnit);
     }
   }
-  if (left < 0) left = total(0);
-  if (left == 0) {
-    rejected = 0;
-    left = total(0);
-  }
-  for (int i = n + tid; i < t.max_tokens; i += kThreads) path[i] = -1;
-  if (tid == 0) {
-    a.n_path[b] = n;
-    chosen = -1;
-  }
-  __syncthreads();
-  // floor(u W) with u a multiple of 2^-24 and W below 2^62
-  const int64_t u = (int64_t)(a.u_sample[b] * 16777216.f);
-  const int64_t goal = u * (left >> 24) + ((u * (left & 0xFFFFFF)) >> 24);
-  int64_t before = 0;
-  for (int w = 0; w < warp; w++) before += sums[w];
-  if (left > 0 && before <= goal && goal < before + sums[warp]) {  // one warp: the entry is in its share
-    for (int x0 = warp * span; x0 < min((warp + 1) * span, V); x0 += 32) {
-      const int x = x0 + lane;
-      int64_t s = x < min((warp + 1) * span, V) ? fixed(residual(res, p, q, x, rejected)) : 0;
-#pragma unroll
-      for (int d = 1; d < 32; d <<= 1) {
-        const int64_t y = __shfl_up_sync(~0u, s, d);
-        if (lane >= d) s += y;
-      }
-      const uint32_t past = __ballot_sync(~0u, before + s > goal);
-      if (past) {
-        if (lane == 0) chosen = x0 + __ffs(past) - 1;
-        break;
-      }
-      before += __shfl_sync(~0u, s, 31);
+  if (left <= 0) left = total(cur, count = 0);
+  if (rank == 0) {
+    if (tid >= n && tid < t.max_tokens) path[tid] = -1;
+    if (tid == 0) {
+      a.n_path[b] = n;
+      if (left <= 0) a.next_token[b] = -1;
     }
   }
-  __syncthreads();
-  if (tid == 0) a.next_token[b] = chosen;
+  // floor(u W) with u a multiple of 2^-24 and W below 2^62
+  const int64_t u = (int64_t)(fminf(fmaxf(a.u_sample[b], 0.f), 1.f - 1.f / 16777216.f) * 16777216.f);
+  const int64_t goal = u * (left >> 24) + ((u * (left & 0xFFFFFF)) >> 24);
+  // the CTA, the warp's run and then the entry in which the running sum passes the goal
+  int64_t before = 0;
+  const int slot = (passes - 1) & 1;
+  for (int c = 0; c < rank; c++) before += cta_sum[slot][c];
+  if (!(left > 0 && before <= goal && goal < before + cta_sum[slot][rank])) return;
+  int w = 0;
+  while (w < kWarps - 1 && before + warp_sum[w] <= goal) before += warp_sum[w++];
+  const int lo = (rank * kWarps + w) * span, hi = min(lo + span, V);
+  const int each = span / kThreads + 1;
+  const T *p = rows_p + cur * a.p_row, *q = kCertain || count == 0 ? nullptr : rows_q + cur * a.q_row;
+  auto entry = [&](int x) -> int64_t {
+    return fixed(residual<kCertain>(refused, weight(load(p, x)), q ? weight(load(q, x)) : 0.f, x, count));
+  };
+  const int x0 = lo + tid * each, x1 = min(x0 + each, hi);
+  int64_t mine = 0, all;
+  for (int x = x0; x < x1; x++) mine += entry(x);
+  before += block_scan(mine, part, all);
+  if (before <= goal && goal < before + mine) {  // one thread
+    int x = x0;
+    for (; x < x1 - 1; x++) {
+      before += entry(x);
+      if (before > goal) break;
+    }
+    a.next_token[b] = x;
+  }
+}
+
+template <typename T>
+int verify_run(const unison_kv_tree &t, const unison_kv_verify_args &a, void *stream) {
+  // CTAs per session: as many as the sessions leave room for (two CTAs on a
+  // multiprocessor), none with less than 2,048 entries.
+  const int room = 2 * kv_sm_count() / t.n_seqs, wanted = (a.vocab + 2047) / 2048;
+  int ctas = 1;
+  while (ctas < kMaxCluster && ctas * 2 <= max(room, 1) && ctas < wanted) ctas *= 2;
+  return kv_launch("kv_verify", dim3(t.n_seqs * ctas), dim3(kThreads), 0, stream, ctas,
+                   a.q ? verify_kernel<T, false> : verify_kernel<T, true>, t, a);
 }
 
 }  // namespace
@@ -158,14 +215,10 @@ extern "C" int unison_kv_verify(const unison_kv_tree *tree, const unison_kv_veri
   if (!args->path || !args->n_path || !args->next_token || !args->u_sample || args->path_stride < tree->max_tokens)
     return UNISON_ERR_ARG;
   if (tree->n_tokens > 0 && (!args->p || !args->token || !args->u || !tree->parent)) return UNISON_ERR_ARG;
-  const dim3 grid(tree->n_seqs), block(kThreads);
   switch (args->dtype) {
-    case UNISON_KV_FP32:
-      return kv_launch("kv_verify", grid, block, 0, cuda_stream, false, verify_kernel<float>, *tree, *args);
-    case UNISON_KV_BF16:
-      return kv_launch("kv_verify", grid, block, 0, cuda_stream, false, verify_kernel<__nv_bfloat16>, *tree, *args);
-    case UNISON_KV_FP16:
-      return kv_launch("kv_verify", grid, block, 0, cuda_stream, false, verify_kernel<__half>, *tree, *args);
+    case UNISON_KV_FP32: return verify_run<float>(*tree, *args, cuda_stream);
+    case UNISON_KV_BF16: return verify_run<__nv_bfloat16>(*tree, *args, cuda_stream);
+    case UNISON_KV_FP16: return verify_run<__half>(*tree, *args, cuda_stream);
     default: return UNISON_ERR_ARG;
   }
 }
