@@ -47,8 +47,11 @@ int kv_sm_count();
 // (`done`: a bit per device, kept by the caller beside the kernel).
 bool kv_allow_smem(const void *kernel, int bytes, uint64_t *done);
 
-// Queues a kernel of clusters of `cluster` CTAs.  The verdict is the launch's
-// own, not an older error's.
+// Queues a kernel of clusters of `cluster` CTAs.  kAfterLast instead: a kernel
+// that may be set up while the one before it on the stream ends, and calls
+// wait_for_last_kernel before it reads that one's results.  The verdict is the
+// launch's own, not an older error's.
+constexpr int kAfterLast = 0;
 template <typename... P, typename... A>
 int kv_launch(const char *name, dim3 grid, dim3 block, size_t smem, void *stream, int cluster, void (*kernel)(P...),
               A &&...args) {
@@ -61,12 +64,17 @@ int kv_launch(const char *name, dim3 grid, dim3 block, size_t smem, void *stream
     lc.dynamicSmemBytes = smem;
     lc.stream = static_cast<cudaStream_t>(stream);
     cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = cluster;
-    at[0].val.clusterDim.y = 1;
-    at[0].val.clusterDim.z = 1;
+    if (cluster == kAfterLast) {
+      at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+      at[0].val.programmaticStreamSerializationAllowed = 1;
+    } else {
+      at[0].id = cudaLaunchAttributeClusterDimension;
+      at[0].val.clusterDim.x = cluster;
+      at[0].val.clusterDim.y = 1;
+      at[0].val.clusterDim.z = 1;
+    }
     lc.attrs = at;
-    lc.numAttrs = cluster > 1 ? 1 : 0;
+    lc.numAttrs = cluster == 1 ? 0 : 1;
     e = cudaLaunchKernelEx(&lc, kernel, static_cast<P>(args)...);
   }
   count_launches(1);
@@ -125,6 +133,8 @@ __device__ __forceinline__ int kv_page(const unison_kv_cache &c, int b, int slot
   return -1;
 }
 
+__device__ __forceinline__ void wait_for_last_kernel() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 __device__ __forceinline__ uint32_t smem_u32(const void *p) {
   return static_cast<uint32_t>(__cvta_generic_to_shared(p));
 }
@@ -181,21 +191,6 @@ __device__ __forceinline__ uint32_t swizzled(uint32_t base, int row, int chunk) 
 }
 
 // ------------------------------------------------- sharing out the tiles --
-// The work of a call is a list of key tiles: session by session, KV head by
-// head, row tile by row tile, key tile by key tile.  Every CTA takes an equal
-// run of it, whatever the sessions' lengths are; a run may begin and end
-// inside a segment (one session, head and row tile).
-struct KvWalk {
-  int b;          // session
-  int64_t begin;  // index of its first tile in the list
-};
-
-// Tiles of one session.
-template <int kTile>
-__device__ __forceinline__ int kv_key_tiles(int len, int tokens) {
-  return tokens ? (len + kTile - 1) / kTile + 1 : 0;  // the last one holds the new tokens
-}
-
 // All threads of a CTA add their values; every thread gets the exclusive
 // prefix and the sum.  `part`: 33 words of shared memory.
 __device__ __forceinline__ int64_t block_scan(int64_t x, int64_t *part, int64_t &total) {
@@ -209,18 +204,76 @@ __device__ __forceinline__ int64_t block_scan(int64_t x, int64_t *part, int64_t 
   __syncthreads();
   if (lane == 31) part[warp] = y;
   __syncthreads();
-  if (threadIdx.x == 0) {
-    int64_t s = 0;
-    for (int w = 0; w < warps; w++) {
-      const int64_t v = part[w];
-      part[w] = s;
-      s += v;
+  if (warp == 0) {
+    const int64_t mine = lane < warps ? part[lane] : 0;
+    int64_t s = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int64_t z = __shfl_up_sync(~0u, s, d);
+      if (lane >= d) s += z;
     }
-    part[32] = s;
+    __syncwarp();
+    part[lane] = s - mine;
+    if (lane == 31) part[32] = s;
   }
   __syncthreads();
   total = part[32];
   return part[warp] + y - x;
+}
+
+// The work of a call is a list of key tiles, session by session.  Every run
+// (one CTA, or a few that share its keys) takes an equal stretch of the list,
+// whatever the sessions' lengths are.
+struct KvRun {
+  int64_t total;  // tiles of the call
+  int runs;       // that have work: one tile at least
+  int64_t at, end;
+  int b;          // the session that `at` lies in
+  int64_t begin;  // index of its first tile
+};
+struct KvRunShared {
+  int64_t part[33], begin;
+  int b;
+};
+// By all threads of a CTA.  tiles(b): tiles of session b.  False: no work.
+template <typename F>
+__device__ __forceinline__ bool kv_find_run(KvRun &r, KvRunShared &sh, int n_seqs, int runs, int run, F tiles) {
+  const int tid = threadIdx.x, step = blockDim.x;
+  int64_t mine = tid < n_seqs ? tiles(tid) : 0, n;
+  int64_t before = block_scan(mine, sh.part, n);
+  r.total = n;
+  for (int b0 = step; b0 < n_seqs; b0 += step) {
+    block_scan(b0 + tid < n_seqs ? tiles(b0 + tid) : 0, sh.part, n);
+    r.total += n;
+  }
+  r.runs = (int)min((int64_t)runs, r.total);
+  if (run >= r.runs) return false;
+  r.at = r.total * run / r.runs;
+  r.end = r.total * (run + 1) / r.runs;
+  int64_t sum = 0;
+  for (int b0 = 0;; b0 += step) {
+    if (n_seqs > step) {  // else the first values still stand
+      mine = b0 + tid < n_seqs ? tiles(b0 + tid) : 0;
+      before = sum + block_scan(mine, sh.part, n);
+    }
+    if (r.at >= before && r.at < before + mine) {
+      sh.b = b0 + tid;
+      sh.begin = before;
+    }
+    sum += n_seqs > step ? n : r.total;
+    if (r.at < sum) break;
+  }
+  __syncthreads();
+  r.b = sh.b;
+  r.begin = sh.begin;
+  return true;
+}
+// The run in whose stretch a tile lies.
+__device__ __forceinline__ int kv_run_of(const KvRun &r, int64_t tile) {
+  int c = (int)min((tile + 1) * r.runs / r.total, (int64_t)r.runs - 1);  // about right: the exact one is a step away
+  while (c > 0 && r.total * c / r.runs > tile) c--;
+  while (r.total * (c + 1) / r.runs <= tile) c++;
+  return c;
 }
 
 }  // namespace unison

@@ -1,26 +1,11 @@
 // Attention of drafted tokens over the paged cache (unison_kv_attend).
-#include "kv.cuh"
+#include "kv_attend.cuh"
 
 namespace unison {
 namespace {
 
 constexpr int kThreads = 128;
 constexpr int kTile = 64;  // keys of a tile
-
-struct AttendParams {
-  unison_kv_cache c;
-  unison_kv_tree t;
-  unison_kv_step s;
-  float *partial;  // [grid][2][rows][DP + 2]
-  struct AttendPart *part;  // [grid]
-  int group;
-};
-
-// What a CTA leaves to be joined: the segment that begins in its run and goes
-// on in the runs of the CTAs up to `last`.
-struct AttendPart {
-  int b, head, row_tile, last;  // last < 0: nothing
-};
 
 template <int DP>
 constexpr int kAttendStages = DP <= 128 ? 3 : 2;
@@ -38,9 +23,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) attend_kernel(con
   constexpr int kWarpKeys = kTile / kGroups;
   constexpr int kChunks = DP / 8;
   extern __shared__ __align__(128) unsigned char smem[];
-  __shared__ int64_t scan_part[33];
-  __shared__ int found_b;
-  __shared__ int64_t found_begin;
+  __shared__ KvRunShared shared_run;
   __shared__ const T *row_k[2][kTile], *row_v[2][kTile];
   __shared__ uint32_t row_ok[8][2];
   __shared__ float merge_m[4][16], merge_l[4][16];
@@ -55,34 +38,13 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) attend_kernel(con
   auto seq_tiles = [&](int b) -> int64_t {
     const int tokens = kv_tokens(P.t, b, P.c.status).count;
     const int row_tiles = (tokens * G + kRows - 1) / kRows;
-    return (int64_t)kv_key_tiles<kTile>(kv_length(P.c, b), tokens) * row_tiles * H;
+    return (int64_t)attend_key_tiles(kv_length(P.c, b), tokens, kTile) * row_tiles * H;
   };
-  // all tiles, then the session in which this CTA's run begins
-  int64_t total = 0;
-  for (int b0 = 0; b0 < P.c.n_seqs; b0 += kThreads) {
-    int64_t n;
-    block_scan(b0 + tid < P.c.n_seqs ? seq_tiles(b0 + tid) : 0, scan_part, n);
-    total += n;
-  }
-  const int grid = (int)min((int64_t)gridDim.x, total);  // CTAs that have work: one tile at least
-  if ((int)blockIdx.x >= grid) return;
-  int64_t at = total * blockIdx.x / grid;
-  const int64_t end = total * (blockIdx.x + 1) / grid;
-  int64_t sum = 0;
-  for (int b0 = 0; b0 < P.c.n_seqs; b0 += kThreads) {
-    const int64_t mine = b0 + tid < P.c.n_seqs ? seq_tiles(b0 + tid) : 0;
-    int64_t n;
-    const int64_t before = sum + block_scan(mine, scan_part, n);
-    if (at >= before && at < before + mine) {
-      found_b = b0 + tid;
-      found_begin = before;
-    }
-    sum += n;
-    if (at < sum) break;
-  }
-  __syncthreads();
-  int b = found_b;
-  int64_t seq_begin = found_begin;
+  KvRun run;
+  if (!kv_find_run(run, shared_run, P.c.n_seqs, gridDim.x, blockIdx.x, seq_tiles)) return;
+  int b = run.b;
+  int64_t at = run.at, seq_begin = run.begin;
+  const int64_t end = run.end;
 
   while (at < end) {
     // ---- the segment that `at` lies in
@@ -93,7 +55,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) attend_kernel(con
     }
     const KvRange tok = kv_tokens(P.t, b, nullptr);
     const int len = kv_length(P.c, b);
-    const int key_tiles = kv_key_tiles<kTile>(len, tok.count);
+    const int key_tiles = attend_key_tiles(len, tok.count, kTile);
     const int row_tiles = (tok.count * G + kRows - 1) / kRows;
     const int64_t rel = at - seq_begin;
     const int seg = (int)(rel / key_tiles);
@@ -320,6 +282,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) attend_kernel(con
     const bool whole = kt0 == 0 && kt1 == key_tiles;
     const bool starts = kt0 == 0;
     float *part = P.partial + ((int64_t)blockIdx.x * 2 + (starts ? 1 : 0)) * (kRows * (DP + 2));
+    float *part_m = part + kRows * DP, *part_l = part_m + kRows;
     for (int i = tid; i < kRows * (DP / 2); i += kThreads) {
       const int r = i / (DP / 2), d = i % (DP / 2) * 2;
       if (r >= rows || d >= D) continue;
@@ -353,78 +316,125 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) attend_kernel(con
           P.s.lse[(int64_t)(tok.first + node) * P.s.n_q_heads + head * G + row % G] =
               (top + log2f(l)) * 0.6931471805599453f;
       } else {
-        part[r * (DP + 2) + d] = x;
-        part[r * (DP + 2) + d + 1] = y;
+        *reinterpret_cast<float2 *>(part + r * DP + d) = make_float2(x, y);
         if (d == 0) {
-          part[r * (DP + 2) + DP] = top;
-          part[r * (DP + 2) + DP + 1] = l;
+          part_m[r] = top;
+          part_l[r] = l;
         }
       }
     }
-    if (starts && !whole && tid == 0) {
-      // the CTA in whose run the segment's last tile lies
-      const int64_t tile = seg_begin + key_tiles - 1;
-      int c = (int)((tile + 1) * grid / total);  // about right: the exact one is a step away
-      c = min(max(c, 0), grid - 1);
-      while (c > 0 && total * c / grid > tile) c--;
-      while (total * (c + 1) / grid <= tile) c++;
-      P.part[blockIdx.x] = {b, head, row_tile, c};
-    }
+    if (starts && !whole && tid == 0)
+      P.part[blockIdx.x] = {b, head, row_tile, kv_run_of(run, seg_begin + key_tiles - 1)};
     at = seg_begin + kt1;
   }
 }
 
-// Joins the parts of the segments that lie in several CTAs' runs.  One CTA per
-// run of the other kernel and 16 rows.
-template <typename T, int DP, int MT>
-__global__ void __launch_bounds__(kThreads) attend_join_kernel(const AttendParams P) {
-  constexpr int kRows = MT * 16;
+// Joins the parts of the segments that lie in several runs: one CTA per CTA of
+// the other kernel and four rows.  The parts' statistics become weights in
+// shared memory, in rounds of kParts; the threads of a row then add up 16 bytes
+// of it each, from parts of their own where there are threads to spare.
+constexpr int kJoin = 256;
+constexpr int kJoinRows = 4;
+constexpr int kParts = 256;
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(kJoin) attend_join_kernel(const AttendParams P) {
+  constexpr int kVec = DP / 4;                            // threads of a row
+  constexpr int kShares = kJoin / (kJoinRows * kVec);     // that add up different parts
+  __shared__ float weight[kJoinRows][kParts];
+  __shared__ float4 sums[kShares][kJoinRows][kVec];
+  __shared__ float row_l[kJoinRows], row_top[kJoinRows];
+  wait_for_last_kernel();
   const AttendPart seg = P.part[blockIdx.x];
   if (seg.last < 0) return;
-  const int D = P.c.head_dim, G = P.group;
+  const int D = P.c.head_dim, G = P.group, R = P.rows;
   const KvRange tok = kv_tokens(P.t, seg.b, nullptr);
-  const int rows = min(tok.count * G - seg.row_tile * kRows, kRows);
-  const int parts = seg.last - blockIdx.x + 1;
-  constexpr int64_t kStep = (int64_t)2 * kRows * (DP + 2);
-  // the first CTA's part is its second one, the others' is their first
-  const float *first = P.partial + (int64_t)blockIdx.x * kStep + kRows * (DP + 2);
-  const float *rest = P.partial + (int64_t)blockIdx.x * kStep;
-  for (int i = threadIdx.x; i < 16 * (DP / 2); i += kThreads) {
-    const int r = blockIdx.y * 16 + i / (DP / 2), d = i % (DP / 2) * 2;
-    if (r >= rows || d >= D) continue;
-    float top = first[r * (DP + 2) + DP];
-    for (int p = 1; p < parts; p++) top = fmaxf(top, rest[p * kStep + r * (DP + 2) + DP]);
-    const float base = top == -INFINITY ? 0.f : top;
-    float x = 0.f, y = 0.f, l = 0.f;
-    for (int p = 0; p < parts; p++) {
-      const float *q = (p ? rest + p * kStep : first) + r * (DP + 2);
-      const float f = exp2_fast(q[DP] - base);
-      l += q[DP + 1] * f;
-      x += q[d] * f;
-      y += q[d + 1] * f;
-    }
-    const int row = seg.row_tile * kRows + r, node = row / G;
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    T *dst = static_cast<T *>(P.s.out) + (tok.first + node) * P.s.out_token + (seg.head * G + row % G) * P.s.out_head + d;
-    *reinterpret_cast<uint32_t *>(dst) = KvType<T>::pack(x * inv, y * inv);
-    if (d == 0 && P.s.lse)
-      P.s.lse[(int64_t)(tok.first + node) * P.s.n_q_heads + seg.head * G + row % G] =
-          (top + log2f(l)) * 0.6931471805599453f;
+  const int rows = min(tok.count * G - seg.row_tile * R, R);
+  const int row0 = blockIdx.y * kJoinRows;
+  if (row0 >= rows) return;
+  const int step = P.row_groups;  // CTAs from one run to the next
+  const int parts = seg.last - (int)blockIdx.x / step + 1;
+  const int64_t stride = (int64_t)2 * R * (DP + 2) * step;
+  // the first run's part is its second one, the others' is their first
+  const float *rest = P.partial + (int64_t)blockIdx.x * 2 * R * (DP + 2);
+  const float *first = rest + R * (DP + 2);
+  auto part = [&](int p) { return p ? rest + p * stride : first; };
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  float top = -INFINITY, l = 0.f;
+  if (warp < kJoinRows && row0 + warp < rows) {
+    for (int p = lane; p < parts; p += 32) top = fmaxf(top, part(p)[R * DP + row0 + warp]);
+#pragma unroll
+    for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
   }
+  const float base = top == -INFINITY ? 0.f : top;
+  const int row = threadIdx.x / kVec % kJoinRows, share = threadIdx.x / (kVec * kJoinRows), col = threadIdx.x % kVec * 4;
+  float4 sum = {0.f, 0.f, 0.f, 0.f};
+  for (int p0 = 0; p0 < parts; p0 += kParts) {
+    const int n = min(parts - p0, kParts);
+    __syncthreads();
+    if (warp < kJoinRows && row0 + warp < rows)
+      for (int p = lane; p < n; p += 32) {
+        const float *q = part(p0 + p) + R * DP + row0 + warp;
+        const float f = exp2_fast(q[0] - base);
+        weight[warp][p] = f;
+        l += q[R] * f;
+      }
+    __syncthreads();
+    if (row0 + row < rows && col < D)
+#pragma unroll 8
+      for (int p = share; p < n; p += kShares) {
+        const float4 x = *reinterpret_cast<const float4 *>(part(p0 + p) + (row0 + row) * DP + col);
+        const float f = weight[row][p];
+        sum.x += x.x * f, sum.y += x.y * f, sum.z += x.z * f, sum.w += x.w * f;
+      }
+  }
+  if (warp < kJoinRows) {
+#pragma unroll
+    for (int d = 16; d; d >>= 1) l += __shfl_xor_sync(~0u, l, d);
+    if (lane == 0) row_l[warp] = l, row_top[warp] = top;
+  }
+  sums[share][row][col / 4] = sum;
+  __syncthreads();
+  if (share > 0 || row0 + row >= rows || col >= D) return;
+#pragma unroll
+  for (int s = 1; s < kShares; s++) {
+    const float4 x = sums[s][row][col / 4];
+    sum.x += x.x, sum.y += x.y, sum.z += x.z, sum.w += x.w;
+  }
+  l = row_l[row];
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const int at = seg.row_tile * R + row0 + row, node = at / G;
+  T *dst = static_cast<T *>(P.s.out) + (tok.first + node) * P.s.out_token + (seg.head * G + at % G) * P.s.out_head + col;
+  *reinterpret_cast<uint2 *>(dst) =
+      make_uint2(KvType<T>::pack(sum.x * inv, sum.y * inv), KvType<T>::pack(sum.z * inv, sum.w * inv));
+  if (col == 0 && P.s.lse)
+    P.s.lse[(int64_t)(tok.first + node) * P.s.n_q_heads + seg.head * G + at % G] =
+        (row_top[row] + log2f(l)) * 0.6931471805599453f;
 }
 
 struct AttendPlan {
-  int dp, mt, grid;
+  int dp, rows, row_groups, grid;
+  bool tc;
   uint64_t bytes;
 };
 
 AttendPlan attend_plan(int head_dim, int max_rows) {
   AttendPlan p;
   p.dp = head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256;
-  p.mt = max_rows <= 16 ? 1 : max_rows <= 32 ? 2 : 4;
-  p.grid = kv_sm_count() * (p.dp <= 128 ? 2 : 1);
-  p.bytes = (uint64_t)p.grid * (2 * p.mt * 16 * (p.dp + 2) * 4 + sizeof(AttendPart));
+  p.tc = max_rows > 64 && p.dp <= 128;
+  p.rows = p.tc ? kTcRows : max_rows <= 16 ? 16 : max_rows <= 32 ? 32 : 64;
+  // CTAs that go through the same keys with row tiles of their own
+  p.row_groups = p.tc ? min((max_rows + kTcRows - 1) / kTcRows, 4) : 1;
+  p.grid = p.tc ? kv_sm_count() / p.row_groups * p.row_groups : kv_sm_count() * (p.dp <= 128 ? 2 : 1);
+  p.bytes = (uint64_t)p.grid * (2 * p.rows * (p.dp + 2) * 4 + sizeof(AttendPart));
   return p;
+}
+
+template <typename T, int DP>
+int attend_join(const AttendParams &p, const AttendPlan &plan, int max_rows, void *stream) {
+  return kv_launch("kv_attend_join", dim3(plan.grid, (min(max_rows, plan.rows) + kJoinRows - 1) / kJoinRows),
+                   dim3(kJoin), 0, stream, kAfterLast, attend_join_kernel<T, DP>, p);
 }
 
 template <typename T, int DP, int MT>
@@ -432,25 +442,29 @@ int attend_run(const AttendParams &p, const AttendPlan &plan, void *stream) {
   static uint64_t done = 0;
   constexpr int smem = kAttendSmem<DP, MT>;
   if (!kv_allow_smem(reinterpret_cast<const void *>(attend_kernel<T, DP, MT>), smem, &done)) return UNISON_ERR_CUDA;
-  int rc = kv_launch("kv_attend", dim3(plan.grid), dim3(kThreads), smem, stream, 1, attend_kernel<T, DP, MT>, p);
-  if (rc != UNISON_OK) return rc;
-  return kv_launch("kv_attend_join", dim3(plan.grid, MT), dim3(kThreads), 0, stream, 1,
-                   attend_join_kernel<T, DP, MT>, p);
+  return kv_launch("kv_attend", dim3(plan.grid), dim3(kThreads), smem, stream, 1, attend_kernel<T, DP, MT>, p);
+}
+
+template <typename T, int DP>
+int attend_rows(const AttendParams &p, const AttendPlan &plan, int max_rows, void *stream) {
+  int rc;
+  if constexpr (DP <= 128) {
+    if (plan.tc) {
+      rc = attend_tc<T, DP>(p, plan.grid, stream);
+      return rc == UNISON_OK ? attend_join<T, DP>(p, plan, max_rows, stream) : rc;
+    }
+  }
+  rc = plan.rows == 16   ? attend_run<T, DP, 1>(p, plan, stream)
+       : plan.rows == 32 ? attend_run<T, DP, 2>(p, plan, stream)
+                         : attend_run<T, DP, 4>(p, plan, stream);
+  return rc == UNISON_OK ? attend_join<T, DP>(p, plan, max_rows, stream) : rc;
 }
 
 template <typename T>
-int attend_pick(const AttendParams &p, const AttendPlan &plan, void *stream) {
-  switch (plan.dp * 8 + plan.mt) {
-    case 64 * 8 + 1: return attend_run<T, 64, 1>(p, plan, stream);
-    case 64 * 8 + 2: return attend_run<T, 64, 2>(p, plan, stream);
-    case 64 * 8 + 4: return attend_run<T, 64, 4>(p, plan, stream);
-    case 128 * 8 + 1: return attend_run<T, 128, 1>(p, plan, stream);
-    case 128 * 8 + 2: return attend_run<T, 128, 2>(p, plan, stream);
-    case 128 * 8 + 4: return attend_run<T, 128, 4>(p, plan, stream);
-    case 256 * 8 + 1: return attend_run<T, 256, 1>(p, plan, stream);
-    case 256 * 8 + 2: return attend_run<T, 256, 2>(p, plan, stream);
-    default: return attend_run<T, 256, 4>(p, plan, stream);
-  }
+int attend_pick(const AttendParams &p, const AttendPlan &plan, int max_rows, void *stream) {
+  return plan.dp == 64    ? attend_rows<T, 64>(p, plan, max_rows, stream)
+         : plan.dp == 128 ? attend_rows<T, 128>(p, plan, max_rows, stream)
+                          : attend_rows<T, 256>(p, plan, max_rows, stream);
 }
 
 }  // namespace
@@ -524,8 +538,10 @@ extern "C" int unison_kv_attend(const unison_kv_cache *cache, const unison_kv_tr
   p.group = step->n_q_heads / cache->n_heads;
   const AttendPlan plan = attend_plan(cache->head_dim, tree->max_tokens * p.group);
   if (!workspace || !kv_aligned(workspace, 16) || workspace_bytes < plan.bytes) return UNISON_ERR_ARG;
+  p.rows = plan.rows;
+  p.row_groups = plan.row_groups;
   p.part = static_cast<AttendPart *>(workspace);
   p.partial = reinterpret_cast<float *>(p.part + plan.grid);
-  return cache->dtype == UNISON_KV_BF16 ? attend_pick<__nv_bfloat16>(p, plan, cuda_stream)
-                                        : attend_pick<__half>(p, plan, cuda_stream);
+  return cache->dtype == UNISON_KV_BF16 ? attend_pick<__nv_bfloat16>(p, plan, tree->max_tokens * p.group, cuda_stream)
+                                        : attend_pick<__half>(p, plan, tree->max_tokens * p.group, cuda_stream);
 }

@@ -1,0 +1,493 @@
+// Attention of many query rows per KV head on the tensor cores (the variant of
+// unison_kv_attend for trees whose nodes x query heads exceed 64 rows).
+//
+// A CTA takes up to 256 query rows, two tiles of 128, and walks the keys in
+// tiles of 128.  Warps have roles:
+//   warps 8-11   copy the paged rows of K and V, and the query rows, into
+//                shared memory in the swizzled form that the tensor cores read
+//   warp 12      issues the products S = Q K^T and O += P V; S, P (over S) and
+//                O stay in tensor memory
+//   warps 0-3, 4-7  one query tile each: a thread per row turns S into weights
+// While one tile's weights are computed, the other tile's products run.  O is
+// rescaled only when a row's maximum has grown by more than 2^8 over the one
+// its weights are relative to; the sums are 32 bits wide, so weights up to 2^8
+// cost no accuracy.
+#include "kv_attend.cuh"
+#include "kv_tc.cuh"
+
+namespace unison {
+namespace {
+
+constexpr int kThreads = 512;
+constexpr int kTile = 128;
+constexpr int kCopyWarp = 8, kIssueWarp = 12;
+// Registers of a thread that computes weights, and of the others: 256 threads
+// each, together what the launch has (512 x 128).
+constexpr int kRegsWeights = 192, kRegsOthers = 64;
+constexpr float kSlack = 8.f;
+
+template <int DP>
+constexpr int kSlots = DP == 128 ? 5 : 8;  // tiles of K or V on their way
+template <int DP>
+constexpr int kTcSmem = 1024 + kTcRows *DP * 2 + kSlots<DP> *kTile *DP * 2;
+
+template <int DP>
+struct TcShared {
+  KvRunShared run;
+  uint64_t kv_full[kSlots<DP>], kv_free[kSlots<DP>], q_full, q_free, s_full[2], p_full[2], pv_done[2], idle;
+  uint32_t row_ok[8][4];  // which keys of a tile exist
+  int odd[4];             // whether a segment's new values hold infinities or NaN
+  uint32_t tmem;
+  volatile int dead;
+};
+
+// What every role works out alike for the segment that `at` lies in.
+struct Segment {
+  int b, head, row_tile, rows, tiles, kt0, kt1, len;
+  KvRange tok;
+};
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const AttendParams P) {
+  constexpr uint32_t kTileBytes = kTile * DP * 2, kBlock = kTile * 128;
+  extern __shared__ unsigned char smem_raw[];
+  __shared__ TcShared<DP> sh;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int D = P.c.head_dim, H = P.c.n_heads, G = P.group;
+  const uint32_t q_base = (smem_u32(smem_raw) + 1023) & ~1023u, slot_base = q_base + kTcRows * DP * 2;
+  const int groups = P.row_groups, rank = blockIdx.x % groups;
+  if (tid == 0) P.part[blockIdx.x].last = -1;
+
+  auto seq_tiles = [&](int b) -> int64_t {
+    const int tokens = kv_tokens(P.t, b, P.c.status).count;
+    const int row_tiles = (tokens * G + kTcRows - 1) / kTcRows;
+    return (int64_t)attend_key_tiles(kv_length(P.c, b), tokens, kTile) * ((row_tiles + groups - 1) / groups) * H;
+  };
+  KvRun run;
+  if (!kv_find_run(run, sh.run, P.c.n_seqs, gridDim.x / groups, blockIdx.x / groups, seq_tiles)) return;
+
+  if (tid == 0) {
+    for (int i = 0; i < kSlots<DP>; i++) {
+      bar_init(smem_u32(&sh.kv_full[i]), 128);
+      bar_init(smem_u32(&sh.kv_free[i]), 1);
+    }
+    bar_init(smem_u32(&sh.q_full), 128);
+    bar_init(smem_u32(&sh.q_free), 1);
+    bar_init(smem_u32(&sh.idle), 1);
+    for (int i = 0; i < 2; i++) {
+      bar_init(smem_u32(&sh.s_full[i]), 2);
+      bar_init(smem_u32(&sh.p_full[i]), 128);
+      bar_init(smem_u32(&sh.pv_done[i]), 2);
+    }
+    sh.dead = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == kIssueWarp) tmem_alloc(smem_u32(&sh.tmem), 512);
+  tmem_before_sync();
+  __syncthreads();
+  tmem_after_sync();
+  const uint32_t tmem = sh.tmem;  // S of the two query tiles, then their O
+
+  int b = run.b;
+  int64_t at = run.at, seq_begin = run.begin, seg_begin = 0;
+  auto next_segment = [&](Segment &g) {
+    int64_t mine = seq_tiles(b);
+    while (at >= seq_begin + mine) {
+      seq_begin += mine;
+      mine = seq_tiles(++b);
+    }
+    g.b = b;
+    g.tok = kv_tokens(P.t, b, nullptr);
+    g.len = kv_length(P.c, b);
+    g.tiles = attend_key_tiles(g.len, g.tok.count, kTile);
+    const int row_tiles = (g.tok.count * G + kTcRows - 1) / kTcRows;
+    const int row_groups = (row_tiles + groups - 1) / groups;
+    const int seg = (int)((at - seq_begin) / g.tiles);
+    seg_begin = seq_begin + (int64_t)seg * g.tiles;
+    g.head = seg / row_groups;
+    g.row_tile = seg % row_groups * groups + rank;
+    g.rows = min(g.tok.count * G - g.row_tile * kTcRows, kTcRows);  // <= 0: this CTA has none
+    g.kt0 = (int)(at - seg_begin);
+    g.kt1 = (int)min((int64_t)g.tiles, run.end - seg_begin);
+    at = seg_begin + g.kt1;
+  };
+
+  if (warp >= kCopyWarp && warp < kIssueWarp) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOthers));
+    // ------------------------------------------------------------- copies
+    const int w = warp - kCopyWarp;
+    constexpr int kChunks = DP / 8, kRowsAtOnce = 32 / kChunks;
+    const int chunk = lane % kChunks, sub = lane / kChunks;
+    const T *dummy = static_cast<const T *>(P.s.q);
+    int item = 0, tile_no = 0, seg_no = 0;
+    uint32_t pending = 0;  // barrier of the copies that are still on their way
+    bool ok = true;
+    auto arrive_later = [&](uint32_t bar) {
+      cp_commit();
+      if (pending) {
+        cp_wait<1>();
+        fence_to_tensor();
+        bar_arrive(pending);
+      }
+      pending = bar;
+    };
+    auto flush = [&]() {
+      cp_wait<0>();
+      if (pending) {
+        fence_to_tensor();
+        bar_arrive(pending);
+      }
+      pending = 0;
+    };
+    // Copies this warp's 32 rows of a tile; lane i knows row i's address.
+    auto copy_rows = [&](uint32_t dst, const T *mine) {
+#pragma unroll 4
+      for (int r = 0; r < 32; r += kRowsAtOnce) {
+        const T *src = reinterpret_cast<const T *>(__shfl_sync(~0u, reinterpret_cast<unsigned long long>(mine), r + sub));
+        const bool there = src != nullptr && chunk * 8 < D;
+        cp_async16(operand_chunk(dst, kTile, w * 32 + r + sub, chunk), there ? src + chunk * 8 : dummy, there);
+      }
+    };
+    auto slot_for = [&](uint32_t &bar) -> uint32_t {  // waits until the next slot is free
+      const int s = item % kSlots<DP>, n = item / kSlots<DP>;
+      if (n > 0) ok = __all_sync(~0u, bar_wait(smem_u32(&sh.kv_free[s]), (n - 1) & 1, &sh.dead));
+      item++;
+      bar = smem_u32(&sh.kv_full[s]);
+      return slot_base + s * kTileBytes;
+    };
+    while (at < run.end && ok) {
+      Segment g;
+      next_segment(g);
+      if (g.rows <= 0) continue;
+      const int last_tile = g.tiles - 1;
+      auto find_page = [&](int kt, int &off) -> int {
+        const int slot = kt * kTile + w * 32 + lane;
+        off = 0;
+        return kt < last_tile && slot < g.len ? kv_page(P.c, g.b, slot, off) : -1;
+      };
+      int off;
+      int page = find_page(g.kt0, off);
+      if (w == 0 && lane == 0) sh.odd[seg_no & 3] = 0;
+      for (int kt = g.kt0; kt < g.kt1 && ok; kt++) {
+        const T *k = nullptr, *v = nullptr;
+        if (kt == last_tile) {
+          const int j = w * 32 + lane;
+          if (j < g.tok.count) {
+            k = static_cast<const T *>(P.s.k_new) + (g.tok.first + j) * P.s.k_token + g.head * P.s.k_head;
+            v = static_cast<const T *>(P.s.v_new) + (g.tok.first + j) * P.s.v_token + g.head * P.s.v_head;
+          }
+        } else if (page >= 0) {
+          k = static_cast<const T *>(P.c.k) + page * P.c.k_page + g.head * P.c.k_head + off * P.c.k_slot;
+          v = static_cast<const T *>(P.c.v) + page * P.c.v_page + g.head * P.c.v_head + off * P.c.v_slot;
+        }
+        const uint32_t there = __ballot_sync(~0u, k != nullptr);
+        if (lane == 0) sh.row_ok[tile_no & 7][w] = there;
+        tile_no++;
+        if (kt + 1 < g.kt1) page = find_page(kt + 1, off);
+        uint32_t bar;
+        uint32_t dst = slot_for(bar);
+        if (!ok) break;
+        copy_rows(dst, k);
+        arrive_later(bar);
+        if (kt == g.kt0) {  // the segment's query rows: when the last segment's products have read theirs
+          if (seg_no > 0) ok = __all_sync(~0u, bar_wait(smem_u32(&sh.q_free), (seg_no - 1) & 1, &sh.dead));
+          if (!ok) break;
+          for (int q = 0; q < (g.rows > 128 ? 2 : 1); q++) {
+            const int r = q * 128 + w * 32 + lane, row = g.row_tile * kTcRows + r;
+            const T *src = nullptr;
+            if (r < g.rows)
+              src = static_cast<const T *>(P.s.q) + (g.tok.first + row / G) * P.s.q_token +
+                    (g.head * G + row % G) * P.s.q_head;
+            copy_rows(q_base + q * kTileBytes, src);
+          }
+          arrive_later(smem_u32(&sh.q_full));
+        }
+        dst = slot_for(bar);
+        if (!ok) break;
+        copy_rows(dst, v);
+        arrive_later(bar);
+        if (kt == last_tile) {
+          // A new token that a row does not see must not reach it as 0 * inf:
+          // such values become 0 here and are put back, row by row, at the end.
+          cp_wait<0>();
+          bool odd = false;
+          for (int r = 0; r < 32; r += kRowsAtOnce) {
+            const uint32_t a = operand_chunk(dst, kTile, w * 32 + r + sub, chunk);
+            uint32_t x[4];
+            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(a) : "memory");
+            bool bad = false;
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+              constexpr uint32_t e = KvType<T>::kExponent;
+              if ((x[i] & e) == e) x[i] &= 0xFFFF0000u, bad = true;
+              if ((x[i] >> 16 & e) == e) x[i] &= 0xFFFFu, bad = true;
+            }
+            if (bad) {
+              asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]) : "memory");
+              odd = true;
+            }
+          }
+          if (odd) sh.odd[seg_no & 3] = 1;
+          flush();
+        }
+      }
+      seg_no++;
+    }
+    flush();
+  } else if (warp >= kIssueWarp) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOthers));
+    if (warp == kIssueWarp && lane == 0) {
+      // ----------------------------------------------------------- products
+      const uint32_t shape_s = product_shape(kOperandType<T>, 128, kTile, false, P.s.scale < 0.f);
+      const uint32_t shape_o = product_shape(kOperandType<T>, 128, DP, true, false);
+      int item = 0, seg_no = 0, p_no[2] = {0, 0};
+      bool ok = true;
+      auto take = [&](int &s) -> uint32_t {  // waits for the next slot's tile
+        s = item % kSlots<DP>;
+        ok = ok && bar_wait(smem_u32(&sh.kv_full[s]), (item / kSlots<DP>) & 1, &sh.dead);
+        item++;
+        return slot_base + s * kTileBytes;
+      };
+      auto scores = [&](int q, uint32_t keys) {
+  #pragma unroll
+        for (int d = 0; d < DP / 16; d++) {
+          const uint32_t at = d / 4 * kBlock + d % 4 * 32;
+          product_ss(tmem + q * 128, smem_operand(q_base + q * kTileBytes + at, kBlock), smem_operand(keys + at, kBlock),
+                     shape_s, d > 0);
+        }
+        products_done(smem_u32(&sh.s_full[q]));
+        bar_arrive(smem_u32(&sh.s_full[q]));  // hands on what the copies of the keys wrote besides (row_ok)
+      };
+      auto values = [&](int q, uint32_t vals, bool add) {
+        ok = ok && bar_wait(smem_u32(&sh.p_full[q]), p_no[q]++ & 1, &sh.dead);
+        if (!ok) return;
+        tmem_after_sync();
+  #pragma unroll
+        for (int k = 0; k < kTile / 16; k++)
+          product_ts(tmem + 256 + q * DP, tmem + q * 128 + k * 8, smem_operand(vals + k * 2048, kBlock), shape_o, add || k > 0);
+        products_done(smem_u32(&sh.pv_done[q]));
+        bar_arrive(smem_u32(&sh.pv_done[q]));  // and those of the values (odd)
+      };
+      while (at < run.end && ok) {
+        Segment g;
+        next_segment(g);
+        if (g.rows <= 0) continue;
+        const int n = g.kt1 - g.kt0, tiles = g.rows > 128 ? 2 : 1;
+        int ks, vs;
+        uint32_t keys = take(ks);
+        ok = ok && bar_wait(smem_u32(&sh.q_full), seg_no & 1, &sh.dead);
+        if (!ok) break;
+        for (int q = 0; q < tiles; q++) scores(q, keys);
+        products_done(smem_u32(&sh.kv_free[ks]));
+        if (n == 1) products_done(smem_u32(&sh.q_free));
+        for (int i = 0; i < n && ok; i++) {
+          const uint32_t vals = take(vs);
+          for (int q = 0; q < tiles && ok; q++) {
+            values(q, vals, i > 0);
+            if (q == tiles - 1) products_done(smem_u32(&sh.kv_free[vs]));
+            if (i + 1 < n) {
+              if (q == 0) keys = take(ks);
+              if (!ok) break;
+              scores(q, keys);
+              if (q == tiles - 1) {
+                products_done(smem_u32(&sh.kv_free[ks]));
+                if (i + 2 == n) products_done(smem_u32(&sh.q_free));
+              }
+            }
+          }
+        }
+        seg_no++;
+      }
+      // nothing may still be at work when tensor memory is freed
+      products_done(smem_u32(&sh.idle));
+      for (int i = 0; i < 1 << 20 && !bar_try(smem_u32(&sh.idle), 0); i++) {
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsWeights));
+    // ------------------------------------------------------------ weights
+    const int q = warp >> 2, r = tid & 127;
+    const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // this warp's quarter of the 128 lanes
+    const uint32_t s_addr = tmem + q * 128 + lanes, o_addr = tmem + 256 + q * DP + lanes;
+    // (the sign is in the products; not 0, so that -inf stays -inf)
+    const float c = fmaxf(fabsf(P.s.scale) * 1.4426950408889634f, 1.2e-38f);
+    int s_no = 0, seg_no = 0, tile_no = 0;  // products seen, segments, key tiles of this CTA
+    bool ok = true;
+    while (at < run.end && ok) {
+      Segment g;
+      next_segment(g);
+      if (g.rows <= 0) continue;
+      const int mine = seg_no++;
+      if (q * 128 >= g.rows) {  // the segment has no such tile
+        tile_no += g.kt1 - g.kt0;
+        continue;
+      }
+      const int row = g.row_tile * kTcRows + q * 128 + r, node = row / G;
+      const bool used = q * 128 + r < g.rows;
+      const uint64_t mask = !used ? 0 : P.t.mask ? P.t.mask[g.tok.first + node] : ~0ull >> (63 - node);
+      float m = -INFINITY, l = 0.f;
+      for (int kt = g.kt0; kt < g.kt1; kt++, tile_no++) {
+        ok = __all_sync(~0u, bar_wait(smem_u32(&sh.s_full[q]), s_no & 1, &sh.dead));
+        if (!ok) break;
+        tmem_after_sync();
+        uint32_t x[128];
+        tmem_ld32(x, s_addr);
+        tmem_ld32(x + 32, s_addr + 32);
+        tmem_ld32(x + 64, s_addr + 64);
+        tmem_ld32(x + 96, s_addr + 96);
+        uint32_t see[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) see[i] = sh.row_ok[tile_no & 7][i];
+        if (kt == g.tiles - 1) {
+          see[0] &= (uint32_t)mask;
+          see[1] &= (uint32_t)(mask >> 32);
+        }
+        tmem_wait_ld();
+        if (!__all_sync(~0u, (see[0] & see[1] & see[2] & see[3]) == ~0u)) {
+#pragma unroll
+          for (int i = 0; i < 128; i++)
+            if (!(see[i / 32] >> (i % 32) & 1)) x[i] = 0xFF800000u;  // -inf
+        }
+        float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int i = 0; i < 128; i++) t[i & 3] = fmaxf(t[i & 3], __uint_as_float(x[i]));
+        const float top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
+        const float scaled = top * c;
+        if (kt == g.kt0) {
+          m = scaled;
+        } else if (__any_sync(~0u, scaled > m + kSlack)) {
+          const float to = scaled > m + kSlack ? scaled : m;
+          const float f = m == to ? 1.f : exp2_fast(m - to);
+          ok = __all_sync(~0u, bar_wait(smem_u32(&sh.pv_done[q]), (s_no - 1) & 1, &sh.dead));
+          if (!ok) break;
+          tmem_after_sync();
+          for (int d = 0; d < DP; d += 32) {
+            uint32_t o[32];
+            tmem_ld32(o, o_addr + d);
+            tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 32; i++) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+            tmem_st32(o_addr + d, o);
+          }
+          l *= f;
+          m = to;
+        }
+        const float base = m == -INFINITY ? 0.f : m;
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < 128; i += 32) {
+          uint32_t p[16];
+#pragma unroll
+          for (int j = 0; j < 32; j += 2) {
+            const float a = exp2_fast(fmaf(__uint_as_float(x[i + j]), c, -base));
+            const float b = exp2_fast(fmaf(__uint_as_float(x[i + j + 1]), c, -base));
+            sum[j & 2] += a;
+            sum[(j & 2) + 1] += b;
+            p[j / 2] = KvType<T>::pack(a, b);
+          }
+          tmem_st16(s_addr + i / 2, p);
+        }
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        tmem_wait_st();
+        tmem_before_sync();
+        bar_arrive(smem_u32(&sh.p_full[q]));
+        s_no++;
+      }
+      if (!ok) {
+        if (r == 0 && P.c.status) P.c.status[g.b] = UNISON_ERR_TIMEOUT;
+        break;
+      }
+      // ---- results: O is complete when the last product with V is
+      ok = __all_sync(~0u, bar_wait(smem_u32(&sh.pv_done[q]), (s_no - 1) & 1, &sh.dead));
+      if (!ok) break;
+      tmem_after_sync();
+      const bool whole = g.kt0 == 0 && g.kt1 == g.tiles;
+      const bool odd = g.kt1 == g.tiles && sh.odd[mine & 3];
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      float *part = P.partial + ((int64_t)blockIdx.x * 2 + (g.kt0 == 0 ? 1 : 0)) * (kTcRows * (DP + 2));
+      const int pr = q * 128 + r;
+      T *dst = static_cast<T *>(P.s.out) + (g.tok.first + node) * P.s.out_token + (g.head * G + row % G) * P.s.out_head;
+#pragma unroll
+      for (int d0 = 0; d0 < DP; d0 += 32) {
+        uint32_t o[32];
+        tmem_ld32(o, o_addr + d0);
+        tmem_wait_ld();
+        if (used && odd) {
+          const uint64_t see = mask & (~0ull >> (64 - g.tok.count));
+          for (int j = 0; j < g.tok.count; j++) {
+            if (!(see >> j & 1)) continue;
+            const T *v = static_cast<const T *>(P.s.v_new) + (g.tok.first + j) * P.s.v_token + g.head * P.s.v_head + d0;
+#pragma unroll
+            for (int i = 0; i < 32; i++) {
+              const float y = d0 + i < D ? KvType<T>::to_float(v[i]) : 0.f;
+              if (!isfinite(y)) o[i] = __float_as_uint(__uint_as_float(o[i]) + y);
+            }
+          }
+        }
+        if (used && whole) {
+#pragma unroll
+          for (int i = 0; i < 32; i += 8) {
+            if (d0 + i < D) {
+              uint4 y;
+              y.x = KvType<T>::pack(__uint_as_float(o[i]) * inv, __uint_as_float(o[i + 1]) * inv);
+              y.y = KvType<T>::pack(__uint_as_float(o[i + 2]) * inv, __uint_as_float(o[i + 3]) * inv);
+              y.z = KvType<T>::pack(__uint_as_float(o[i + 4]) * inv, __uint_as_float(o[i + 5]) * inv);
+              y.w = KvType<T>::pack(__uint_as_float(o[i + 6]) * inv, __uint_as_float(o[i + 7]) * inv);
+              *reinterpret_cast<uint4 *>(dst + d0 + i) = y;
+            }
+          }
+        } else if (used) {
+#pragma unroll
+          for (int i = 0; i < 32; i += 4)
+            *reinterpret_cast<uint4 *>(part + pr * DP + d0 + i) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+        }
+        __syncwarp();  // the next load is one instruction of the whole warp
+      }
+      if (used) {
+        if (!whole) {
+          part[kTcRows * DP + pr] = m;
+          part[kTcRows * (DP + 1) + pr] = l;
+        } else if (P.s.lse) {
+          P.s.lse[(int64_t)(g.tok.first + node) * P.s.n_q_heads + g.head * G + row % G] = (m + log2f(l)) * 0.6931471805599453f;
+        }
+      }
+      if (!whole && g.kt0 == 0 && r == 0 && q == 0)
+        P.part[blockIdx.x] = {g.b, g.head, g.row_tile, kv_run_of(run, seg_begin + g.tiles - 1)};
+      __syncwarp();
+      tmem_before_sync();  // the next segment's products overwrite O
+    }
+  }
+  __syncwarp();
+  tmem_before_sync();
+  __syncthreads();
+  if (warp == kIssueWarp) {
+    tmem_after_sync();
+    tmem_free(tmem, 512);
+  }
+}
+
+}  // namespace
+
+template <typename T, int DP>
+int attend_tc(const AttendParams &p, int grid, void *stream) {
+  static uint64_t done = 0;
+  const void *kernel = reinterpret_cast<const void *>(attend_tc_kernel<T, DP>);
+  if (!__atomic_load_n(&done, __ATOMIC_RELAXED)) {
+    // the registers that the roles share out must be there: see kRegsWeights
+    cudaFuncAttributes a;
+    if (cudaFuncGetAttributes(&a, kernel) != cudaSuccess) {
+      cudaGetLastError();
+      return UNISON_ERR_CUDA;
+    }
+    if (a.numRegs * kThreads < 256 * (kRegsWeights + kRegsOthers)) return UNISON_ERR_CUDA;
+  }
+  if (!kv_allow_smem(kernel, kTcSmem<DP>, &done)) return UNISON_ERR_CUDA;
+  return kv_launch("kv_attend", dim3(grid), dim3(kThreads), kTcSmem<DP>, stream, 1, attend_tc_kernel<T, DP>, p);
+}
+
+template int attend_tc<__nv_bfloat16, 64>(const AttendParams &, int, void *);
+template int attend_tc<__nv_bfloat16, 128>(const AttendParams &, int, void *);
+template int attend_tc<__half, 64>(const AttendParams &, int, void *);
+template int attend_tc<__half, 128>(const AttendParams &, int, void *);
+
+}  // namespace unison

@@ -258,6 +258,7 @@ __global__ void __launch_bounds__(256) evict_move_kernel(const EvictParams P) {
   const int chunks = P.c.head_dim / 8;
   const int64_t room = (int64_t)P.c.max_pages * P.c.page_size;
   const int32_t *from = P.moves + seg * room, *into = from + room / 2;
+  wait_for_last_kernel();
   const int count = P.count[seg];
   const int warps = P.per_seg * (blockDim.x >> 5);
   const int width = 2 * chunks;
@@ -390,6 +391,6 @@ extern "C" int unison_kv_evict(const unison_kv_cache *cache, const unison_kv_cac
   const int64_t most = into ? min(room, (int64_t)into->max_pages * into->page_size) : room / 2;
   const int64_t fill = ((int64_t)kv_sm_count() * 32 + segs - 1) / (int64_t)segs;
   p.per_seg = (int)max((int64_t)1, min((most + 255) / 256, fill));
-  return kv_launch("kv_evict_move", dim3((unsigned)(segs * p.per_seg)), dim3(256), 0, cuda_stream, 1,
+  return kv_launch("kv_evict_move", dim3((unsigned)(segs * p.per_seg)), dim3(256), 0, cuda_stream, kAfterLast,
                    evict_move_kernel<uint16_t>, p);
 }

@@ -31,9 +31,7 @@ template <typename T, int DP, int QR>
 __global__ void __launch_bounds__(kThreads) observe_kernel(const ObserveParams P) {
   constexpr int kChunks = DP / 8;
   extern __shared__ __align__(128) unsigned char smem[];
-  __shared__ int64_t scan_part[33];
-  __shared__ int found_b;
-  __shared__ int64_t found_begin;
+  __shared__ KvRunShared shared_run;
   __shared__ const T *row_k[2][kTile];
   __shared__ int64_t row_m[4][kTile];
   __shared__ float row_lse[QR];
@@ -49,31 +47,13 @@ __global__ void __launch_bounds__(kThreads) observe_kernel(const ObserveParams P
     if (!tokens) return 0;
     return path_count(P, b, tokens) ? (kv_length(P.c, b) + kTile - 1) / kTile + 1 : 1;
   };
-  int64_t total = 0;
-  for (int b0 = 0; b0 < P.c.n_seqs; b0 += kThreads) {
-    int64_t n;
-    block_scan(b0 + tid < P.c.n_seqs ? (int64_t)key_tiles_of(b0 + tid) * H : 0, scan_part, n);
-    total += n;
-  }
-  const int grid = (int)min((int64_t)gridDim.x, total);
-  if ((int)blockIdx.x >= grid) return;
-  int64_t at = total * blockIdx.x / grid;
-  const int64_t end = total * (blockIdx.x + 1) / grid;
-  int64_t sum = 0;
-  for (int b0 = 0; b0 < P.c.n_seqs; b0 += kThreads) {
-    const int64_t mine = b0 + tid < P.c.n_seqs ? (int64_t)key_tiles_of(b0 + tid) * H : 0;
-    int64_t n;
-    const int64_t before = sum + block_scan(mine, scan_part, n);
-    if (at >= before && at < before + mine) {
-      found_b = b0 + tid;
-      found_begin = before;
-    }
-    sum += n;
-    if (at < sum) break;
-  }
-  __syncthreads();
-  int b = found_b;
-  int64_t seq_begin = found_begin;
+  KvRun run;
+  if (!kv_find_run(run, shared_run, P.c.n_seqs, gridDim.x, blockIdx.x,
+                   [&](int b) { return (int64_t)key_tiles_of(b) * H; }))
+    return;
+  int b = run.b;
+  int64_t at = run.at, seq_begin = run.begin;
+  const int64_t end = run.end;
   const float to_log2 = P.s.scale * 1.4426950408889634f;
 
   while (at < end) {

@@ -9,6 +9,7 @@ queued on the current (or the given) stream and synchronise nothing.
 from __future__ import annotations
 
 import ctypes as C
+import struct
 import threading
 
 import torch
@@ -62,17 +63,16 @@ def lib():
     if _lib is None:
         L = binding.lib()
         with _lock:
-            P = C.POINTER
-            L.unison_kv_attend_workspace.argtypes = [P(KvCache), P(KvTree), C.c_int]
+            A, B = C.c_void_p, C.c_char_p  # a struct's address, a packed struct
+            L.unison_kv_attend_workspace.argtypes = [A, A, C.c_int]
             L.unison_kv_attend_workspace.restype = C.c_uint64
-            L.unison_kv_attend.argtypes = [P(KvCache), P(KvTree), P(KvStep), C.c_void_p, C.c_uint64, C.c_void_p]
-            L.unison_kv_observe.argtypes = [P(KvCache), P(KvTree), P(KvStep), P(KvPath), C.c_void_p]
+            L.unison_kv_attend.argtypes = [A, A, B, A, C.c_uint64, A]
+            L.unison_kv_observe.argtypes = [A, A, B, B, A]
             L.unison_kv_commit.argtypes = L.unison_kv_observe.argtypes
-            L.unison_kv_evict_workspace.argtypes = [P(KvCache)]
+            L.unison_kv_evict_workspace.argtypes = [A]
             L.unison_kv_evict_workspace.restype = C.c_uint64
-            L.unison_kv_evict.argtypes = [P(KvCache), P(KvCache), C.c_void_p, C.c_int32, C.c_int32, C.c_void_p,
-                                          C.c_uint64, C.c_void_p]
-            L.unison_kv_verify.argtypes = [P(KvTree), P(KvVerify), C.c_void_p]
+            L.unison_kv_evict.argtypes = [A, A, A, C.c_int32, C.c_int32, A, C.c_uint64, A]
+            L.unison_kv_verify.argtypes = [A, B, A]
             _lib = L
     return _lib
 
@@ -83,11 +83,11 @@ def _need(ok, what):
 
 
 def _dense(x, dtype, shape, what):
-    if x is not None:
-        _need(x.dtype == dtype and tuple(x.shape) == shape and x.is_contiguous(),
-              f"{what}: a contiguous {dtype} tensor of shape {shape} is wanted")
-        return x.data_ptr()
-    return None
+    if x is None:
+        return None
+    if x.dtype is not dtype or x.shape != shape or not x.is_contiguous():
+        raise ValueError(f"{what}: a contiguous {dtype} tensor of shape {shape} is wanted")
+    return x.data_ptr()
 
 
 class Cache:
@@ -124,7 +124,9 @@ class Cache:
             _dense(length, torch.int32, (n,), "length"), _dense(next_pos, torch.int32, (n,), "next_pos"),
             _dense(status, torch.int32, (n,), "status"), *k.stride()[:3], *v.stride()[:3], *m, n, pages, k.shape[0],
             k.shape[2], k.shape[1], k.shape[3], DTYPE[k.dtype], 0)
-        self.ref = C.byref(self.struct)
+        self.address = C.addressof(self.struct)
+        self.scale = self.head_dim ** -0.5
+        self.scratch = {}  # bytes of workspace by the sizes that they depend on
 
 
 class Tree:
@@ -143,112 +145,145 @@ class Tree:
         self.struct = KvTree(_dense(offsets, torch.int32, (self.n_seqs + 1,), "offsets"),
                              _dense(mask, torch.int64, (n,), "mask"), _dense(parent, torch.int32, (n,), "parent"),
                              self.n_seqs, n, max_tokens, 0)
-        self.ref = C.byref(self.struct)
+        self.address = C.addressof(self.struct)
 
 
-def _step(cache, tree, q, k_new, v_new, out, lse, mass_new, scale):
-    """The C struct of a step's tensors, each [token, head, head_dim] with a contiguous last axis."""
-    args, strides = [], []
-    for x, heads in ((q, None), (k_new, cache.n_heads), (v_new, cache.n_heads), (out, None)):
-        if x is None:
-            args.append(None)
-            strides += (0, 0)
-            continue
-        s, t = x.shape, x.stride()
-        if x.dtype != cache.dtype or len(s) != 3 or s[0] != tree.n_tokens or s[2] != cache.head_dim or t[2] != 1 or \
-                (heads is not None and s[1] != heads):
-            raise ValueError("step tensors: [token, head, head_dim] of the cache's type and sizes, last axis contiguous")
-        args.append(x.data_ptr())
-        strides += t[:2]
-    return KvStep(*args, None if lse is None else lse.data_ptr(), None if mass_new is None else mass_new.data_ptr(),
-                  *strides, 0 if q is None else q.shape[1], cache.head_dim ** -0.5 if scale is None else scale)
+# One packed unison_kv_step, unison_kv_path and unison_kv_verify_args: a call
+# passes the bytes, which ctypes hands over without a copy or a conversion per
+# field.
+_STEP = struct.Struct("=6Q8qif")
+_PATH = struct.Struct("=2Qq")
+_VERIFY = struct.Struct("=2Q2q6Qq2i")
+assert (_STEP.size, _PATH.size, _VERIFY.size) == (C.sizeof(KvStep), C.sizeof(KvPath), C.sizeof(KvVerify))
+_NO_STRIDES = (0, 0, 0)
+
+
+def _rows(cache, x, n, heads):
+    """(pointer, strides) of a step's tensor [n, heads, head_dim] of the cache's type, its last axis contiguous."""
+    s = x.stride()
+    if x.dtype is not cache.dtype or x.shape != (n, heads, cache.head_dim) or s[2] != 1:
+        raise ValueError(f"step tensors: {cache.dtype} [{n}, {heads}, {cache.head_dim}], last axis contiguous")
+    return x.data_ptr(), s
 
 
 def _path(tree, path, n_path):
     if path is None:
         return None
-    _need(path.dtype == torch.int32 and path.dim() == 2 and path.shape[0] == tree.n_seqs and path.stride(1) == 1 and
-          path.shape[1] >= tree.max_tokens, "path: int32 [session, max_tokens]")
-    return C.byref(KvPath(path.data_ptr(), _dense(n_path, torch.int32, (tree.n_seqs,), "n_path"), path.stride(0)))
+    s = path.stride()
+    if path.dtype is not torch.int32 or path.dim() != 2 or path.shape[0] != tree.n_seqs or s[1] != 1 or \
+            path.shape[1] < tree.max_tokens:
+        raise ValueError("path: int32 [session, max_tokens]")
+    return _PATH.pack(path.data_ptr(), _dense(n_path, torch.int32, (tree.n_seqs,), "n_path"), s[0])
 
 
-class _On:
-    """Allocations of a call belong to the stream that it is queued on."""
+def _queue(device, stream):
+    """The raw handle of a call's stream."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(device.index)
+    return getattr(stream, "cuda_stream", stream)
 
-    def __init__(self, stream):
-        self.given = stream
-        self.handle = binding._stream_handle(stream)
-        self.context = None
 
-    def __enter__(self):
-        if self.given is not None and hasattr(self.given, "cuda_stream"):
-            self.context = torch.cuda.stream(self.given)
-            self.context.__enter__()
-        return self.handle
-
-    def __exit__(self, *e):
-        if self.context is not None:
-            self.context.__exit__(*e)
+def _on(stream, call, *args, **kw):
+    """A call with a torch stream: what it allocates belongs to that stream."""
+    with torch.cuda.stream(stream):
+        return call(*args, **kw)
 
 
 def attend(cache: Cache, tree: Tree, q, k_new, v_new, scale=None, out=None, lse=None, workspace=None, stream=None):
     """unison_kv_attend: (out [token, q head, head_dim], lse float32 [token, q
     head]).  scale defaults to head_dim ** -0.5; workspace: a uint8 tensor of
     at least ``attend_workspace`` bytes, else one is allocated."""
-    with _On(stream) as handle:
-        out = torch.empty_like(q) if out is None else out
-        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if lse is None else lse
-        _need(out.shape == q.shape, "out: the shape of q")
-        _dense(lse, torch.float32, tuple(q.shape[:2]), "lse")
-        step = _step(cache, tree, q, k_new, v_new, out, lse, None, scale)
-        if workspace is None:
-            workspace = torch.empty(attend_workspace(cache, tree, q.shape[1]), dtype=torch.uint8, device=q.device)
-        binding._check("unison_kv_attend", lib().unison_kv_attend(
-            cache.ref, tree.ref, C.byref(step), workspace.data_ptr(), workspace.numel(), handle))
+    if isinstance(stream, torch.cuda.Stream):
+        return _on(stream, attend, cache, tree, q, k_new, v_new, scale, out, lse, workspace)
+    n, heads = tree.n_tokens, q.shape[1]
+    qp, qs = _rows(cache, q, n, heads)
+    kp, ks = _rows(cache, k_new, n, cache.n_heads)
+    vp, vs = _rows(cache, v_new, n, cache.n_heads)
+    if out is None:
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    op, os = _rows(cache, out, n, heads)
+    if lse is None:
+        lse = torch.empty(n, heads, dtype=torch.float32, device=cache.device)
+        lp = lse.data_ptr()
+    else:
+        lp = _dense(lse, torch.float32, (n, heads), "lse")
+    if workspace is None:
+        workspace = torch.empty(attend_workspace(cache, tree, heads), dtype=torch.uint8, device=cache.device)
+    rc = lib().unison_kv_attend(
+        cache.address, tree.address,
+        _STEP.pack(qp, kp, vp, op, lp, 0, qs[0], qs[1], ks[0], ks[1], vs[0], vs[1], os[0], os[1], heads,
+                   cache.scale if scale is None else scale),
+        workspace.data_ptr(), workspace.numel(), _queue(cache.device, stream))
+    if rc:
+        binding._check("unison_kv_attend", rc)
     return out, lse
 
 
 def attend_workspace(cache: Cache, tree: Tree, n_q_heads: int) -> int:
-    return int(lib().unison_kv_attend_workspace(cache.ref, tree.ref, n_q_heads))
+    """Bytes of scratch that attend takes (a function of the sizes alone)."""
+    key = tree.max_tokens, n_q_heads
+    n = cache.scratch.get(key)
+    if n is None:
+        n = cache.scratch[key] = int(lib().unison_kv_attend_workspace(cache.address, tree.address, n_q_heads))
+    return n
 
 
 def observe(cache: Cache, tree: Tree, q, lse, k_new, scale=None, path=None, n_path=None, mass_new=None, stream=None):
     """unison_kv_observe: adds to cache.mass; returns mass_new, float32 [token,
     head], the weight of the new tokens themselves."""
-    with _On(stream) as handle:
-        mass_new = torch.empty((tree.n_tokens, cache.n_heads), dtype=torch.float32, device=q.device) \
-            if mass_new is None else mass_new
-        _dense(mass_new, torch.float32, (tree.n_tokens, cache.n_heads), "mass_new")
-        _dense(lse, torch.float32, tuple(q.shape[:2]), "lse")
-        step = _step(cache, tree, q, k_new, None, None, lse, mass_new, scale)
-        binding._check("unison_kv_observe", lib().unison_kv_observe(
-            cache.ref, tree.ref, C.byref(step), _path(tree, path, n_path), handle))
+    if isinstance(stream, torch.cuda.Stream):
+        return _on(stream, observe, cache, tree, q, lse, k_new, scale, path, n_path, mass_new)
+    n, heads = tree.n_tokens, q.shape[1]
+    qp, qs = _rows(cache, q, n, heads)
+    kp, ks = _rows(cache, k_new, n, cache.n_heads)
+    lp = _dense(lse, torch.float32, (n, heads), "lse")
+    if mass_new is None:
+        mass_new = torch.empty(n, cache.n_heads, dtype=torch.float32, device=cache.device)
+    rc = lib().unison_kv_observe(
+        cache.address, tree.address,
+        _STEP.pack(qp, kp, 0, 0, lp, _dense(mass_new, torch.float32, (n, cache.n_heads), "mass_new"), qs[0], qs[1],
+                   ks[0], ks[1], 0, 0, 0, 0, heads, cache.scale if scale is None else scale),
+        _path(tree, path, n_path), _queue(cache.device, stream))
+    if rc:
+        binding._check("unison_kv_observe", rc)
     return mass_new
 
 
 def commit(cache: Cache, tree: Tree, k_new, v_new, mass_new=None, path=None, n_path=None, stream=None) -> None:
     """unison_kv_commit: the accepted tokens go into the pages, length and
     next_pos grow.  Without path every new token is accepted."""
-    _dense(mass_new, torch.float32, (tree.n_tokens, cache.n_heads), "mass_new")
-    step = _step(cache, tree, None, k_new, v_new, None, None, mass_new, 0.0)
-    binding._check("unison_kv_commit", lib().unison_kv_commit(
-        cache.ref, tree.ref, C.byref(step), _path(tree, path, n_path), binding._stream_handle(stream)))
+    n = tree.n_tokens
+    kp, ks = _rows(cache, k_new, n, cache.n_heads)
+    vp, vs = _rows(cache, v_new, n, cache.n_heads)
+    mp = _dense(mass_new, torch.float32, (n, cache.n_heads), "mass_new")
+    rc = lib().unison_kv_commit(
+        cache.address, tree.address,
+        _STEP.pack(0, kp, vp, 0, 0, mp or 0, 0, 0, ks[0], ks[1], vs[0], vs[1], 0, 0, 0, 0.0),
+        _path(tree, path, n_path), _queue(cache.device, stream))
+    if rc:
+        binding._check("unison_kv_commit", rc)
 
 
 def evict_workspace(cache: Cache) -> int:
-    return int(lib().unison_kv_evict_workspace(cache.ref))
+    """Bytes of scratch that evict takes (a function of the sizes alone)."""
+    n = cache.scratch.get("evict")
+    if n is None:
+        n = cache.scratch["evict"] = int(lib().unison_kv_evict_workspace(cache.address))
+    return n
 
 
 def evict(cache: Cache, keep, sink=0, recent=0, into: Cache | None = None, workspace=None, stream=None) -> None:
     """unison_kv_evict: at most keep[b] (int32 tensor) slots of each session
     stay, in place or, with ``into``, in another cache."""
-    _dense(keep, torch.int32, (cache.n_seqs,), "keep")
-    with _On(stream) as handle:
-        if workspace is None:
-            workspace = torch.empty(evict_workspace(cache), dtype=torch.uint8, device=cache.device)
-        binding._check("unison_kv_evict", lib().unison_kv_evict(
-            cache.ref, None if into is None else into.ref, keep.data_ptr(), sink, recent, workspace.data_ptr(),
-            workspace.numel(), handle))
+    if isinstance(stream, torch.cuda.Stream):
+        return _on(stream, evict, cache, keep, sink, recent, into, workspace)
+    if workspace is None:
+        workspace = torch.empty(evict_workspace(cache), dtype=torch.uint8, device=cache.device)
+    rc = lib().unison_kv_evict(
+        cache.address, None if into is None else into.address, _dense(keep, torch.int32, (cache.n_seqs,), "keep"), sink,
+        recent, workspace.data_ptr(), workspace.numel(), _queue(cache.device, stream))
+    if rc:
+        binding._check("unison_kv_evict", rc)
 
 
 def verify(tree: Tree, token, p, q, u, u_sample, path=None, n_path=None, next_token=None, stream=None):
@@ -256,22 +291,32 @@ def verify(tree: Tree, token, p, q, u, u_sample, path=None, n_path=None, next_to
     next_token [session]), all int32.  p, q: [token, vocab] probabilities of
     one type (q None: certain drafts); token int32 [token]; u float32 [token];
     u_sample float32 [session]."""
-    n, t = tree.n_seqs, tree.max_tokens
-    for x in (p, q):
-        _need(x is None or (x.dim() == 2 and x.dtype == p.dtype and x.dtype in DTYPE and x.stride(1) == 1 and
-                            x.shape == (tree.n_tokens, p.shape[1])), "p, q: [token, vocab] of one type")
-    with _On(stream) as handle:
-        new = lambda *s: torch.empty(s, dtype=torch.int32, device=p.device)  # noqa: E731
-        path = new(n, t) if path is None else path
-        n_path = new(n) if n_path is None else n_path
-        next_token = new(n) if next_token is None else next_token
-        _need(path.dtype == torch.int32 and path.dim() == 2 and path.shape[0] == n and path.shape[1] >= t and
-              path.stride(1) == 1, "path: int32 [session, max_tokens]")
-        args = KvVerify(
-            p.data_ptr(), None if q is None else q.data_ptr(), p.stride(0), 0 if q is None else q.stride(0),
-            _dense(token, torch.int32, (tree.n_tokens,), "token"), _dense(u, torch.float32, (tree.n_tokens,), "u"),
-            _dense(u_sample, torch.float32, (n,), "u_sample"), path.data_ptr(),
-            _dense(n_path, torch.int32, (n,), "n_path"), _dense(next_token, torch.int32, (n,), "next_token"),
-            path.stride(0), p.shape[1], DTYPE[p.dtype])
-        binding._check("unison_kv_verify", lib().unison_kv_verify(tree.ref, C.byref(args), handle))
+    if isinstance(stream, torch.cuda.Stream):
+        return _on(stream, verify, tree, token, p, q, u, u_sample, path, n_path, next_token)
+    n, t, total, device = tree.n_seqs, tree.max_tokens, tree.n_tokens, p.device
+    dtype, vocab, ps, qs = p.dtype, p.shape[-1], p.stride(), _NO_STRIDES
+    ok = dtype in DTYPE and p.shape == (total, vocab) and ps[1] == 1
+    if q is not None:
+        qs = q.stride()
+        ok = ok and q.dtype is dtype and q.shape == (total, vocab) and qs[1] == 1
+    _need(ok, "p, q: [token, vocab] of one type, last axis contiguous")
+    if path is None:
+        path = torch.empty(n, t, dtype=torch.int32, device=device)
+    if n_path is None:
+        n_path = torch.empty(n, dtype=torch.int32, device=device)
+    if next_token is None:
+        next_token = torch.empty(n, dtype=torch.int32, device=device)
+    s = path.stride()
+    _need(path.dtype is torch.int32 and path.dim() == 2 and path.shape[0] == n and path.shape[1] >= t and s[1] == 1,
+          "path: int32 [session, max_tokens]")
+    rc = lib().unison_kv_verify(
+        tree.address,
+        _VERIFY.pack(p.data_ptr(), 0 if q is None else q.data_ptr(), ps[0], qs[0],
+                     _dense(token, torch.int32, (total,), "token"), _dense(u, torch.float32, (total,), "u"),
+                     _dense(u_sample, torch.float32, (n,), "u_sample"), path.data_ptr(),
+                     _dense(n_path, torch.int32, (n,), "n_path"), _dense(next_token, torch.int32, (n,), "next_token"),
+                     s[0], vocab, DTYPE[dtype]),
+        _queue(device, stream))
+    if rc:
+        binding._check("unison_kv_verify", rc)
     return path, n_path, next_token

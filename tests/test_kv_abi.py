@@ -40,7 +40,9 @@ class _Args:
         self.into = _made().cache(kv)
         self.out, self.lse = torch.zeros_like(m.q), torch.zeros(m.q.shape[:2])
         self.mass_new = torch.zeros(m.total, m.hkv)
-        self.step = kv._step(self.cache, self.tree, m.q, m.k_new, m.v_new, self.out, self.lse, self.mass_new, 0.1)
+        strides = [s for x in (m.q, m.k_new, m.v_new, self.out) for s in x.stride()[:2]]
+        self.step = kv.KvStep(*(x.data_ptr() for x in (m.q, m.k_new, m.v_new, self.out, self.lse, self.mass_new)),
+                              *strides, m.q.shape[1], 0.1)
         self.path_t = torch.zeros(2, 3, dtype=torch.int32)
         self.path = kv.KvPath(self.path_t.data_ptr(), self.path_t.data_ptr(), 3)
         self.work = torch.zeros(64 << 20, dtype=torch.uint8)
@@ -54,21 +56,21 @@ class _Args:
                              i.data_ptr(), i.data_ptr(), i.data_ptr(), 3, 100, 2)
 
     def attend(self):
-        return self.L.unison_kv_attend(self.cache.ref, self.tree.ref, C.byref(self.step), self.work.data_ptr(),
+        return self.L.unison_kv_attend(self.cache.address, self.tree.address, bytes(self.step), self.work.data_ptr(),
                                        self.bytes, None)
 
     def observe(self):
-        return self.L.unison_kv_observe(self.cache.ref, self.tree.ref, C.byref(self.step), C.byref(self.path), None)
+        return self.L.unison_kv_observe(self.cache.address, self.tree.address, bytes(self.step), bytes(self.path), None)
 
     def commit(self):
-        return self.L.unison_kv_commit(self.cache.ref, self.tree.ref, C.byref(self.step), C.byref(self.path), None)
+        return self.L.unison_kv_commit(self.cache.address, self.tree.address, bytes(self.step), bytes(self.path), None)
 
     def evict(self):
-        return self.L.unison_kv_evict(self.cache.ref, self.into.ref, self.keep, self.sink, self.recent,
+        return self.L.unison_kv_evict(self.cache.address, self.into.address, self.keep, self.sink, self.recent,
                                       self.work.data_ptr(), self.bytes, None)
 
     def verify(self):
-        return self.L.unison_kv_verify(self.tree.ref, C.byref(self.v), None)
+        return self.L.unison_kv_verify(self.tree.address, bytes(self.v), None)
 
 
 ARG, RANGE = -1, -4
@@ -133,14 +135,14 @@ def test_refusals(kv, i):
 
 def test_null_structs_are_refused(kv):
     a, L = _Args(kv), kv.lib()
-    assert L.unison_kv_attend(None, a.tree.ref, C.byref(a.step), a.work.data_ptr(), a.bytes, None) == ARG
-    assert L.unison_kv_attend(a.cache.ref, None, C.byref(a.step), a.work.data_ptr(), a.bytes, None) == ARG
-    assert L.unison_kv_attend(a.cache.ref, a.tree.ref, None, a.work.data_ptr(), a.bytes, None) == ARG
-    assert L.unison_kv_observe(a.cache.ref, a.tree.ref, None, None, None) == ARG
-    assert L.unison_kv_commit(a.cache.ref, a.tree.ref, None, None, None) == ARG
+    assert L.unison_kv_attend(None, a.tree.address, bytes(a.step), a.work.data_ptr(), a.bytes, None) == ARG
+    assert L.unison_kv_attend(a.cache.address, None, bytes(a.step), a.work.data_ptr(), a.bytes, None) == ARG
+    assert L.unison_kv_attend(a.cache.address, a.tree.address, None, a.work.data_ptr(), a.bytes, None) == ARG
+    assert L.unison_kv_observe(a.cache.address, a.tree.address, None, None, None) == ARG
+    assert L.unison_kv_commit(a.cache.address, a.tree.address, None, None, None) == ARG
     assert L.unison_kv_evict(None, None, a.keep, 0, 0, a.work.data_ptr(), a.bytes, None) == ARG
-    assert L.unison_kv_verify(None, C.byref(a.v), None) == ARG
-    assert L.unison_kv_verify(a.tree.ref, None, None) == ARG
+    assert L.unison_kv_verify(None, bytes(a.v), None) == ARG
+    assert L.unison_kv_verify(a.tree.address, None, None) == ARG
     assert L.unison_kv_attend_workspace(None, None, 8) == 0
     assert L.unison_kv_evict_workspace(None) == 0
 
