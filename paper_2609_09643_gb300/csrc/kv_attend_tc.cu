@@ -36,7 +36,7 @@ struct TcShared {
   KvRunShared run;
   uint64_t kv_full[kSlots<DP>], kv_free[kSlots<DP>], q_full, q_free, s_full[2], p_full[2], pv_done[2], idle;
   uint32_t row_ok[8][4];  // which keys of a tile exist
-  int odd[4];             // whether a segment's new values hold infinities or NaN
+  bool odd[4][4];         // whether new values that a copying warp read hold infinities or NaN, of four segments
   uint32_t tmem;
   volatile int dead;
 };
@@ -68,7 +68,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const AttendPara
 
   if (tid == 0) {
     for (int i = 0; i < kSlots<DP>; i++) {
-      bar_init(smem_u32(&sh.kv_full[i]), 128);
+      bar_init(smem_u32(&sh.kv_full[i]), 128 + 4);  // every copying thread, and every warp's own stores
       bar_init(smem_u32(&sh.kv_free[i]), 1);
     }
     bar_init(smem_u32(&sh.q_full), 128);
@@ -120,25 +120,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const AttendPara
     const int chunk = lane % kChunks, sub = lane / kChunks;
     const T *dummy = static_cast<const T *>(P.s.q);
     int item = 0, tile_no = 0, seg_no = 0;
-    uint32_t pending = 0;  // barrier of the copies that are still on their way
     bool ok = true;
-    auto arrive_later = [&](uint32_t bar) {
-      cp_commit();
-      if (pending) {
-        cp_wait<1>();
-        fence_to_tensor();
-        bar_arrive(pending);
-      }
-      pending = bar;
-    };
-    auto flush = [&]() {
-      cp_wait<0>();
-      if (pending) {
-        fence_to_tensor();
-        bar_arrive(pending);
-      }
-      pending = 0;
-    };
     // Copies this warp's 32 rows of a tile; lane i knows row i's address.
     auto copy_rows = [&](uint32_t dst, const T *mine) {
 #pragma unroll 4
@@ -167,7 +149,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const AttendPara
       };
       int off;
       int page = find_page(g.kt0, off);
-      if (w == 0 && lane == 0) sh.odd[seg_no & 3] = 0;
+      bool odd = false;
       for (int kt = g.kt0; kt < g.kt1 && ok; kt++) {
         const T *k = nullptr, *v = nullptr;
         if (kt == last_tile) {
@@ -181,14 +163,17 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const AttendPara
           v = static_cast<const T *>(P.c.v) + page * P.c.v_page + g.head * P.c.v_head + off * P.c.v_slot;
         }
         const uint32_t there = __ballot_sync(~0u, k != nullptr);
-        if (lane == 0) sh.row_ok[tile_no & 7][w] = there;
-        tile_no++;
         if (kt + 1 < g.kt1) page = find_page(kt + 1, off);
         uint32_t bar;
         uint32_t dst = slot_for(bar);
         if (!ok) break;
         copy_rows(dst, k);
-        arrive_later(bar);
+        bar_arrive_copied(bar);
+        if (lane == 0) {
+          sh.row_ok[tile_no & 7][w] = there;
+          bar_arrive(bar);
+        }
+        tile_no++;
         if (kt == g.kt0) {  // the segment's query rows: when the last segment's products have read theirs
           if (seg_no > 0) ok = __all_sync(~0u, bar_wait(smem_u32(&sh.q_free), (seg_no - 1) & 1, &sh.dead));
           if (!ok) break;
@@ -200,17 +185,17 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const AttendPara
                     (g.head * G + row % G) * P.s.q_head;
             copy_rows(q_base + q * kTileBytes, src);
           }
-          arrive_later(smem_u32(&sh.q_full));
+          bar_arrive_copied(smem_u32(&sh.q_full));
         }
         dst = slot_for(bar);
         if (!ok) break;
         copy_rows(dst, v);
-        arrive_later(bar);
-        if (kt == last_tile) {
+        if (kt < last_tile) {
+          bar_arrive_copied(bar);
+        } else {
           // A new token that a row does not see must not reach it as 0 * inf:
           // such values become 0 here and are put back, row by row, at the end.
-          cp_wait<0>();
-          bool odd = false;
+          asm volatile("cp.async.wait_all;" ::: "memory");
           for (int r = 0; r < 32; r += kRowsAtOnce) {
             const uint32_t a = operand_chunk(dst, kTile, w * 32 + r + sub, chunk);
             uint32_t x[4];
@@ -227,13 +212,17 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const AttendPara
               odd = true;
             }
           }
-          if (odd) sh.odd[seg_no & 3] = 1;
-          flush();
+          odd = __any_sync(~0u, odd);
+          bar_arrive(bar);
+        }
+        if (lane == 0) {
+          sh.odd[seg_no & 3][w] = odd;
+          bar_arrive(bar);
         }
       }
       seg_no++;
     }
-    flush();
+    asm volatile("cp.async.wait_all;" ::: "memory");
   } else if (warp >= kIssueWarp) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOthers));
     if (warp == kIssueWarp && lane == 0) {
@@ -245,6 +234,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const AttendPara
       auto take = [&](int &s) -> uint32_t {  // waits for the next slot's tile
         s = item % kSlots<DP>;
         ok = ok && bar_wait(smem_u32(&sh.kv_full[s]), (item / kSlots<DP>) & 1, &sh.dead);
+        fence_to_tensor();
         item++;
         return slot_base + s * kTileBytes;
       };
@@ -276,6 +266,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const AttendPara
         int ks, vs;
         uint32_t keys = take(ks);
         ok = ok && bar_wait(smem_u32(&sh.q_full), seg_no & 1, &sh.dead);
+        fence_to_tensor();
         if (!ok) break;
         for (int q = 0; q < tiles; q++) scores(q, keys);
         products_done(smem_u32(&sh.kv_free[ks]));
@@ -373,21 +364,25 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const AttendPara
           m = to;
         }
         const float base = m == -INFINITY ? 0.f : m;
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        uint64_t sum[2] = {0, 0};
+        const uint64_t cc = pair(c, c), bb = pair(-base, -base);
 #pragma unroll
         for (int i = 0; i < 128; i += 32) {
           uint32_t p[16];
 #pragma unroll
           for (int j = 0; j < 32; j += 2) {
-            const float a = exp2_fast(fmaf(__uint_as_float(x[i + j]), c, -base));
-            const float b = exp2_fast(fmaf(__uint_as_float(x[i + j + 1]), c, -base));
-            sum[j & 2] += a;
-            sum[(j & 2) + 1] += b;
+            float a, b;
+            unpair(fma_pair(pair(__uint_as_float(x[i + j]), __uint_as_float(x[i + j + 1])), cc, bb), a, b);
+            a = exp2_fast(a);
+            b = exp2_fast(b);
+            sum[j >> 1 & 1] = add_pair(sum[j >> 1 & 1], pair(a, b));
             p[j / 2] = KvType<T>::pack(a, b);
           }
           tmem_st16(s_addr + i / 2, p);
         }
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        float more, less;
+        unpair(add_pair(sum[0], sum[1]), more, less);
+        l += more + less;
         tmem_wait_st();
         tmem_before_sync();
         bar_arrive(smem_u32(&sh.p_full[q]));
@@ -402,7 +397,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const AttendPara
       if (!ok) break;
       tmem_after_sync();
       const bool whole = g.kt0 == 0 && g.kt1 == g.tiles;
-      const bool odd = g.kt1 == g.tiles && sh.odd[mine & 3];
+      const bool *flags = sh.odd[mine & 3];
+      const bool odd = g.kt1 == g.tiles && (flags[0] || flags[1] || flags[2] || flags[3]);
       const float inv = l == 0.f ? 0.f : 1.f / l;
       float *part = P.partial + ((int64_t)blockIdx.x * 2 + (g.kt0 == 0 ? 1 : 0)) * (kTcRows * (DP + 2));
       const int pr = q * 128 + r;

@@ -1,5 +1,5 @@
 // Attention weight of accepted tokens on every cached token (unison_kv_observe).
-#include "kv.cuh"
+#include "kv_observe.cuh"
 
 namespace unison {
 namespace {
@@ -7,19 +7,6 @@ namespace {
 constexpr int kThreads = 128;
 constexpr int kTile = 64;   // keys of a tile: 16 of each warp
 constexpr int kStages = 3;
-
-struct ObserveParams {
-  unison_kv_cache c;
-  unison_kv_tree t;
-  unison_kv_step s;
-  unison_kv_path path;
-  int group;
-};
-
-// Accepted nodes of a session.
-__device__ __forceinline__ int path_count(const ObserveParams &P, int b, int tokens) {
-  return P.path.path ? min(max(P.path.n_path[b], 0), tokens) : tokens;
-}
 
 template <int DP, int QR>
 constexpr int kObserveSmem = kStages *kTile *DP * 2 + QR *DP * 2;
@@ -42,11 +29,7 @@ __global__ void __launch_bounds__(kThreads) observe_kernel(const ObserveParams P
   const uint32_t k_base = smem_u32(smem);
   const uint32_t q_base = k_base + kStages * kTile * DP * 2;
 
-  auto key_tiles_of = [&](int b) -> int {
-    const int tokens = kv_tokens(P.t, b, P.c.status).count;
-    if (!tokens) return 0;
-    return path_count(P, b, tokens) ? (kv_length(P.c, b) + kTile - 1) / kTile + 1 : 1;
-  };
+  auto key_tiles_of = [&](int b) -> int { return observe_key_tiles(P, b, kTile); };
   KvRun run;
   if (!kv_find_run(run, shared_run, P.c.n_seqs, gridDim.x, blockIdx.x,
                    [&](int b) { return (int64_t)key_tiles_of(b) * H; }))
@@ -75,9 +58,8 @@ __global__ void __launch_bounds__(kThreads) observe_kernel(const ObserveParams P
     auto load_rows = [&](int row0) {  // QR query rows with their statistics
       for (int i = tid; i < QR * kChunks; i += kThreads) {
         const int r = row0 + i / kChunks, c = i % kChunks;
-        int node = 0;
-        if (r < rows) node = P.path.path ? P.path.path[(int64_t)b * P.path.path_stride + r / G] : r / G;
-        const bool ok = r < rows && (unsigned)node < (unsigned)tok.count;
+        const int node = r < rows ? observe_node(P, b, tok.count, r / G) : -1;
+        const bool ok = node >= 0;
         const T *src = static_cast<const T *>(P.s.q);
         if (ok) src += (tok.first + node) * P.s.q_token + (head * G + r % G) * P.s.q_head;
         cp_async16(swizzled<DP>(q_base, i / kChunks, c), c * 8 < D ? src + c * 8 : src, ok && c * 8 < D);
@@ -231,9 +213,9 @@ int observe_run(const ObserveParams &p, void *stream) {
 template <typename T>
 int observe_pick(const ObserveParams &p, int max_rows, void *stream) {
   const int d = p.c.head_dim;
-  if (d <= 64) return max_rows <= 64 ? observe_run<T, 64, 64>(p, stream) : observe_run<T, 64, 512>(p, stream);
-  if (d <= 128) return max_rows <= 64 ? observe_run<T, 128, 64>(p, stream) : observe_run<T, 128, 512>(p, stream);
-  return max_rows <= 64 ? observe_run<T, 256, 64>(p, stream) : observe_run<T, 256, 192>(p, stream);
+  if (d <= 128 && max_rows <= kObserveTcRows)
+    return d <= 64 ? observe_tc<T, 64>(p, max_rows, stream) : observe_tc<T, 128>(p, max_rows, stream);
+  return d <= 128 ? observe_run<T, 128, 512>(p, stream) : observe_run<T, 256, 192>(p, stream);
 }
 
 }  // namespace
@@ -256,7 +238,7 @@ extern "C" int unison_kv_observe(const unison_kv_cache *cache, const unison_kv_t
       (!kv_rows_ok(cache->k, cache->k_page | cache->k_head, cache->k_slot) || !cache->mass))
     return UNISON_ERR_ARG;
   if (path && path->path && (!path->n_path || path->path_stride < 0)) return UNISON_ERR_ARG;
-  ObserveParams p;
+  ObserveParams p = {};
   p.c = *cache;
   p.t = *tree;
   p.s = *step;

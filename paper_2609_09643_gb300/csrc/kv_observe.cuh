@@ -1,0 +1,39 @@
+// What the kernels of unison_kv_observe share.
+#pragma once
+
+#include "kv.cuh"
+
+namespace unison {
+
+struct ObserveParams {
+  unison_kv_cache c;
+  unison_kv_tree t;
+  unison_kv_step s;
+  unison_kv_path path;
+  int group;         // query heads of a KV head
+  int q_rows, slots;  // tensor cores: query rows that fit, key tiles on their way
+};
+
+// Accepted nodes of a session.
+__device__ __forceinline__ int path_count(const ObserveParams &P, int b, int tokens) {
+  return P.path.path ? min(max(P.path.n_path[b], 0), tokens) : tokens;
+}
+// Key tiles of a session; the last one holds its new tokens, the only one
+// where no token was accepted.
+__device__ __forceinline__ int observe_key_tiles(const ObserveParams &P, int b, int tile) {
+  const int tokens = kv_tokens(P.t, b, P.c.status).count;
+  if (!tokens) return 0;
+  return path_count(P, b, tokens) ? (kv_length(P.c, b) + tile - 1) / tile + 1 : 1;
+}
+
+// Query row r of a session's accepted path, as a token of the session, or -1.
+__device__ __forceinline__ int observe_node(const ObserveParams &P, int b, int tokens, int i) {
+  const int node = P.path.path ? P.path.path[(int64_t)b * P.path.path_stride + i] : i;
+  return (unsigned)node < (unsigned)tokens ? node : -1;
+}
+
+constexpr int kObserveTcRows = 512;  // most query rows per KV head on the tensor cores
+template <typename T, int DP>
+int observe_tc(ObserveParams p, int max_rows, void *stream);
+
+}  // namespace unison

@@ -1,0 +1,367 @@
+// Attention weight on cached keys by the tensor cores (the variant of
+// unison_kv_observe for head sizes up to 128 and up to 512 query rows).
+//
+// The keys are the rows of the product and the query rows its columns: a
+// thread owns a key, reads its scores from tensor memory, and adds their
+// weights in its registers, so nothing is exchanged between threads and no
+// atomics are needed.  A CTA keeps the query rows of one segment (session and
+// KV head) in shared memory and streams tiles of 128 keys past them.  Roles:
+//   warps 8-11      copy key tiles and, per segment, the query rows
+//   warp 12         issues the products, 128 query rows at a time, into four
+//                   buffers of tensor memory
+//   warps 0-3, 4-7  turn the scores of a buffer into weights, in turn
+#include "kv_observe.cuh"
+#include "kv_tc.cuh"
+
+namespace unison {
+namespace {
+
+constexpr int kThreads = 416;
+constexpr int kTile = 128;
+constexpr int kCopyWarp = 8, kIssueWarp = 12;
+constexpr int kBuffers = 4, kMostSlots = 6;
+constexpr int kNodes = UNISON_KV_MAX_TOKENS;
+// Tiles whose keys' accounts are kept in shared memory: those on their way,
+// those in tensor memory, and the two that are being finished.
+constexpr int kMarks = 16;
+constexpr int kMarkBytes = kMarks * kTile * 12;
+
+struct ObserveShared {
+  KvRunShared run;
+  uint64_t k_full[kMostSlots], k_free[kMostSlots], q_full, q_free, t_full[kBuffers], t_free[kBuffers], seg_done[2],
+      part_full, part_free, idle;
+  uint64_t mask[2][kNodes];  // of the accepted nodes
+  float part[kTile];         // the second group's sums
+  bool plain[2][4];          // whether every row that a copying warp read has weight to give
+  uint32_t tmem;
+  volatile int dead;
+};
+
+struct Segment {
+  int b, head, rows, tiles, kt0, kt1, len;
+  KvRange tok;
+};
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const ObserveParams P) {
+  constexpr uint32_t kTileBytes = kTile * DP * 2, kBlock = kTile * 128;
+  extern __shared__ unsigned char smem_raw[];
+  __shared__ ObserveShared sh;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int D = P.c.head_dim, H = P.c.n_heads, G = P.group;
+  const uint32_t q_base = (smem_u32(smem_raw) + 1023) & ~1023u, slot_base = q_base + P.q_rows * DP * 2;
+  // log-sums of the rows, of two segments, in log2 units and negated; -inf: no weight from this row
+  float *const lse_base = reinterpret_cast<float *>(smem_raw + (slot_base - smem_u32(smem_raw)) + P.slots * kTileBytes);
+
+  float **const marks_at = reinterpret_cast<float **>(lse_base + 2 * P.q_rows);  // where a key's weight goes
+  float *const marks_old = reinterpret_cast<float *>(marks_at + kMarks * kTile);  // what is there
+
+  KvRun run;
+  if (!kv_find_run(run, sh.run, P.c.n_seqs, gridDim.x, blockIdx.x,
+                   [&](int b) { return (int64_t)observe_key_tiles(P, b, kTile) * H; }))
+    return;
+  if (tid == 0) {
+    for (int i = 0; i < kMostSlots; i++) {
+      bar_init(smem_u32(&sh.k_full[i]), 256);  // copies, and stores, of every copying thread
+      bar_init(smem_u32(&sh.k_free[i]), 1);
+    }
+    for (int i = 0; i < kBuffers; i++) {
+      bar_init(smem_u32(&sh.t_full[i]), 2);
+      bar_init(smem_u32(&sh.t_free[i]), 128);
+    }
+    bar_init(smem_u32(&sh.q_full), 256);
+    bar_init(smem_u32(&sh.q_free), 1);
+    bar_init(smem_u32(&sh.seg_done[0]), 256);
+    bar_init(smem_u32(&sh.seg_done[1]), 256);
+    bar_init(smem_u32(&sh.part_full), 128);
+    bar_init(smem_u32(&sh.part_free), 128);
+    bar_init(smem_u32(&sh.idle), 1);
+    sh.dead = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == kIssueWarp) tmem_alloc(smem_u32(&sh.tmem), 512);
+  tmem_before_sync();
+  __syncthreads();
+  tmem_after_sync();
+  const uint32_t tmem = sh.tmem;
+
+  int b = run.b;
+  int64_t at = run.at, seq_begin = run.begin;
+  auto next_segment = [&](Segment &g) {
+    int64_t mine = (int64_t)observe_key_tiles(P, b, kTile) * H;
+    while (at >= seq_begin + mine) {
+      seq_begin += mine;
+      mine = (int64_t)observe_key_tiles(P, ++b, kTile) * H;
+    }
+    g.b = b;
+    g.tok = kv_tokens(P.t, b, nullptr);
+    g.len = kv_length(P.c, b);
+    g.rows = path_count(P, b, g.tok.count) * G;
+    g.tiles = observe_key_tiles(P, b, kTile);
+    g.head = (int)((at - seq_begin) / g.tiles);
+    const int64_t seg_begin = seq_begin + (int64_t)g.head * g.tiles;
+    g.kt0 = (int)(at - seg_begin);
+    g.kt1 = (int)min((int64_t)g.tiles, run.end - seg_begin);
+    at = seg_begin + g.kt1;
+  };
+
+  if (warp >= kCopyWarp && warp < kIssueWarp) {
+    // ------------------------------------------------------------- copies
+    const int w = warp - kCopyWarp, thread = tid - kCopyWarp * 32;
+    constexpr int kChunks = DP / 8, kRowsAtOnce = 32 / kChunks;
+    const int chunk = lane % kChunks, sub = lane / kChunks;
+    const T *dummy = static_cast<const T *>(P.s.q);
+    int item = 0, seg_no = 0, tile_no = 0;
+    bool ok = true;
+    // Copies this warp's 32 rows of 128; lane i knows row i's address.
+    auto copy_rows = [&](uint32_t dst, const T *mine) {
+#pragma unroll 8
+      for (int r = 0; r < 32; r += kRowsAtOnce) {
+        const T *src = reinterpret_cast<const T *>(__shfl_sync(~0u, reinterpret_cast<unsigned long long>(mine), r + sub));
+        const bool there = src != nullptr && chunk * 8 < D;
+        cp_async16(operand_chunk(dst, kTile, w * 32 + r + sub, chunk), there ? src + chunk * 8 : dummy, there);
+      }
+    };
+    while (at < run.end && ok) {
+      Segment g;
+      next_segment(g);
+      auto find_page = [&](int kt, int &off) -> int {
+        const int slot = kt * kTile + w * 32 + lane;
+        off = 0;
+        return kt < g.tiles - 1 && slot < g.len ? kv_page(P.c, g.b, slot, off) : -1;
+      };
+      int off;
+      int page = find_page(g.kt0, off);
+      for (int kt = g.kt0; kt < g.kt1; kt++) {
+        const T *k = nullptr;
+        float *m = nullptr;
+        if (kt == g.tiles - 1) {
+          const int j = w * 32 + lane;
+          if (j < g.tok.count && P.s.mass_new) {
+            k = static_cast<const T *>(P.s.k_new) + (g.tok.first + j) * P.s.k_token + g.head * P.s.k_head;
+            m = P.s.mass_new + (int64_t)(g.tok.first + j) * H + g.head;
+          }
+        } else if (page >= 0) {
+          k = static_cast<const T *>(P.c.k) + page * P.c.k_page + g.head * P.c.k_head + off * P.c.k_slot;
+          m = P.c.mass + page * P.c.m_page + g.head * P.c.m_head + off * P.c.m_slot;
+        }
+        if (kt + 1 < g.kt1) page = find_page(kt + 1, off);
+        const int s = item % P.slots, n = item / P.slots;
+        if (n > 0) ok = __all_sync(~0u, bar_wait(smem_u32(&sh.k_free[s]), (n - 1) & 1, &sh.dead));
+        if (!ok) break;
+        item++;
+        copy_rows(slot_base + s * kTileBytes, k);
+        const int mark = tile_no++ % kMarks * kTile + w * 32 + lane;
+        if (m && kt < g.tiles - 1)
+          asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(marks_old + mark)), "l"(m) : "memory");
+        bar_arrive_copied(smem_u32(&sh.k_full[s]));
+        marks_at[mark] = m;
+        bar_arrive(smem_u32(&sh.k_full[s]));
+        if (kt == g.kt0) {
+          // The segment's rows: when the last one's products have read theirs,
+          // and nobody reads the statistics of the one before any more.
+          if (seg_no > 0) ok = __all_sync(~0u, bar_wait(smem_u32(&sh.q_free), (seg_no - 1) & 1, &sh.dead));
+          if (ok && seg_no > 1) ok = __all_sync(~0u, bar_wait(smem_u32(&sh.seg_done[seg_no & 1]), ((seg_no >> 1) - 1) & 1, &sh.dead));
+          if (!ok) break;
+          float *lse = lse_base + (seg_no & 1) * P.q_rows;
+          bool plain = true;
+          for (int r0 = 0; r0 < g.rows; r0 += 128) {
+            const int r = r0 + w * 32 + lane;
+            const int node = r < g.rows ? observe_node(P, g.b, g.tok.count, r / G) : -1;
+            const T *src = nullptr;
+            float l = -INFINITY;
+            if (node >= 0) {
+              src = static_cast<const T *>(P.s.q) + (g.tok.first + node) * P.s.q_token + (g.head * G + r % G) * P.s.q_head;
+              l = P.s.lse[(int64_t)(g.tok.first + node) * P.s.n_q_heads + g.head * G + r % G] * -1.4426950408889634f;
+              if (l == INFINITY) l = -INFINITY;
+            }
+            if (r < g.rows && l == -INFINITY) plain = false;
+            lse[r] = l;
+            copy_rows(q_base + r0 / 128 * kTileBytes, src);
+          }
+          if (thread < kNodes) {
+            const int node = thread * G < g.rows ? observe_node(P, g.b, g.tok.count, thread) : -1;
+            sh.mask[seg_no & 1][thread] =
+                node < 0 ? 0 : P.t.mask ? P.t.mask[g.tok.first + node] : ~0ull >> (63 - node);
+          }
+          plain = __all_sync(~0u, plain);
+          if (lane == 0) sh.plain[seg_no & 1][w] = plain;
+          bar_arrive_copied(smem_u32(&sh.q_full));
+          bar_arrive(smem_u32(&sh.q_full));
+        }
+      }
+      seg_no++;
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+  } else if (warp == kIssueWarp && lane == 0) {
+    // ----------------------------------------------------------- products
+    int item = 0, seg_no = 0, job = 0;
+    bool ok = true;
+    while (at < run.end && ok) {
+      Segment g;
+      next_segment(g);
+      for (int kt = g.kt0; kt < g.kt1 && ok; kt++) {
+        const int s = item % P.slots;
+        ok = bar_wait(smem_u32(&sh.k_full[s]), (item / P.slots) & 1, &sh.dead);
+        if (ok && kt == g.kt0) ok = bar_wait(smem_u32(&sh.q_full), seg_no & 1, &sh.dead);
+        fence_to_tensor();
+        item++;
+        const uint32_t keys = slot_base + s * kTileBytes;
+        for (int r0 = 0; (r0 == 0 || r0 < g.rows) && ok; r0 += 128, job++) {
+          const int buf = job % kBuffers;
+          if (job >= kBuffers) ok = bar_wait(smem_u32(&sh.t_free[buf]), (job / kBuffers - 1) & 1, &sh.dead);
+          if (!ok) break;
+          tmem_after_sync();
+          const int columns = (max(min(g.rows - r0, 128), 1) + 15) & ~15;
+          const uint32_t shape = product_shape(kOperandType<T>, kTile, columns, false, false);
+#pragma unroll
+          for (int d = 0; d < DP / 16; d++) {
+            const uint32_t o = d / 4 * kBlock + d % 4 * 32;
+            product_ss(tmem + buf * 128, smem_operand(keys + o, kBlock),
+                       smem_operand(q_base + r0 / 128 * kTileBytes + o, kBlock), shape, d > 0);
+          }
+          products_done(smem_u32(&sh.t_full[buf]));
+          bar_arrive(smem_u32(&sh.t_full[buf]));  // hands on what the copies wrote besides
+        }
+        products_done(smem_u32(&sh.k_free[s]));
+      }
+      products_done(smem_u32(&sh.q_free));
+      seg_no++;
+    }
+    // nothing may still be at work when tensor memory is freed
+    products_done(smem_u32(&sh.idle));
+    for (int i = 0; i < 1 << 20 && !bar_try(smem_u32(&sh.idle), 0); i++) {
+    }
+  } else if (warp < kCopyWarp) {
+    // ------------------------------------------------------------ weights
+    const int wg = warp >> 2, key = tid & 127;
+    const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // this warp's quarter of the 128 lanes
+    const float c = P.s.scale * 1.4426950408889634f;
+    int job = 0, seg_no = 0, tile_no = 0, shared_tiles = 0;
+    bool ok = true;
+    while (at < run.end && ok) {
+      Segment g;
+      next_segment(g);
+      const float *lse = lse_base + (seg_no & 1) * P.q_rows;
+      const uint64_t *mask = sh.mask[seg_no & 1];
+      const int chunks = max((g.rows + 127) / 128, 1);
+      for (int kt = g.kt0; kt < g.kt1; kt++, tile_no++) {
+        const bool last = kt == g.tiles - 1;
+        // chunk by chunk in turn; a tile of one chunk is done by one group alone
+        const int first = chunks == 1 ? tile_no & 1 : 0;
+        const bool writes = wg == first;
+        uint64_t sum[2] = {0, 0};
+        for (int i = 0; i < chunks; i++, job++) {
+          if (((i + first) & 1) != wg) continue;
+          const int buf = job % kBuffers;
+          ok = __all_sync(~0u, bar_wait(smem_u32(&sh.t_full[buf]), (job / kBuffers) & 1, &sh.dead));
+          if (!ok) break;
+          tmem_after_sync();
+          const int n = min(g.rows - i * 128, 128);
+          const bool *plain = sh.plain[seg_no & 1];
+          const bool checked = last || !(plain[0] && plain[1] && plain[2] && plain[3]);
+          const uint32_t from = tmem + buf * 128 + lanes;
+          const float *l = lse + i * 128;
+          uint32_t x[2][32];
+          tmem_ld32(x[0], from);
+#pragma unroll
+          for (int r0 = 0; r0 < 128; r0 += 32) {
+            if (r0 < n) {
+              uint32_t(&v)[32] = x[r0 / 32 & 1];
+              tmem_wait_ld();
+              if (r0 + 32 < n) tmem_ld32(x[~(r0 / 32) & 1], from + r0 + 32);
+              if (!checked && r0 + 32 <= n) {
+                const uint64_t cc = pair(c, c);
+#pragma unroll
+                for (int j = 0; j < 32; j += 4) {
+                  const ulonglong2 y = *reinterpret_cast<const ulonglong2 *>(l + r0 + j);
+                  float e[4];
+                  unpair(fma_pair(pair(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), cc, y.x), e[0], e[1]);
+                  unpair(fma_pair(pair(__uint_as_float(v[j + 2]), __uint_as_float(v[j + 3])), cc, y.y), e[2], e[3]);
+                  sum[0] = add_pair(sum[0], pair(exp2_fast(e[0]), exp2_fast(e[1])));
+                  sum[1] = add_pair(sum[1], pair(exp2_fast(e[2]), exp2_fast(e[3])));
+                }
+              } else {
+                int node = (i * 128 + r0) / G, head = (i * 128 + r0) % G;
+#pragma unroll
+                for (int j = 0; j < 32; j += 2) {
+                  float e[2];
+#pragma unroll
+                  for (int h = 0; h < 2; h++) {
+                    const float y = l[r0 + j + h];
+                    const bool see = r0 + j + h < n && y != -INFINITY &&
+                                     (!last || (node < kNodes && key < 64 && mask[node] >> key & 1));
+                    e[h] = see ? exp2_fast(fmaf(__uint_as_float(v[j + h]), c, y)) : 0.f;
+                    if (++head == G) head = 0, node++;
+                  }
+                  sum[j >> 1 & 1] = add_pair(sum[j >> 1 & 1], pair(e[0], e[1]));
+                  if (r0 + j + 2 >= n) break;
+                }
+              }
+              __syncwarp();
+            }
+          }
+          tmem_before_sync();
+          bar_arrive(smem_u32(&sh.t_free[buf]));
+        }
+        if (!ok) break;
+        float all, other;
+        unpair(add_pair(sum[0], sum[1]), all, other);
+        all += other;
+        if (chunks > 1) {  // the two groups' sums, in this order
+          if (wg == 1) {
+            if (shared_tiles > 0) ok = bar_wait(smem_u32(&sh.part_free), (shared_tiles - 1) & 1, &sh.dead);
+            if (ok) sh.part[key] = all;
+            bar_arrive(smem_u32(&sh.part_full));
+          } else {
+            ok = bar_wait(smem_u32(&sh.part_full), shared_tiles & 1, &sh.dead);
+            if (ok) all += sh.part[key];
+            bar_arrive(smem_u32(&sh.part_free));
+          }
+          shared_tiles++;
+          ok = __all_sync(~0u, ok);
+          if (!ok) break;
+        }
+        if (writes) {
+          const int mark = tile_no % kMarks * kTile + key;
+          float *to = marks_at[mark];
+          if (to) *to = last ? all : marks_old[mark] + all;
+        }
+      }
+      if (!ok && key == 0 && P.c.status) P.c.status[g.b] = UNISON_ERR_TIMEOUT;
+      bar_arrive(smem_u32(&sh.seg_done[seg_no & 1]));
+      seg_no++;
+    }
+  }
+  __syncwarp();
+  tmem_before_sync();
+  __syncthreads();
+  if (warp == kIssueWarp) {
+    tmem_after_sync();
+    tmem_free(tmem, 512);
+  }
+}
+
+}  // namespace
+
+template <typename T, int DP>
+int observe_tc(ObserveParams p, int max_rows, void *stream) {
+  constexpr int kTileBytes = kTile * DP * 2;
+  constexpr int kMost = 226 << 10;
+  static uint64_t done = 0;
+  p.q_rows = (max_rows + 127) / 128 * 128;
+  const int fixed = 1024 + p.q_rows * (DP * 2 + 8) + kMarkBytes + (int)sizeof(ObserveShared);
+  p.slots = min(kMostSlots, (kMost - fixed) / kTileBytes);
+  const int bytes = fixed - (int)sizeof(ObserveShared) + p.slots * kTileBytes;
+  if (!kv_allow_smem(reinterpret_cast<const void *>(observe_tc_kernel<T, DP>), kMost - (int)sizeof(ObserveShared), &done))
+    return UNISON_ERR_CUDA;
+  return kv_launch("kv_observe", dim3(kv_sm_count()), dim3(kThreads), max(bytes, 120 << 10), stream, 1,
+                   observe_tc_kernel<T, DP>, p);
+}
+
+template int observe_tc<__nv_bfloat16, 64>(ObserveParams, int, void *);
+template int observe_tc<__nv_bfloat16, 128>(ObserveParams, int, void *);
+template int observe_tc<__half, 64>(ObserveParams, int, void *);
+template int observe_tc<__half, 128>(ObserveParams, int, void *);
+
+}  // namespace unison

@@ -27,6 +27,7 @@ def check_attend(kv, m, mask=None, cache=None, scale=None, **kw):
     tree = m.tree(kv)
     out, lse = kv.attend(cache, tree, m.q, m.k_new, m.v_new, scale, **kw)
     torch.cuda.synchronize()
+    assert not m.status.any()
     want, want_lse, tol, tol_lse = ref.attend(m, mask=mask, scale=scale)
     got, got_lse = f64(out), f64(lse)
     assert np.array_equal(np.isnan(got), np.isnan(want))
@@ -212,6 +213,7 @@ def check_observe(kv, m, paths=None, lse=None):
     before = f64(m.mass)
     new = kv.observe(cache, tree, m.q, lse, m.k_new, path=path, n_path=n_path)
     torch.cuda.synchronize()
+    assert not m.status.any()
     added, bound, want_new, bound_new = ref.observe(m, lse, paths)
     expect, tol = before.copy(), np.zeros(before.shape)
     for b, n in enumerate(m.lens):
