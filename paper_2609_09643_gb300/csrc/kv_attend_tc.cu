@@ -13,7 +13,7 @@
 // its weights are relative to; the sums are 32 bits wide, so weights up to 2^8
 // cost no accuracy.
 #include "kv_attend.cuh"
-#include "kv_tc.cuh"
+#include "kv_copy.cuh"
 
 namespace unison {
 namespace {
@@ -23,7 +23,7 @@ constexpr int kTile = 128;
 constexpr int kCopyWarp = 8, kIssueWarp = 12;
 // Registers of a thread that computes weights, and of the others: 256 threads
 // each, together what the launch has (512 x 128).
-constexpr int kRegsWeights = 192, kRegsOthers = 64;
+constexpr int kRegsWeights = 184, kRegsOthers = 72;
 constexpr float kSlack = 8.f;
 
 template <int DP>
@@ -47,8 +47,12 @@ struct Segment {
   KvRange tok;
 };
 
+struct AttendTcParams : AttendParams {
+  KvBoxes k_boxes, v_boxes;
+};
+
 template <typename T, int DP>
-__global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const AttendParams P) {
+__global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_constant__ AttendTcParams P) {
   constexpr uint32_t kTileBytes = kTile * DP * 2, kBlock = kTile * 128;
   extern __shared__ unsigned char smem_raw[];
   __shared__ TcShared<DP> sh;
@@ -68,10 +72,10 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const AttendPara
 
   if (tid == 0) {
     for (int i = 0; i < kSlots<DP>; i++) {
-      bar_init(smem_u32(&sh.kv_full[i]), 128 + 4);  // every copying thread, and every warp's own stores
+      bar_init(smem_u32(&sh.kv_full[i]), 4);  // copying warps
       bar_init(smem_u32(&sh.kv_free[i]), 1);
     }
-    bar_init(smem_u32(&sh.q_full), 128);
+    bar_init(smem_u32(&sh.q_full), 4);
     bar_init(smem_u32(&sh.q_free), 1);
     bar_init(smem_u32(&sh.idle), 1);
     for (int i = 0; i < 2; i++) {
@@ -116,23 +120,13 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const AttendPara
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOthers));
     // ------------------------------------------------------------- copies
     const int w = warp - kCopyWarp;
-    constexpr int kChunks = DP / 8, kRowsAtOnce = 32 / kChunks;
-    const int chunk = lane % kChunks, sub = lane / kChunks;
-    const T *dummy = static_cast<const T *>(P.s.q);
+    KvCopier<T, DP> copier(w, lane, D, P.s.q);
     int item = 0, tile_no = 0, seg_no = 0;
+    const bool by_boxes = P.k_boxes.rows && P.v_boxes.rows;
     bool ok = true;
-    // Copies this warp's 32 rows of a tile; lane i knows row i's address.
-    auto copy_rows = [&](uint32_t dst, const T *mine) {
-#pragma unroll 4
-      for (int r = 0; r < 32; r += kRowsAtOnce) {
-        const T *src = reinterpret_cast<const T *>(__shfl_sync(~0u, reinterpret_cast<unsigned long long>(mine), r + sub));
-        const bool there = src != nullptr && chunk * 8 < D;
-        cp_async16(operand_chunk(dst, kTile, w * 32 + r + sub, chunk), there ? src + chunk * 8 : dummy, there);
-      }
-    };
     auto slot_for = [&](uint32_t &bar) -> uint32_t {  // waits until the next slot is free
       const int s = item % kSlots<DP>, n = item / kSlots<DP>;
-      if (n > 0) ok = __all_sync(~0u, bar_wait(smem_u32(&sh.kv_free[s]), (n - 1) & 1, &sh.dead));
+      if (n > 0) ok = copier.wait(smem_u32(&sh.kv_free[s]), (n - 1) & 1, &sh.dead);
       item++;
       bar = smem_u32(&sh.kv_full[s]);
       return slot_base + s * kTileBytes;
@@ -142,121 +136,144 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const AttendPara
       next_segment(g);
       if (g.rows <= 0) continue;
       const int last_tile = g.tiles - 1;
-      auto find_page = [&](int kt, int &off) -> int {
-        const int slot = kt * kTile + w * 32 + lane;
-        off = 0;
-        return kt < last_tile && slot < g.len ? kv_page(P.c, g.b, slot, off) : -1;
-      };
-      int off;
-      int page = find_page(g.kt0, off);
-      bool odd = false;
-      for (int kt = g.kt0; kt < g.kt1 && ok; kt++) {
-        const T *k = nullptr, *v = nullptr;
-        if (kt == last_tile) {
-          const int j = w * 32 + lane;
-          if (j < g.tok.count) {
-            k = static_cast<const T *>(P.s.k_new) + (g.tok.first + j) * P.s.k_token + g.head * P.s.k_head;
-            v = static_cast<const T *>(P.s.v_new) + (g.tok.first + j) * P.s.v_token + g.head * P.s.v_head;
+      // the query rows: when the last segment's products have read theirs
+      if (seg_no > 0) ok = copier.wait(smem_u32(&sh.q_free), (seg_no - 1) & 1, &sh.dead);
+      if (!ok) break;
+      for (int q = 0; q < (g.rows > 128 ? 2 : 1); q++) {
+        const int r = q * 128 + w * 32 + lane, row = g.row_tile * kTcRows + r;
+        const T *src = nullptr;
+        if (r < g.rows)
+          src = static_cast<const T *>(P.s.q) + (g.tok.first + row / G) * P.s.q_token + (g.head * G + row % G) * P.s.q_head;
+        copier.rows(q_base + q * kTileBytes, src);
+      }
+      copier.issued(smem_u32(&sh.q_full));
+      int kt = g.kt0;
+      const int boxed = by_boxes ? min(g.kt1, g.len / kTile) : kt;  // full tiles go by boxes
+      if (w > 0) {
+        // (the other warps keep step: a barrier's parity tells only its last phase)
+        if (kt < boxed) copier.landed();
+        for (; kt < boxed && ok; kt++, tile_no++)
+          for (int part = 0; part < 2; part++) {
+            uint32_t bar;
+            slot_for(bar);
+            if (!ok) break;
+            if (lane == 0) bar_arrive(bar);
           }
-        } else if (page >= 0) {
-          k = static_cast<const T *>(P.c.k) + page * P.c.k_page + g.head * P.c.k_head + off * P.c.k_slot;
-          v = static_cast<const T *>(P.c.v) + page * P.c.v_page + g.head * P.c.v_head + off * P.c.v_slot;
-        }
-        const uint32_t there = __ballot_sync(~0u, k != nullptr);
-        if (kt + 1 < g.kt1) page = find_page(kt + 1, off);
-        uint32_t bar;
-        uint32_t dst = slot_for(bar);
-        if (!ok) break;
-        copy_rows(dst, k);
-        bar_arrive_copied(bar);
-        if (lane == 0) {
-          sh.row_ok[tile_no & 7][w] = there;
-          bar_arrive(bar);
-        }
-        tile_no++;
-        if (kt == g.kt0) {  // the segment's query rows: when the last segment's products have read theirs
-          if (seg_no > 0) ok = __all_sync(~0u, bar_wait(smem_u32(&sh.q_free), (seg_no - 1) & 1, &sh.dead));
+      } else {
+        const int boxes = by_boxes ? kTile / P.k_boxes.rows : 0;
+        int page = -1, off = 0;
+        auto find_box = [&](int kt) {
+          if (lane < boxes) page = kv_page(P.c, g.b, kt * kTile + lane * P.k_boxes.rows, off);
+        };
+        if (kt < boxed) find_box(kt);
+        for (; kt < boxed; kt++, tile_no++) {
+          uint32_t bar;
+          uint32_t dst = slot_for(bar);
           if (!ok) break;
-          for (int q = 0; q < (g.rows > 128 ? 2 : 1); q++) {
-            const int r = q * 128 + w * 32 + lane, row = g.row_tile * kTcRows + r;
-            const T *src = nullptr;
-            if (r < g.rows)
-              src = static_cast<const T *>(P.s.q) + (g.tok.first + row / G) * P.s.q_token +
-                    (g.head * G + row % G) * P.s.q_head;
-            copy_rows(q_base + q * kTileBytes, src);
-          }
-          bar_arrive_copied(smem_u32(&sh.q_full));
-        }
-        dst = slot_for(bar);
-        if (!ok) break;
-        copy_rows(dst, v);
-        if (kt < last_tile) {
-          bar_arrive_copied(bar);
-        } else {
-          // A new token that a row does not see must not reach it as 0 * inf:
-          // such values become 0 here and are put back, row by row, at the end.
-          asm volatile("cp.async.wait_all;" ::: "memory");
-          for (int r = 0; r < 32; r += kRowsAtOnce) {
-            const uint32_t a = operand_chunk(dst, kTile, w * 32 + r + sub, chunk);
-            uint32_t x[4];
-            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(a) : "memory");
-            bool bad = false;
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-              constexpr uint32_t e = KvType<T>::kExponent;
-              if ((x[i] & e) == e) x[i] &= 0xFFFF0000u, bad = true;
-              if ((x[i] >> 16 & e) == e) x[i] &= 0xFFFFu, bad = true;
+          const int p = page, o = off;
+          const uint32_t there = __ballot_sync(~0u, lane >= boxes || p >= 0);
+          // (row 32 i + j of the tile lies in box (32 i + j) / rows)
+          if (lane < 4) {
+            uint32_t word = ~0u;
+            if (there != ~0u) {
+              word = 0;
+              for (int j = 0; j < 32; j++) word |= (there >> ((lane * 32 + j) / P.k_boxes.rows) & 1) << j;
             }
-            if (bad) {
-              asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]) : "memory");
-              odd = true;
-            }
+            sh.row_ok[tile_no & 7][lane] = word;
           }
-          odd = __any_sync(~0u, odd);
-          bar_arrive(bar);
+          __syncwarp();
+          tile_boxes<DP>(dst, P.k_boxes, bar, g.head, p, o);
+          if (kt + 1 < boxed) find_box(kt + 1);
+          dst = slot_for(bar);
+          if (!ok) break;
+          tile_boxes<DP>(dst, P.v_boxes, bar, g.head, p, o);
+          if (kt == g.kt0) copier.landed();
         }
-        if (lane == 0) {
-          sh.odd[seg_no & 3][w] = odd;
-          bar_arrive(bar);
+      }
+      // the other tiles, row by row
+      for (; kt < g.kt1 && ok; kt++, tile_no++) {
+        const int j = w * 32 + lane;  // this lane's row: a slot of a page, or a new token
+        const bool last = kt == last_tile, fresh = last && j < g.tok.count;
+        int page = -1, off = 0;
+        if (!last && kt * kTile + j < g.len) page = kv_page(P.c, g.b, kt * kTile + j, off);
+        const uint32_t there = __ballot_sync(~0u, fresh || page >= 0);
+        for (int part = 0; part < 2 && ok; part++) {  // keys, values
+          const T *src = nullptr;
+          if (fresh)
+            src = part ? static_cast<const T *>(P.s.v_new) + (g.tok.first + j) * P.s.v_token + g.head * P.s.v_head
+                       : static_cast<const T *>(P.s.k_new) + (g.tok.first + j) * P.s.k_token + g.head * P.s.k_head;
+          else if (page >= 0)
+            src = part ? static_cast<const T *>(P.c.v) + page * P.c.v_page + g.head * P.c.v_head + off * P.c.v_slot
+                       : static_cast<const T *>(P.c.k) + page * P.c.k_page + g.head * P.c.k_head + off * P.c.k_slot;
+          uint32_t bar;
+          const uint32_t dst = slot_for(bar);
+          if (!ok) break;
+          copier.rows(dst, src);
+          if (part == 0) {
+            if (lane == 0) sh.row_ok[tile_no & 7][w] = there;
+            copier.issued(bar);
+          } else if (!last) {
+            copier.issued(bar);
+          } else {
+            // A new token that a row does not see must not reach it as 0 * inf:
+            // such values become 0 here and are put back, row by row, at the end.
+            copier.issued(0);
+            copier.landed();
+            const bool odd = copier.zero_odd_values(dst);
+            if (lane == 0) sh.odd[seg_no & 3][w] = odd;
+            copier.arrive(bar);
+          }
         }
       }
       seg_no++;
     }
-    asm volatile("cp.async.wait_all;" ::: "memory");
+    copier.landed();
+    if (!ok) copier.give_up();
   } else if (warp >= kIssueWarp) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOthers));
-    if (warp == kIssueWarp && lane == 0) {
-      // ----------------------------------------------------------- products
+    if (warp == kIssueWarp) {
+      // --------------------------------------------------------- products
+      // (the whole warp goes along, one lane issues)
       const uint32_t shape_s = product_shape(kOperandType<T>, 128, kTile, false, P.s.scale < 0.f);
       const uint32_t shape_o = product_shape(kOperandType<T>, 128, DP, true, false);
+      const uint32_t q_rows = smem_operand(q_base, kBlock), slots = smem_operand(slot_base, kBlock);
       int item = 0, seg_no = 0, p_no[2] = {0, 0};
       bool ok = true;
       auto take = [&](int &s) -> uint32_t {  // waits for the next slot's tile
         s = item % kSlots<DP>;
-        ok = ok && bar_wait(smem_u32(&sh.kv_full[s]), (item / kSlots<DP>) & 1, &sh.dead);
-        fence_to_tensor();
+        ok = __all_sync(~0u, bar_wait(smem_u32(&sh.kv_full[s]), (item / kSlots<DP>) & 1, &sh.dead));
         item++;
-        return slot_base + s * kTileBytes;
+        return slots + s * (kTileBytes >> 4);
       };
       auto scores = [&](int q, uint32_t keys) {
-  #pragma unroll
-        for (int d = 0; d < DP / 16; d++) {
-          const uint32_t at = d / 4 * kBlock + d % 4 * 32;
-          product_ss(tmem + q * 128, smem_operand(q_base + q * kTileBytes + at, kBlock), smem_operand(keys + at, kBlock),
-                     shape_s, d > 0);
+        if (elect_one()) {
+          const uint32_t a = q_rows + q * (kTileBytes >> 4);
+#pragma unroll
+          for (int d = 0; d < DP / 16; d++) {
+            const uint32_t at = (d / 4 * kBlock + d % 4 * 32) >> 4;
+            product_ss(tmem + q * 128, a + at, keys + at, shape_s, d > 0);
+          }
+          products_done(smem_u32(&sh.s_full[q]));
+          bar_arrive(smem_u32(&sh.s_full[q]));  // hands on what the copies of the keys wrote besides (row_ok)
         }
-        products_done(smem_u32(&sh.s_full[q]));
-        bar_arrive(smem_u32(&sh.s_full[q]));  // hands on what the copies of the keys wrote besides (row_ok)
+        __syncwarp();
       };
       auto values = [&](int q, uint32_t vals, bool add) {
-        ok = ok && bar_wait(smem_u32(&sh.p_full[q]), p_no[q]++ & 1, &sh.dead);
+        ok = __all_sync(~0u, bar_wait(smem_u32(&sh.p_full[q]), p_no[q]++ & 1, &sh.dead));
         if (!ok) return;
         tmem_after_sync();
-  #pragma unroll
-        for (int k = 0; k < kTile / 16; k++)
-          product_ts(tmem + 256 + q * DP, tmem + q * 128 + k * 8, smem_operand(vals + k * 2048, kBlock), shape_o, add || k > 0);
-        products_done(smem_u32(&sh.pv_done[q]));
-        bar_arrive(smem_u32(&sh.pv_done[q]));  // and those of the values (odd)
+        if (elect_one()) {
+#pragma unroll
+          for (int k = 0; k < kTile / 16; k++)
+            product_ts(tmem + 256 + q * DP, tmem + q * 128 + k * 8, vals + k * (2048 >> 4), shape_o, add || k > 0);
+          products_done(smem_u32(&sh.pv_done[q]));
+          bar_arrive(smem_u32(&sh.pv_done[q]));  // and those of the values (odd)
+        }
+        __syncwarp();
+      };
+      auto release = [&](uint64_t &bar) {
+        if (elect_one()) products_done(smem_u32(&bar));
+        __syncwarp();
       };
       while (at < run.end && ok) {
         Segment g;
@@ -265,24 +282,24 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const AttendPara
         const int n = g.kt1 - g.kt0, tiles = g.rows > 128 ? 2 : 1;
         int ks, vs;
         uint32_t keys = take(ks);
-        ok = ok && bar_wait(smem_u32(&sh.q_full), seg_no & 1, &sh.dead);
-        fence_to_tensor();
+        if (ok) ok = __all_sync(~0u, bar_wait(smem_u32(&sh.q_full), seg_no & 1, &sh.dead));
         if (!ok) break;
         for (int q = 0; q < tiles; q++) scores(q, keys);
-        products_done(smem_u32(&sh.kv_free[ks]));
-        if (n == 1) products_done(smem_u32(&sh.q_free));
+        release(sh.kv_free[ks]);
+        if (n == 1) release(sh.q_free);
         for (int i = 0; i < n && ok; i++) {
           const uint32_t vals = take(vs);
           for (int q = 0; q < tiles && ok; q++) {
             values(q, vals, i > 0);
-            if (q == tiles - 1) products_done(smem_u32(&sh.kv_free[vs]));
+            if (!ok) break;
+            if (q == tiles - 1) release(sh.kv_free[vs]);
             if (i + 1 < n) {
               if (q == 0) keys = take(ks);
               if (!ok) break;
               scores(q, keys);
               if (q == tiles - 1) {
-                products_done(smem_u32(&sh.kv_free[ks]));
-                if (i + 2 == n) products_done(smem_u32(&sh.q_free));
+                release(sh.kv_free[ks]);
+                if (i + 2 == n) release(sh.q_free);
               }
             }
           }
@@ -290,8 +307,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const AttendPara
         seg_no++;
       }
       // nothing may still be at work when tensor memory is freed
-      products_done(smem_u32(&sh.idle));
-      for (int i = 0; i < 1 << 20 && !bar_try(smem_u32(&sh.idle), 0); i++) {
+      release(sh.idle);
+      for (int i = 0; i < 1 << 20 && !__all_sync(~0u, bar_try(smem_u32(&sh.idle), 0)); i++) {
       }
     }
   } else {
@@ -478,7 +495,11 @@ int attend_tc(const AttendParams &p, int grid, void *stream) {
     if (a.numRegs * kThreads < 256 * (kRegsWeights + kRegsOthers)) return UNISON_ERR_CUDA;
   }
   if (!kv_allow_smem(kernel, kTcSmem<DP>, &done)) return UNISON_ERR_CUDA;
-  return kv_launch("kv_attend", dim3(grid), dim3(kThreads), kTcSmem<DP>, stream, 1, attend_tc_kernel<T, DP>, p);
+  AttendTcParams q;
+  static_cast<AttendParams &>(q) = p;
+  kv_boxes(q.k_boxes, p.c, p.c.k, p.c.k_page, p.c.k_head, p.c.k_slot);
+  kv_boxes(q.v_boxes, p.c, p.c.v, p.c.v_page, p.c.v_head, p.c.v_slot);
+  return kv_launch("kv_attend", dim3(grid), dim3(kThreads), kTcSmem<DP>, stream, 1, attend_tc_kernel<T, DP>, q);
 }
 
 template int attend_tc<__nv_bfloat16, 64>(const AttendParams &, int, void *);

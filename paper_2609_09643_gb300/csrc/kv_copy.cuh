@@ -1,0 +1,150 @@
+// Tiles of paged rows on their way into the tensor cores' operands, for the
+// four copying warps of a CTA.
+//
+// Full tiles of caches whose pages divide a tile (or the other way round) go by
+// TMA: one warp sends the boxes, and the hardware reports the bytes to the
+// tile's barrier.  Every other tile (the last one of
+// a session, its new tokens, odd page sizes or strides) and the query rows go
+// by 16-byte copies, which can leave out single rows.  (128 keys of 128
+// elements cost the warps about 2,000 cycles by copies, and next to nothing by TMA.)
+#pragma once
+
+#include <cuda.h>
+
+#include "kv_tc.cuh"
+
+namespace unison {
+
+constexpr int kTileRows = 128;
+
+// The pool of keys or values for TMA: [page][two of slot, head][element].
+struct KvBoxes {
+  CUtensorMap map;
+  int rows;         // of a box, 0: not by TMA
+  bool head_first;  // heads lie closer together than slots
+};
+// On the host; rows = 0 where the pool does not allow it.
+void kv_boxes(KvBoxes &x, const unison_kv_cache &c, const void *pool, int64_t page, int64_t head, int64_t slot);
+
+__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {  // an arrival that announces bytes
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void box_copy(uint32_t dst, const KvBoxes &x, uint32_t bar, int col, int slot, int head,
+                                         int page) {
+  const int c1 = x.head_first ? head : slot, c2 = x.head_first ? slot : head;
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], "
+      "[%6];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(&x.map)), "r"(col), "r"(c1), "r"(c2), "r"(page), "r"(bar)
+      : "memory");
+}
+
+// All boxes of a full tile, by one warp: lane i knows the page that box i lies
+// in, and the slot of that page that it begins with.  The warp's arrival at the
+// tile's barrier announces the bytes.
+template <int DP>
+__device__ __forceinline__ void tile_boxes(uint32_t dst, const KvBoxes &x, uint32_t bar, int head, int page, int off) {
+  constexpr int kHalves = DP / 64;
+  const int lane = threadIdx.x & 31;
+  if (lane == 0) bar_expect(bar, kTileRows * DP * 2);
+  __syncwarp();
+  const int box = lane / kHalves, col = lane % kHalves * 64;
+  const int p = __shfl_sync(~0u, page, box), o = __shfl_sync(~0u, off, box);
+  if (box * x.rows < kTileRows)
+    box_copy(dst + col * (kTileRows * 2) + box * x.rows * 128, x, bar, col, o, head, p);
+  __syncwarp();
+}
+
+// A copying warp.  Each item (a tile, or the query rows) ends with one arrival
+// of the warp at the item's barrier: two items later, when the copies have
+// landed and are fenced.
+template <typename T, int DP>
+struct KvCopier {
+  static constexpr int kChunks = DP / 8, kAtOnce = 32 / kChunks;
+  int w, lane, head_dim;
+  unsigned long long nowhere;    // an address that may be read: copies of nothing want one all the same
+  uint32_t waiting[2] = {0, 0};  // barriers of the copies that are still on their way
+
+  __device__ __forceinline__ KvCopier(int warp, int ln, int dim, const void *any)
+      : w(warp), lane(ln), head_dim(dim), nowhere(reinterpret_cast<unsigned long long>(any)) {}
+
+  // This warp's 32 rows of 128; lane i knows row i's address, null: zeros.
+  __device__ __forceinline__ void rows(uint32_t dst, const T *mine) {
+    const int chunk = lane % kChunks, sub = lane / kChunks;
+    const bool inside = chunk * 8 < head_dim;
+    constexpr int kBatch = 8;
+#pragma unroll
+    for (int r0 = 0; r0 < 32; r0 += kBatch * kAtOnce) {
+      unsigned long long src[kBatch];
+#pragma unroll
+      for (int i = 0; i < kBatch; i++)
+        src[i] = __shfl_sync(~0u, reinterpret_cast<unsigned long long>(mine), r0 + i * kAtOnce + sub);
+#pragma unroll
+      for (int i = 0; i < kBatch; i++) {
+        const bool there = src[i] != 0 && inside;
+        const T *p = reinterpret_cast<const T *>(there ? src[i] + chunk * 16 : nowhere);
+        cp_async16(operand_chunk(dst, kTileRows, w * 32 + r0 + i * kAtOnce + sub, chunk), p, there);
+      }
+    }
+  }
+
+  // The item's copies have all been issued; 0: it needs no arrival of them.
+  __device__ __forceinline__ void issued(uint32_t bar) {
+    cp_commit();
+    if (waiting[0]) {
+      cp_wait<2>();
+      arrive(waiting[0]);
+    }
+    waiting[0] = waiting[1];
+    waiting[1] = bar;
+  }
+  __device__ __forceinline__ void landed() {  // all of them
+    cp_wait<0>();
+    for (int i = 0; i < 2; i++)
+      if (waiting[i]) arrive(waiting[i]);
+    waiting[0] = waiting[1] = 0;
+  }
+  // Waits for what others do with earlier items: none of those may be held back.
+  __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int *dead) {
+    if (__all_sync(~0u, bar_try(bar, parity))) return true;
+    landed();
+    return __all_sync(~0u, bar_wait(bar, parity, dead));
+  }
+  // Infinities and NaN in this warp's rows of a tile become 0; whether there were any.
+  __device__ __forceinline__ bool zero_odd_values(uint32_t tile) {
+    bool odd = false;
+    __syncwarp();
+    for (int i = lane; i < 32 * kChunks; i += 32) {
+      const uint32_t a = operand_chunk(tile, kTileRows, w * 32 + i / kChunks, i % kChunks);
+      uint32_t x[4];
+      asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
+                   : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3])
+                   : "r"(a)
+                   : "memory");
+      bool bad = false;
+#pragma unroll
+      for (int j = 0; j < 4; j++) {
+        constexpr uint32_t e = KvType<T>::kExponent;
+        if ((x[j] & e) == e) x[j] &= 0xFFFF0000u, bad = true;
+        if ((x[j] >> 16 & e) == e) x[j] &= 0xFFFFu, bad = true;
+      }
+      if (bad) {
+        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3])
+                     : "memory");
+        odd = true;
+      }
+    }
+    return __any_sync(~0u, odd);
+  }
+  // After a wait that ran out: boxes on their way may still arrive for a while.
+  __device__ __forceinline__ void give_up() {
+    for (int i = 0; i < 1000; i++) __nanosleep(1000);
+  }
+  __device__ __forceinline__ void arrive(uint32_t bar) {
+    fence_to_tensor();
+    __syncwarp();
+    if (lane == 0) bar_arrive(bar);
+  }
+};
+
+}  // namespace unison

@@ -10,8 +10,8 @@
 //   warp 12         issues the products, 128 query rows at a time, into four
 //                   buffers of tensor memory
 //   warps 0-3, 4-7  turn the scores of a buffer into weights, in turn
+#include "kv_copy.cuh"
 #include "kv_observe.cuh"
-#include "kv_tc.cuh"
 
 namespace unison {
 namespace {
@@ -42,8 +42,12 @@ struct Segment {
   KvRange tok;
 };
 
+struct ObserveTcParams : ObserveParams {
+  KvBoxes k_boxes;
+};
+
 template <typename T, int DP>
-__global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const ObserveParams P) {
+__global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_constant__ ObserveTcParams P) {
   constexpr uint32_t kTileBytes = kTile * DP * 2, kBlock = kTile * 128;
   extern __shared__ unsigned char smem_raw[];
   __shared__ ObserveShared sh;
@@ -56,20 +60,27 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const ObservePa
   float **const marks_at = reinterpret_cast<float **>(lse_base + 2 * P.q_rows);  // where a key's weight goes
   float *const marks_old = reinterpret_cast<float *>(marks_at + kMarks * kTile);  // what is there
 
+  // A tile's share of the run: its keys' way here, or the products and weights
+  // of its chunks of 128 query rows, where those take longer.
+  auto share = [&](int b, int tokens) {
+    const int chunks = (path_count(P, b, tokens) * G + 127) / 128;
+    return max(4, 3 * chunks);
+  };
   KvRun run;
-  if (!kv_find_run(run, sh.run, P.c.n_seqs, gridDim.x, blockIdx.x,
-                   [&](int b) { return (int64_t)observe_key_tiles(P, b, kTile) * H; }))
+  if (!kv_find_run(run, sh.run, P.c.n_seqs, gridDim.x, blockIdx.x, [&](int b) {
+        return (int64_t)observe_key_tiles(P, b, kTile) * H * share(b, kv_tokens(P.t, b, nullptr).count);
+      }))
     return;
   if (tid == 0) {
     for (int i = 0; i < kMostSlots; i++) {
-      bar_init(smem_u32(&sh.k_full[i]), 256);  // copies, and stores, of every copying thread
+      bar_init(smem_u32(&sh.k_full[i]), 4);  // copying warps
       bar_init(smem_u32(&sh.k_free[i]), 1);
     }
     for (int i = 0; i < kBuffers; i++) {
       bar_init(smem_u32(&sh.t_full[i]), 2);
       bar_init(smem_u32(&sh.t_free[i]), 128);
     }
-    bar_init(smem_u32(&sh.q_full), 256);
+    bar_init(smem_u32(&sh.q_full), 4);
     bar_init(smem_u32(&sh.q_free), 1);
     bar_init(smem_u32(&sh.seg_done[0]), 256);
     bar_init(smem_u32(&sh.seg_done[1]), 256);
@@ -87,150 +98,172 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const ObservePa
 
   int b = run.b;
   int64_t at = run.at, seq_begin = run.begin;
-  auto next_segment = [&](Segment &g) {
-    int64_t mine = (int64_t)observe_key_tiles(P, b, kTile) * H;
-    while (at >= seq_begin + mine) {
-      seq_begin += mine;
-      mine = (int64_t)observe_key_tiles(P, ++b, kTile) * H;
+  // The next tiles of one head in this run: those whose share begins in it.
+  auto next_segment = [&](Segment &g) -> bool {
+    while (at < run.end) {
+      g.tok = kv_tokens(P.t, b, nullptr);
+      g.tiles = observe_key_tiles(P, b, kTile);
+      const int64_t each = share(b, g.tok.count), all = (int64_t)g.tiles * H;
+      const int64_t tile = (at - seq_begin + each - 1) / each;
+      const int64_t end = min((run.end - seq_begin + each - 1) / each, all);
+      if (tile < end) {
+        g.b = b;
+        g.len = kv_length(P.c, b);
+        g.rows = path_count(P, b, g.tok.count) * G;
+        g.head = (int)(tile / g.tiles);
+        g.kt0 = (int)(tile % g.tiles);
+        g.kt1 = (int)min((int64_t)g.tiles, g.kt0 + end - tile);
+        at = seq_begin + (tile + g.kt1 - g.kt0) * each;
+        return true;
+      }
+      seq_begin += all * each;
+      at = max(at, seq_begin);
+      b++;
     }
-    g.b = b;
-    g.tok = kv_tokens(P.t, b, nullptr);
-    g.len = kv_length(P.c, b);
-    g.rows = path_count(P, b, g.tok.count) * G;
-    g.tiles = observe_key_tiles(P, b, kTile);
-    g.head = (int)((at - seq_begin) / g.tiles);
-    const int64_t seg_begin = seq_begin + (int64_t)g.head * g.tiles;
-    g.kt0 = (int)(at - seg_begin);
-    g.kt1 = (int)min((int64_t)g.tiles, run.end - seg_begin);
-    at = seg_begin + g.kt1;
+    return false;
   };
 
   if (warp >= kCopyWarp && warp < kIssueWarp) {
     // ------------------------------------------------------------- copies
-    const int w = warp - kCopyWarp, thread = tid - kCopyWarp * 32;
-    constexpr int kChunks = DP / 8, kRowsAtOnce = 32 / kChunks;
-    const int chunk = lane % kChunks, sub = lane / kChunks;
-    const T *dummy = static_cast<const T *>(P.s.q);
+    const int w = warp - kCopyWarp;
+    KvCopier<T, DP> copier(w, lane, D, P.s.q);
     int item = 0, seg_no = 0, tile_no = 0;
     bool ok = true;
-    // Copies this warp's 32 rows of 128; lane i knows row i's address.
-    auto copy_rows = [&](uint32_t dst, const T *mine) {
-#pragma unroll 8
-      for (int r = 0; r < 32; r += kRowsAtOnce) {
-        const T *src = reinterpret_cast<const T *>(__shfl_sync(~0u, reinterpret_cast<unsigned long long>(mine), r + sub));
-        const bool there = src != nullptr && chunk * 8 < D;
-        cp_async16(operand_chunk(dst, kTile, w * 32 + r + sub, chunk), there ? src + chunk * 8 : dummy, there);
-      }
-    };
-    while (at < run.end && ok) {
-      Segment g;
-      next_segment(g);
-      auto find_page = [&](int kt, int &off) -> int {
-        const int slot = kt * kTile + w * 32 + lane;
-        off = 0;
-        return kt < g.tiles - 1 && slot < g.len ? kv_page(P.c, g.b, slot, off) : -1;
-      };
-      int off;
-      int page = find_page(g.kt0, off);
-      for (int kt = g.kt0; kt < g.kt1; kt++) {
-        const T *k = nullptr;
-        float *m = nullptr;
-        if (kt == g.tiles - 1) {
-          const int j = w * 32 + lane;
-          if (j < g.tok.count && P.s.mass_new) {
-            k = static_cast<const T *>(P.s.k_new) + (g.tok.first + j) * P.s.k_token + g.head * P.s.k_head;
-            m = P.s.mass_new + (int64_t)(g.tok.first + j) * H + g.head;
-          }
-        } else if (page >= 0) {
-          k = static_cast<const T *>(P.c.k) + page * P.c.k_page + g.head * P.c.k_head + off * P.c.k_slot;
-          m = P.c.mass + page * P.c.m_page + g.head * P.c.m_head + off * P.c.m_slot;
+    Segment g;
+    while (ok && next_segment(g)) {
+      // The segment's rows: when the last one's products have read theirs, and
+      // nobody reads the statistics of the one before any more.
+      if (seg_no > 0) ok = copier.wait(smem_u32(&sh.q_free), (seg_no - 1) & 1, &sh.dead);
+      if (ok && seg_no > 1)
+        ok = copier.wait(smem_u32(&sh.seg_done[seg_no & 1]), ((seg_no >> 1) - 1) & 1, &sh.dead);
+      if (!ok) break;
+      float *lse = lse_base + (seg_no & 1) * P.q_rows;
+      const int j = w * 32 + lane;  // this lane's row of a tile
+      bool plain = true;
+      for (int r0 = 0; r0 < g.rows; r0 += 128) {
+        const int r = r0 + j;
+        const int node = r < g.rows ? observe_node(P, g.b, g.tok.count, r / G) : -1;
+        const T *src = nullptr;
+        float l = -INFINITY;
+        if (node >= 0) {
+          src = static_cast<const T *>(P.s.q) + (g.tok.first + node) * P.s.q_token + (g.head * G + r % G) * P.s.q_head;
+          l = P.s.lse[(int64_t)(g.tok.first + node) * P.s.n_q_heads + g.head * G + r % G] * -1.4426950408889634f;
+          if (l == INFINITY) l = -INFINITY;
         }
-        if (kt + 1 < g.kt1) page = find_page(kt + 1, off);
+        if (r < g.rows && l == -INFINITY) plain = false;
+        lse[r] = l;
+        copier.rows(q_base + r0 / 128 * kTileBytes, src);
+      }
+      if (j < kNodes) {
+        const int node = j * G < g.rows ? observe_node(P, g.b, g.tok.count, j) : -1;
+        sh.mask[seg_no & 1][j] = node < 0 ? 0 : P.t.mask ? P.t.mask[g.tok.first + node] : ~0ull >> (63 - node);
+      }
+      plain = __all_sync(~0u, plain);
+      if (lane == 0) sh.plain[seg_no & 1][w] = plain;
+      copier.issued(smem_u32(&sh.q_full));
+
+      // a tile's pages are looked up two tiles ahead, the weights there one ahead
+      auto find_page = [&](int kt, int &off) -> int {
+        off = 0;
+        return kt < g.tiles - 1 && kt * kTile + j < g.len ? kv_page(P.c, g.b, kt * kTile + j, off) : -1;
+      };
+      auto account = [&](int page, int off) -> float * {
+        return page < 0 ? nullptr : P.c.mass + page * P.c.m_page + g.head * P.c.m_head + off * P.c.m_slot;
+      };
+      int next_off = 0, next_page = find_page(g.kt0, next_off), later_off = 0, later_page = -1;
+      if (g.kt0 + 1 < g.kt1) later_page = find_page(g.kt0 + 1, later_off);
+      float *next_m = account(next_page, next_off);
+      float next_old = next_m ? *next_m : 0.f;
+      const int boxed = P.k_boxes.rows ? g.len / kTile : 0;  // full tiles go by boxes
+      for (int kt = g.kt0; kt < g.kt1; kt++) {
+        const int page = next_page, off = next_off;
+        float *m = next_m;
+        const float old = next_old;
+        next_page = later_page, next_off = later_off;
+        next_m = kt + 1 < g.kt1 ? account(next_page, next_off) : nullptr;
+        next_old = next_m ? *next_m : 0.f;
+        if (kt + 2 < g.kt1) later_page = find_page(kt + 2, later_off);
         const int s = item % P.slots, n = item / P.slots;
-        if (n > 0) ok = __all_sync(~0u, bar_wait(smem_u32(&sh.k_free[s]), (n - 1) & 1, &sh.dead));
+        if (n > 0) ok = copier.wait(smem_u32(&sh.k_free[s]), (n - 1) & 1, &sh.dead);
         if (!ok) break;
         item++;
-        copy_rows(slot_base + s * kTileBytes, k);
-        const int mark = tile_no++ % kMarks * kTile + w * 32 + lane;
-        if (m && kt < g.tiles - 1)
-          asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(marks_old + mark)), "l"(m) : "memory");
-        bar_arrive_copied(smem_u32(&sh.k_full[s]));
+        const uint32_t dst = slot_base + s * kTileBytes, bar = smem_u32(&sh.k_full[s]);
+        const bool fresh = kt == g.tiles - 1 && j < g.tok.count && P.s.mass_new;
+        if (fresh) m = P.s.mass_new + (int64_t)(g.tok.first + j) * H + g.head;
+        const int mark = tile_no++ % kMarks * kTile + j;
         marks_at[mark] = m;
-        bar_arrive(smem_u32(&sh.k_full[s]));
-        if (kt == g.kt0) {
-          // The segment's rows: when the last one's products have read theirs,
-          // and nobody reads the statistics of the one before any more.
-          if (seg_no > 0) ok = __all_sync(~0u, bar_wait(smem_u32(&sh.q_free), (seg_no - 1) & 1, &sh.dead));
-          if (ok && seg_no > 1) ok = __all_sync(~0u, bar_wait(smem_u32(&sh.seg_done[seg_no & 1]), ((seg_no >> 1) - 1) & 1, &sh.dead));
-          if (!ok) break;
-          float *lse = lse_base + (seg_no & 1) * P.q_rows;
-          bool plain = true;
-          for (int r0 = 0; r0 < g.rows; r0 += 128) {
-            const int r = r0 + w * 32 + lane;
-            const int node = r < g.rows ? observe_node(P, g.b, g.tok.count, r / G) : -1;
-            const T *src = nullptr;
-            float l = -INFINITY;
-            if (node >= 0) {
-              src = static_cast<const T *>(P.s.q) + (g.tok.first + node) * P.s.q_token + (g.head * G + r % G) * P.s.q_head;
-              l = P.s.lse[(int64_t)(g.tok.first + node) * P.s.n_q_heads + g.head * G + r % G] * -1.4426950408889634f;
-              if (l == INFINITY) l = -INFINITY;
-            }
-            if (r < g.rows && l == -INFINITY) plain = false;
-            lse[r] = l;
-            copy_rows(q_base + r0 / 128 * kTileBytes, src);
+        marks_old[mark] = old;
+        __syncwarp();
+        if (kt < boxed) {
+          if (w == 0) {
+            // (found before, by the lane of the box's first row: in the nearest cache)
+            int p = page, o = off;
+            if (P.k_boxes.rows * lane < kTile) p = kv_page(P.c, g.b, kt * kTile + P.k_boxes.rows * lane, o);
+            tile_boxes<DP>(dst, P.k_boxes, bar, g.head, p, o);
+          } else if (lane == 0) {
+            bar_arrive(bar);
           }
-          if (thread < kNodes) {
-            const int node = thread * G < g.rows ? observe_node(P, g.b, g.tok.count, thread) : -1;
-            sh.mask[seg_no & 1][thread] =
-                node < 0 ? 0 : P.t.mask ? P.t.mask[g.tok.first + node] : ~0ull >> (63 - node);
-          }
-          plain = __all_sync(~0u, plain);
-          if (lane == 0) sh.plain[seg_no & 1][w] = plain;
-          bar_arrive_copied(smem_u32(&sh.q_full));
-          bar_arrive(smem_u32(&sh.q_full));
+          if (kt == g.kt0) copier.landed();
+        } else {
+          const T *src = nullptr;
+          if (fresh)
+            src = static_cast<const T *>(P.s.k_new) + (g.tok.first + j) * P.s.k_token + g.head * P.s.k_head;
+          else if (page >= 0)
+            src = static_cast<const T *>(P.c.k) + page * P.c.k_page + g.head * P.c.k_head + off * P.c.k_slot;
+          copier.rows(dst, src);
+          copier.issued(bar);
         }
       }
       seg_no++;
     }
-    asm volatile("cp.async.wait_all;" ::: "memory");
-  } else if (warp == kIssueWarp && lane == 0) {
+    copier.landed();
+    if (!ok) copier.give_up();
+  } else if (warp == kIssueWarp) {
     // ----------------------------------------------------------- products
+    // (the whole warp goes along, one lane issues)
+    const uint32_t q_rows = smem_operand(q_base, kBlock), slots = smem_operand(slot_base, kBlock);
     int item = 0, seg_no = 0, job = 0;
     bool ok = true;
-    while (at < run.end && ok) {
-      Segment g;
-      next_segment(g);
+    auto release = [&](uint64_t &bar) {
+      if (elect_one()) products_done(smem_u32(&bar));
+      __syncwarp();
+    };
+    Segment g;
+    while (ok && next_segment(g)) {
       for (int kt = g.kt0; kt < g.kt1 && ok; kt++) {
         const int s = item % P.slots;
-        ok = bar_wait(smem_u32(&sh.k_full[s]), (item / P.slots) & 1, &sh.dead);
-        if (ok && kt == g.kt0) ok = bar_wait(smem_u32(&sh.q_full), seg_no & 1, &sh.dead);
-        fence_to_tensor();
+        ok = __all_sync(~0u, bar_wait(smem_u32(&sh.k_full[s]), (item / P.slots) & 1, &sh.dead));
+        if (ok && kt == g.kt0) ok = __all_sync(~0u, bar_wait(smem_u32(&sh.q_full), seg_no & 1, &sh.dead));
         item++;
-        const uint32_t keys = slot_base + s * kTileBytes;
+        const uint32_t keys = slots + s * (kTileBytes >> 4);
         for (int r0 = 0; (r0 == 0 || r0 < g.rows) && ok; r0 += 128, job++) {
           const int buf = job % kBuffers;
-          if (job >= kBuffers) ok = bar_wait(smem_u32(&sh.t_free[buf]), (job / kBuffers - 1) & 1, &sh.dead);
+          if (job >= kBuffers)
+            ok = __all_sync(~0u, bar_wait(smem_u32(&sh.t_free[buf]), (job / kBuffers - 1) & 1, &sh.dead));
           if (!ok) break;
           tmem_after_sync();
           const int columns = (max(min(g.rows - r0, 128), 1) + 15) & ~15;
           const uint32_t shape = product_shape(kOperandType<T>, kTile, columns, false, false);
+          if (elect_one()) {
+            const uint32_t rows = q_rows + r0 / 128 * (kTileBytes >> 4);
 #pragma unroll
-          for (int d = 0; d < DP / 16; d++) {
-            const uint32_t o = d / 4 * kBlock + d % 4 * 32;
-            product_ss(tmem + buf * 128, smem_operand(keys + o, kBlock),
-                       smem_operand(q_base + r0 / 128 * kTileBytes + o, kBlock), shape, d > 0);
+            for (int d = 0; d < DP / 16; d++) {
+              const uint32_t o = (d / 4 * kBlock + d % 4 * 32) >> 4;
+              product_ss(tmem + buf * 128, keys + o, rows + o, shape, d > 0);
+            }
+            products_done(smem_u32(&sh.t_full[buf]));
+            bar_arrive(smem_u32(&sh.t_full[buf]));  // hands on what the copies wrote besides
           }
-          products_done(smem_u32(&sh.t_full[buf]));
-          bar_arrive(smem_u32(&sh.t_full[buf]));  // hands on what the copies wrote besides
+          __syncwarp();
         }
-        products_done(smem_u32(&sh.k_free[s]));
+        release(sh.k_free[s]);
       }
-      products_done(smem_u32(&sh.q_free));
+      release(sh.q_free);
       seg_no++;
     }
     // nothing may still be at work when tensor memory is freed
-    products_done(smem_u32(&sh.idle));
-    for (int i = 0; i < 1 << 20 && !bar_try(smem_u32(&sh.idle), 0); i++) {
+    release(sh.idle);
+    for (int i = 0; i < 1 << 20 && !__all_sync(~0u, bar_try(smem_u32(&sh.idle), 0)); i++) {
     }
   } else if (warp < kCopyWarp) {
     // ------------------------------------------------------------ weights
@@ -239,9 +272,8 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const ObservePa
     const float c = P.s.scale * 1.4426950408889634f;
     int job = 0, seg_no = 0, tile_no = 0, shared_tiles = 0;
     bool ok = true;
-    while (at < run.end && ok) {
-      Segment g;
-      next_segment(g);
+    Segment g;
+    while (ok && next_segment(g)) {
       const float *lse = lse_base + (seg_no & 1) * P.q_rows;
       const uint64_t *mask = sh.mask[seg_no & 1];
       const int chunks = max((g.rows + 127) / 128, 1);
@@ -325,7 +357,7 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const ObservePa
         if (writes) {
           const int mark = tile_no % kMarks * kTile + key;
           float *to = marks_at[mark];
-          if (to) *to = last ? all : marks_old[mark] + all;
+          if (to) *to = marks_old[mark] + all;
         }
       }
       if (!ok && key == 0 && P.c.status) P.c.status[g.b] = UNISON_ERR_TIMEOUT;
@@ -355,8 +387,11 @@ int observe_tc(ObserveParams p, int max_rows, void *stream) {
   const int bytes = fixed - (int)sizeof(ObserveShared) + p.slots * kTileBytes;
   if (!kv_allow_smem(reinterpret_cast<const void *>(observe_tc_kernel<T, DP>), kMost - (int)sizeof(ObserveShared), &done))
     return UNISON_ERR_CUDA;
+  ObserveTcParams q;
+  static_cast<ObserveParams &>(q) = p;
+  kv_boxes(q.k_boxes, p.c, p.c.k, p.c.k_page, p.c.k_head, p.c.k_slot);
   return kv_launch("kv_observe", dim3(kv_sm_count()), dim3(kThreads), max(bytes, 120 << 10), stream, 1,
-                   observe_tc_kernel<T, DP>, p);
+                   observe_tc_kernel<T, DP>, q);
 }
 
 template int observe_tc<__nv_bfloat16, 64>(ObserveParams, int, void *);

@@ -14,11 +14,6 @@ __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
 __device__ __forceinline__ void bar_arrive(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-// An arrival of this thread as soon as its copies so far have landed.  It does
-// not order the thread's own stores: those need an arrival of their own.
-__device__ __forceinline__ void bar_arrive_copied(uint32_t bar) {
-  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
-}
 __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
   uint32_t ok;
   asm volatile(
@@ -31,7 +26,7 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
 // Waits until the phase of that parity is complete.  Gives up after about a
 // second, or when another thread of the CTA has: false, and *dead is set.
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *dead) {
-  for (int i = 0; i < 1 << 20; i++) {
+  for (int i = 0; i < 1 << 18; i++) {
     if (bar_try(bar, parity)) return true;
     if (*dead) return false;
   }
@@ -112,9 +107,10 @@ __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t *r) {
 // stride offset, version 1, swizzle mode 2.  The same one serves both majors:
 // rows along the sum (values: MN-major) or along the other axis (K-major, where
 // the leading offset is not used).
-__device__ __forceinline__ uint64_t smem_operand(uint32_t addr, uint32_t block) {
-  return (uint64_t)((addr & 0x3FFFF) >> 4) | (uint64_t)(block >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 |
-         2ull << 61;
+// (The upper word is the same for all of them.)
+constexpr uint32_t kOperandHigh = 1024 >> 4 | 1u << 14 | 2u << 29;
+__device__ __forceinline__ uint32_t smem_operand(uint32_t addr, uint32_t block) {
+  return (addr & 0x3FFFF) >> 4 | block >> 4 << 16;
 }
 // Instruction descriptor: 16-bit operands (type 0: fp16, 1: bf16), 32-bit sums,
 // m rows, n columns; the second operand K-major or MN-major; the first negated.
@@ -127,20 +123,26 @@ constexpr int kOperandType = 1;
 template <>
 constexpr int kOperandType<__half> = 0;
 
+// One lane of a converged warp.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t one;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xFFFFFFFF;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(one));
+  return one != 0;
+}
 // d (+)= a b, both in shared memory; 16 elements of the sum.  By one thread.
-__device__ __forceinline__ void product_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t shape, bool add) {
+__device__ __forceinline__ void product_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t shape, bool add) {
   asm volatile(
-      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-      " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
-      "l"(a), "l"(b), "r"(shape), "r"((uint32_t)add)
+      "{\n .reg .pred p;\n .reg .b64 a, b;\n setp.ne.b32 p, %4, 0;\n mov.b64 a, {%1, %5};\n mov.b64 b, {%2, %5};\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n}\n" ::"r"(d),
+      "r"(a), "r"(b), "r"(shape), "r"((uint32_t)add), "r"(kOperandHigh)
       : "memory");
 }
 // The same with a in tensor memory.
-__device__ __forceinline__ void product_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t shape, bool add) {
+__device__ __forceinline__ void product_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t shape, bool add) {
   asm volatile(
-      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d),
-      "r"(a), "l"(b), "r"(shape), "r"((uint32_t)add)
+      "{\n .reg .pred p;\n .reg .b64 b;\n setp.ne.b32 p, %4, 0;\n mov.b64 b, {%2, %5};\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n}\n" ::"r"(d),
+      "r"(a), "r"(b), "r"(shape), "r"((uint32_t)add), "r"(kOperandHigh)
       : "memory");
 }
 // The barrier gets one arrival when all products of this thread so far are done.

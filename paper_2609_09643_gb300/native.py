@@ -16,7 +16,8 @@ CSRC = os.path.join(PKG, "csrc")
 OUT = os.path.join(PKG, "_build")
 LIB = os.path.join(OUT, "libunison.so")
 SOURCES = ["trace.cu", "replay.cu", "rank.cu", "profile.cu", "selftest.cu",
-           "kv_attend.cu", "kv_attend_tc.cu", "kv_observe.cu", "kv_observe_tc.cu", "kv_cache.cu", "kv_verify.cu"]
+           "kv_attend.cu", "kv_attend_tc.cu", "kv_observe.cu", "kv_observe_tc.cu", "kv_cache.cu",
+           "kv_copy.cu", "kv_verify.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-O2"]
 
