@@ -18,12 +18,9 @@
 namespace unison {
 namespace {
 
-constexpr int kThreads = 512;
+constexpr int kThreads = 416;
 constexpr int kTile = 128;
 constexpr int kCopyWarp = 8, kIssueWarp = 12;
-// Registers of a thread that computes weights, and of the others: 256 threads
-// each, together what the launch has (512 x 128).
-constexpr int kRegsWeights = 184, kRegsOthers = 72;
 constexpr float kSlack = 8.f;
 
 template <int DP>
@@ -117,7 +114,6 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
   };
 
   if (warp >= kCopyWarp && warp < kIssueWarp) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOthers));
     // ------------------------------------------------------------- copies
     const int w = warp - kCopyWarp;
     KvCopier<T, DP> copier(w, lane, D, P.s.q);
@@ -230,7 +226,6 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     copier.landed();
     if (!ok) copier.give_up();
   } else if (warp >= kIssueWarp) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOthers));
     if (warp == kIssueWarp) {
       // --------------------------------------------------------- products
       // (the whole warp goes along, one lane issues)
@@ -312,7 +307,6 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
       }
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsWeights));
     // ------------------------------------------------------------ weights
     const int q = warp >> 2, r = tid & 127;
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // this warp's quarter of the 128 lanes
@@ -338,11 +332,6 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
         ok = __all_sync(~0u, bar_wait(smem_u32(&sh.s_full[q]), s_no & 1, &sh.dead));
         if (!ok) break;
         tmem_after_sync();
-        uint32_t x[128];
-        tmem_ld32(x, s_addr);
-        tmem_ld32(x + 32, s_addr + 32);
-        tmem_ld32(x + 64, s_addr + 64);
-        tmem_ld32(x + 96, s_addr + 96);
         uint32_t see[4];
 #pragma unroll
         for (int i = 0; i < 4; i++) see[i] = sh.row_ok[tile_no & 7][i];
@@ -350,56 +339,103 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
           see[0] &= (uint32_t)mask;
           see[1] &= (uint32_t)(mask >> 32);
         }
-        tmem_wait_ld();
-        if (!__all_sync(~0u, (see[0] & see[1] & see[2] & see[3]) == ~0u)) {
+        const bool hidden = !__all_sync(~0u, (see[0] & see[1] & see[2] & see[3]) == ~0u);
+        const uint64_t cc = pair(c, c);
+        uint32_t x[2][32];
+        // One pass where the last reference still serves: the weights wait in
+        // registers until the tile's maximum is known.  (Two passes cost 700
+        // cycles of a tile's 2,400 here.)
+        bool done = false;
+        if (!hidden && kt > g.kt0) {
+          const float base = m == -INFINITY ? 0.f : m;
+          const uint64_t bb = pair(-base, -base);
+          uint64_t sum[2] = {0, 0};
+          float t[2] = {-INFINITY, -INFINITY};
+          uint32_t p[64];
+          tmem_ld32(x[0], s_addr);
 #pragma unroll
-          for (int i = 0; i < 128; i++)
-            if (!(see[i / 32] >> (i % 32) & 1)) x[i] = 0xFF800000u;  // -inf
-        }
-        float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+          for (int i = 0; i < 4; i++) {
+            uint32_t(&v)[32] = x[i & 1];
+            tmem_wait_ld(v);
+            if (i < 3) tmem_ld32(x[~i & 1], s_addr + i * 32 + 32);
 #pragma unroll
-        for (int i = 0; i < 128; i++) t[i & 3] = fmaxf(t[i & 3], __uint_as_float(x[i]));
-        const float top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
-        const float scaled = top * c;
-        if (kt == g.kt0) {
-          m = scaled;
-        } else if (__any_sync(~0u, scaled > m + kSlack)) {
-          const float to = scaled > m + kSlack ? scaled : m;
-          const float f = m == to ? 1.f : exp2_fast(m - to);
-          ok = __all_sync(~0u, bar_wait(smem_u32(&sh.pv_done[q]), (s_no - 1) & 1, &sh.dead));
-          if (!ok) break;
-          tmem_after_sync();
-          for (int d = 0; d < DP; d += 32) {
-            uint32_t o[32];
-            tmem_ld32(o, o_addr + d);
-            tmem_wait_ld();
-#pragma unroll
-            for (int i = 0; i < 32; i++) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-            tmem_st32(o_addr + d, o);
+            for (int j = 0; j < 32; j += 2) {
+              float a = __uint_as_float(v[j]), b = __uint_as_float(v[j + 1]);
+              t[j >> 1 & 1] = fmaxf(fmaxf(t[j >> 1 & 1], a), b);
+              unpair(fma_pair(pair(a, b), cc, bb), a, b);
+              a = exp2_fast(a);
+              b = exp2_fast(b);
+              sum[j >> 1 & 1] = add_pair(sum[j >> 1 & 1], pair(a, b));
+              p[i * 16 + j / 2] = KvType<T>::pack(a, b);
+            }
           }
-          l *= f;
+          done = !__any_sync(~0u, fmaxf(t[0], t[1]) * c > m + kSlack);
+          if (done) {
+            tmem_st32(s_addr, p);
+            tmem_st32(s_addr + 32, p + 32);
+            float more, less;
+            unpair(add_pair(sum[0], sum[1]), more, less);
+            l += more + less;
+          }
+        }
+        if (!done) {
+          // Two passes, 32 scores at a time: the maximum, then the weights.
+          auto hide = [&](uint32_t(&v)[32], uint32_t word) {
+#pragma unroll
+            for (int i = 0; i < 32; i++)
+              if (!(word >> i & 1)) v[i] = 0xFF800000u;  // -inf
+          };
+          auto word_of = [&](int i) { return i == 0 ? see[0] : i == 1 ? see[1] : i == 2 ? see[2] : see[3]; };
+          float t = -INFINITY;
+#pragma unroll 1
+          for (int i = 0; i < 4; i++) {
+            tmem_ld32(x[0], s_addr + i * 32);
+            tmem_wait_ld(x[0]);
+            if (hidden) hide(x[0], word_of(i));
+#pragma unroll
+            for (int j = 0; j < 32; j++) t = fmaxf(t, __uint_as_float(x[0][j]));
+          }
+          const float to = kt == g.kt0 || t * c > m + kSlack ? t * c : m;
+          if (kt > g.kt0 && __any_sync(~0u, to != m)) {
+            const float f = m == to ? 1.f : exp2_fast(m - to);
+            ok = __all_sync(~0u, bar_wait(smem_u32(&sh.pv_done[q]), (s_no - 1) & 1, &sh.dead));
+            if (!ok) break;
+            tmem_after_sync();
+#pragma unroll 1
+            for (int d = 0; d < DP; d += 32) {
+              tmem_ld32(x[0], o_addr + d);
+              tmem_wait_ld(x[0]);
+#pragma unroll
+              for (int i = 0; i < 32; i++) x[0][i] = __float_as_uint(__uint_as_float(x[0][i]) * f);
+              tmem_st32(o_addr + d, x[0]);
+            }
+            l *= f;
+          }
           m = to;
-        }
-        const float base = m == -INFINITY ? 0.f : m;
-        uint64_t sum[2] = {0, 0};
-        const uint64_t cc = pair(c, c), bb = pair(-base, -base);
+          const float base = m == -INFINITY ? 0.f : m;
+          const uint64_t bb = pair(-base, -base);
+          uint64_t sum = 0;
+#pragma unroll 1
+          for (int i = 0; i < 4; i++) {
+            tmem_ld32(x[0], s_addr + i * 32);
+            tmem_wait_ld(x[0]);
+            if (hidden) hide(x[0], word_of(i));
+            uint32_t p[16];
 #pragma unroll
-        for (int i = 0; i < 128; i += 32) {
-          uint32_t p[16];
-#pragma unroll
-          for (int j = 0; j < 32; j += 2) {
-            float a, b;
-            unpair(fma_pair(pair(__uint_as_float(x[i + j]), __uint_as_float(x[i + j + 1])), cc, bb), a, b);
-            a = exp2_fast(a);
-            b = exp2_fast(b);
-            sum[j >> 1 & 1] = add_pair(sum[j >> 1 & 1], pair(a, b));
-            p[j / 2] = KvType<T>::pack(a, b);
+            for (int j = 0; j < 32; j += 2) {
+              float a, b;
+              unpair(fma_pair(pair(__uint_as_float(x[0][j]), __uint_as_float(x[0][j + 1])), cc, bb), a, b);
+              a = exp2_fast(a);
+              b = exp2_fast(b);
+              sum = add_pair(sum, pair(a, b));
+              p[j / 2] = KvType<T>::pack(a, b);
+            }
+            tmem_st16(s_addr + i * 16, p);  // over scores that have been read
           }
-          tmem_st16(s_addr + i / 2, p);
+          float more, less;
+          unpair(sum, more, less);
+          l += more + less;
         }
-        float more, less;
-        unpair(add_pair(sum[0], sum[1]), more, less);
-        l += more + less;
         tmem_wait_st();
         tmem_before_sync();
         bar_arrive(smem_u32(&sh.p_full[q]));
@@ -420,11 +456,11 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
       float *part = P.partial + ((int64_t)blockIdx.x * 2 + (g.kt0 == 0 ? 1 : 0)) * (kTcRows * (DP + 2));
       const int pr = q * 128 + r;
       T *dst = static_cast<T *>(P.s.out) + (g.tok.first + node) * P.s.out_token + (g.head * G + row % G) * P.s.out_head;
-#pragma unroll
+#pragma unroll 1
       for (int d0 = 0; d0 < DP; d0 += 32) {
         uint32_t o[32];
         tmem_ld32(o, o_addr + d0);
-        tmem_wait_ld();
+        tmem_wait_ld(o);
         if (used && odd) {
           const uint64_t see = mask & (~0ull >> (64 - g.tok.count));
           for (int j = 0; j < g.tok.count; j++) {
@@ -485,15 +521,6 @@ template <typename T, int DP>
 int attend_tc(const AttendParams &p, int grid, void *stream) {
   static uint64_t done = 0;
   const void *kernel = reinterpret_cast<const void *>(attend_tc_kernel<T, DP>);
-  if (!__atomic_load_n(&done, __ATOMIC_RELAXED)) {
-    // the registers that the roles share out must be there: see kRegsWeights
-    cudaFuncAttributes a;
-    if (cudaFuncGetAttributes(&a, kernel) != cudaSuccess) {
-      cudaGetLastError();
-      return UNISON_ERR_CUDA;
-    }
-    if (a.numRegs * kThreads < 256 * (kRegsWeights + kRegsOthers)) return UNISON_ERR_CUDA;
-  }
   if (!kv_allow_smem(kernel, kTcSmem<DP>, &done)) return UNISON_ERR_CUDA;
   AttendTcParams q;
   static_cast<AttendParams &>(q) = p;

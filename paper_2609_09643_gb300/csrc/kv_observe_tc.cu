@@ -294,44 +294,57 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
           const bool checked = last || !(plain[0] && plain[1] && plain[2] && plain[3]);
           const uint32_t from = tmem + buf * 128 + lanes;
           const float *l = lse + i * 128;
-          uint32_t x[2][32];
-          tmem_ld32(x[0], from);
+          int r0 = 0;
+          if (!checked && n >= 32) {
+            // 32 scores at a time, the next ones on their way meanwhile
+            const int groups = n / 32;
+            uint32_t x[2][32];
+            const uint64_t cc = pair(c, c);
+            tmem_ld32(x[0], from);
+#pragma unroll 1
+            for (int k = 0; k < groups; k += 2) {
 #pragma unroll
-          for (int r0 = 0; r0 < 128; r0 += 32) {
-            if (r0 < n) {
-              uint32_t(&v)[32] = x[r0 / 32 & 1];
-              tmem_wait_ld();
-              if (r0 + 32 < n) tmem_ld32(x[~(r0 / 32) & 1], from + r0 + 32);
-              if (!checked && r0 + 32 <= n) {
-                const uint64_t cc = pair(c, c);
+              for (int h = 0; h < 2; h++) {
+                if (k + h < groups) {
+                  uint32_t(&v)[32] = x[h];
+                  tmem_wait_ld(v);
+                  tmem_ld32(x[h ^ 1], from + (r0 + 32 & 127));  // (the last one is not used)
 #pragma unroll
-                for (int j = 0; j < 32; j += 4) {
-                  const ulonglong2 y = *reinterpret_cast<const ulonglong2 *>(l + r0 + j);
-                  float e[4];
-                  unpair(fma_pair(pair(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), cc, y.x), e[0], e[1]);
-                  unpair(fma_pair(pair(__uint_as_float(v[j + 2]), __uint_as_float(v[j + 3])), cc, y.y), e[2], e[3]);
-                  sum[0] = add_pair(sum[0], pair(exp2_fast(e[0]), exp2_fast(e[1])));
-                  sum[1] = add_pair(sum[1], pair(exp2_fast(e[2]), exp2_fast(e[3])));
-                }
-              } else {
-                int node = (i * 128 + r0) / G, head = (i * 128 + r0) % G;
-#pragma unroll
-                for (int j = 0; j < 32; j += 2) {
-                  float e[2];
-#pragma unroll
-                  for (int h = 0; h < 2; h++) {
-                    const float y = l[r0 + j + h];
-                    const bool see = r0 + j + h < n && y != -INFINITY &&
-                                     (!last || (node < kNodes && key < 64 && mask[node] >> key & 1));
-                    e[h] = see ? exp2_fast(fmaf(__uint_as_float(v[j + h]), c, y)) : 0.f;
-                    if (++head == G) head = 0, node++;
+                  for (int j = 0; j < 32; j += 4) {
+                    const ulonglong2 y = *reinterpret_cast<const ulonglong2 *>(l + r0 + j);
+                    float e[4];
+                    unpair(fma_pair(pair(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), cc, y.x), e[0], e[1]);
+                    unpair(fma_pair(pair(__uint_as_float(v[j + 2]), __uint_as_float(v[j + 3])), cc, y.y), e[2], e[3]);
+                    sum[0] = add_pair(sum[0], pair(exp2_fast(e[0]), exp2_fast(e[1])));
+                    sum[1] = add_pair(sum[1], pair(exp2_fast(e[2]), exp2_fast(e[3])));
                   }
-                  sum[j >> 1 & 1] = add_pair(sum[j >> 1 & 1], pair(e[0], e[1]));
-                  if (r0 + j + 2 >= n) break;
+                  r0 += 32;
                 }
               }
-              __syncwarp();
             }
+            tmem_wait_ld();
+          }
+          // the others 16 at a time, each with the question whether it counts
+          int node = (i * 128 + r0) / G, head = (i * 128 + r0) % G;
+#pragma unroll 1
+          for (; r0 < n; r0 += 16) {
+            uint32_t v[16];
+            tmem_ld16(v, from + r0);
+            tmem_wait_ld(v);
+#pragma unroll
+            for (int j = 0; j < 16; j += 2) {
+              float e[2];
+#pragma unroll
+              for (int h = 0; h < 2; h++) {
+                const float y = l[r0 + j + h];
+                const bool see = r0 + j + h < n && y != -INFINITY &&
+                                 (!last || (node < kNodes && key < 64 && mask[node] >> key & 1));
+                e[h] = see ? exp2_fast(fmaf(__uint_as_float(v[j + h]), c, y)) : 0.f;
+                if (last && ++head == G) head = 0, node++;
+              }
+              sum[j >> 1 & 1] = add_pair(sum[j >> 1 & 1], pair(e[0], e[1]));
+            }
+            __syncwarp();
           }
           tmem_before_sync();
           bar_arrive(smem_u32(&sh.t_free[buf]));
