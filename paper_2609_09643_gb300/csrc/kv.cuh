@@ -123,14 +123,22 @@ __device__ __forceinline__ int kv_length(const unison_kv_cache &c, int b) {
   if (c.status && n != len) c.status[b] = UNISON_ERR_RANGE;
   return len;
 }
-// Page of a slot, or -1.  The slot is below max_pages * page_size.
-__device__ __forceinline__ int kv_page(const unison_kv_cache &c, int b, int slot, int &off) {
+// Page of a slot (below max_pages * page_size), as the table has it: to be
+// checked by kv_page_ok when it is used, so that the load may be on its way.
+constexpr int kNoSlot = INT32_MIN;
+__device__ __forceinline__ int kv_page_load(const unison_kv_cache &c, int b, int slot, int &off) {
   const unsigned i = (unsigned)slot / (unsigned)c.page_size;
   off = slot - (int)(i * (unsigned)c.page_size);
-  const int page = __ldg(c.page_table + (int64_t)b * c.max_pages + i);
+  return __ldg(c.page_table + (int64_t)b * c.max_pages + i);
+}
+__device__ __forceinline__ int kv_page_ok(const unison_kv_cache &c, int b, int page) {
   if ((unsigned)page < (unsigned)c.n_pages) return page;
-  if (c.status) c.status[b] = UNISON_ERR_RANGE;
+  if (page != kNoSlot && c.status) c.status[b] = UNISON_ERR_RANGE;
   return -1;
+}
+// Page of a slot, or -1.
+__device__ __forceinline__ int kv_page(const unison_kv_cache &c, int b, int slot, int &off) {
+  return kv_page_ok(c, b, kv_page_load(c, b, slot, off));
 }
 
 __device__ __forceinline__ void wait_for_last_kernel() { asm volatile("griddepcontrol.wait;" ::: "memory"); }

@@ -38,7 +38,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) attend_kernel(con
   auto seq_tiles = [&](int b) -> int64_t {
     const int tokens = kv_tokens(P.t, b, P.c.status).count;
     const int row_tiles = (tokens * G + kRows - 1) / kRows;
-    return (int64_t)attend_key_tiles(kv_length(P.c, b), tokens, kTile) * row_tiles * H;
+    return (int64_t)(attend_key_tiles(kv_length(P.c, b), tokens, kTile) + kSetup) * row_tiles * H;
   };
   KvRun run;
   if (!kv_find_run(run, shared_run, P.c.n_seqs, gridDim.x, blockIdx.x, seq_tiles)) return;
@@ -57,12 +57,11 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) attend_kernel(con
     const int len = kv_length(P.c, b);
     const int key_tiles = attend_key_tiles(len, tok.count, kTile);
     const int row_tiles = (tok.count * G + kRows - 1) / kRows;
-    const int64_t rel = at - seq_begin;
-    const int seg = (int)(rel / key_tiles);
-    const int head = seg / row_tiles, row_tile = seg % row_tiles;
-    const int64_t seg_begin = seq_begin + (int64_t)seg * key_tiles;
-    const int kt0 = (int)(at - seg_begin);
-    const int kt1 = (int)min((int64_t)key_tiles, end - seg_begin);
+    const AttendSpan span = attend_span(at, end, seq_begin, key_tiles);
+    const int head = span.seg / row_tiles, row_tile = span.seg % row_tiles;
+    const int kt0 = span.kt0, kt1 = span.kt1;
+    at = span.begin + kSetup + kt1;
+    if (kt0 >= kt1) continue;
     const int rows = min(tok.count * G - row_tile * kRows, kRows);
     const int last_tile = key_tiles - 1;
 
@@ -83,8 +82,8 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) attend_kernel(con
     auto find_page = [&](int kt, int &off) -> int {  // threads 0 .. kTile-1
       const int slot = kt * kTile + tid;
       off = 0;
-      if (tid >= kTile || kt >= last_tile || slot >= len) return -1;
-      return kv_page(P.c, b, slot, off);
+      if (tid >= kTile || kt >= last_tile || slot >= len) return kNoSlot;
+      return kv_page_load(P.c, b, slot, off);
     };
     auto put_rows = [&](int kt, int page, int off) {
       if (tid >= kTile) return;
@@ -94,7 +93,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) attend_kernel(con
           k = static_cast<const T *>(P.s.k_new) + (tok.first + tid) * P.s.k_token + head * P.s.k_head;
           v = static_cast<const T *>(P.s.v_new) + (tok.first + tid) * P.s.v_token + head * P.s.v_head;
         }
-      } else if (page >= 0) {
+      } else if ((page = kv_page_ok(P.c, b, page)) >= 0) {
         k = static_cast<const T *>(P.c.k) + page * P.c.k_page + head * P.c.k_head + off * P.c.k_slot;
         v = static_cast<const T *>(P.c.v) + page * P.c.v_page + head * P.c.v_head + off * P.c.v_slot;
       }
@@ -324,8 +323,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) attend_kernel(con
       }
     }
     if (starts && !whole && tid == 0)
-      P.part[blockIdx.x] = {b, head, row_tile, kv_run_of(run, seg_begin + key_tiles - 1)};
-    at = seg_begin + kt1;
+      P.part[blockIdx.x] = {b, head, row_tile, kv_run_of(run, span.begin + kSetup + key_tiles - 1)};
   }
 }
 
@@ -350,8 +348,6 @@ __global__ void __launch_bounds__(kJoin) attend_join_kernel(const AttendParams P
   const int D = P.c.head_dim, G = P.group, R = P.rows;
   const KvRange tok = kv_tokens(P.t, seg.b, nullptr);
   const int rows = min(tok.count * G - seg.row_tile * R, R);
-  const int row0 = blockIdx.y * kJoinRows;
-  if (row0 >= rows) return;
   const int step = P.row_groups;  // CTAs from one run to the next
   const int parts = seg.last - (int)blockIdx.x / step + 1;
   const int64_t stride = (int64_t)2 * R * (DP + 2) * step;
@@ -361,56 +357,58 @@ __global__ void __launch_bounds__(kJoin) attend_join_kernel(const AttendParams P
   auto part = [&](int p) { return p ? rest + p * stride : first; };
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  float top = -INFINITY, l = 0.f;
-  if (warp < kJoinRows && row0 + warp < rows) {
-    for (int p = lane; p < parts; p += 32) top = fmaxf(top, part(p)[R * DP + row0 + warp]);
-#pragma unroll
-    for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
-  }
-  const float base = top == -INFINITY ? 0.f : top;
   const int row = threadIdx.x / kVec % kJoinRows, share = threadIdx.x / (kVec * kJoinRows), col = threadIdx.x % kVec * 4;
-  float4 sum = {0.f, 0.f, 0.f, 0.f};
-  for (int p0 = 0; p0 < parts; p0 += kParts) {
-    const int n = min(parts - p0, kParts);
-    __syncthreads();
-    if (warp < kJoinRows && row0 + warp < rows)
-      for (int p = lane; p < n; p += 32) {
-        const float *q = part(p0 + p) + R * DP + row0 + warp;
-        const float f = exp2_fast(q[0] - base);
-        weight[warp][p] = f;
-        l += q[R] * f;
-      }
-    __syncthreads();
-    if (row0 + row < rows && col < D)
+  for (int row0 = blockIdx.y * kJoinRows; row0 < rows; row0 += gridDim.y * kJoinRows) {
+    float top = -INFINITY, l = 0.f;
+    if (warp < kJoinRows && row0 + warp < rows) {
+      for (int p = lane; p < parts; p += 32) top = fmaxf(top, part(p)[R * DP + row0 + warp]);
+#pragma unroll
+      for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+    }
+    const float base = top == -INFINITY ? 0.f : top;
+    float4 sum = {0.f, 0.f, 0.f, 0.f};
+    for (int p0 = 0; p0 < parts; p0 += kParts) {
+      const int n = min(parts - p0, kParts);
+      __syncthreads();
+      if (warp < kJoinRows && row0 + warp < rows)
+        for (int p = lane; p < n; p += 32) {
+          const float *q = part(p0 + p) + R * DP + row0 + warp;
+          const float f = exp2_fast(q[0] - base);
+          weight[warp][p] = f;
+          l += q[R] * f;
+        }
+      __syncthreads();
+      if (row0 + row < rows && col < D)
 #pragma unroll 8
-      for (int p = share; p < n; p += kShares) {
-        const float4 x = *reinterpret_cast<const float4 *>(part(p0 + p) + (row0 + row) * DP + col);
-        const float f = weight[row][p];
-        sum.x += x.x * f, sum.y += x.y * f, sum.z += x.z * f, sum.w += x.w * f;
+        for (int p = share; p < n; p += kShares) {
+          const float4 x = *reinterpret_cast<const float4 *>(part(p0 + p) + (row0 + row) * DP + col);
+          const float f = weight[row][p];
+          sum.x += x.x * f, sum.y += x.y * f, sum.z += x.z * f, sum.w += x.w * f;
+        }
+    }
+    if (warp < kJoinRows) {
+#pragma unroll
+      for (int d = 16; d; d >>= 1) l += __shfl_xor_sync(~0u, l, d);
+      if (lane == 0) row_l[warp] = l, row_top[warp] = top;
+    }
+    sums[share][row][col / 4] = sum;
+    __syncthreads();
+    if (share == 0 && row0 + row < rows && col < D) {
+#pragma unroll
+      for (int s = 1; s < kShares; s++) {
+        const float4 x = sums[s][row][col / 4];
+        sum.x += x.x, sum.y += x.y, sum.z += x.z, sum.w += x.w;
       }
+      l = row_l[row];
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      const int at = seg.row_tile * R + row0 + row, node = at / G, head = seg.head * G + at % G;
+      T *dst = static_cast<T *>(P.s.out) + (tok.first + node) * P.s.out_token + head * P.s.out_head + col;
+      *reinterpret_cast<uint2 *>(dst) =
+          make_uint2(KvType<T>::pack(sum.x * inv, sum.y * inv), KvType<T>::pack(sum.z * inv, sum.w * inv));
+      if (col == 0 && P.s.lse)
+        P.s.lse[(int64_t)(tok.first + node) * P.s.n_q_heads + head] = (row_top[row] + log2f(l)) * 0.6931471805599453f;
+    }
   }
-  if (warp < kJoinRows) {
-#pragma unroll
-    for (int d = 16; d; d >>= 1) l += __shfl_xor_sync(~0u, l, d);
-    if (lane == 0) row_l[warp] = l, row_top[warp] = top;
-  }
-  sums[share][row][col / 4] = sum;
-  __syncthreads();
-  if (share > 0 || row0 + row >= rows || col >= D) return;
-#pragma unroll
-  for (int s = 1; s < kShares; s++) {
-    const float4 x = sums[s][row][col / 4];
-    sum.x += x.x, sum.y += x.y, sum.z += x.z, sum.w += x.w;
-  }
-  l = row_l[row];
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  const int at = seg.row_tile * R + row0 + row, node = at / G;
-  T *dst = static_cast<T *>(P.s.out) + (tok.first + node) * P.s.out_token + (seg.head * G + at % G) * P.s.out_head + col;
-  *reinterpret_cast<uint2 *>(dst) =
-      make_uint2(KvType<T>::pack(sum.x * inv, sum.y * inv), KvType<T>::pack(sum.z * inv, sum.w * inv));
-  if (col == 0 && P.s.lse)
-    P.s.lse[(int64_t)(tok.first + node) * P.s.n_q_heads + seg.head * G + at % G] =
-        (row_top[row] + log2f(l)) * 0.6931471805599453f;
 }
 
 struct AttendPlan {
@@ -433,8 +431,9 @@ AttendPlan attend_plan(int head_dim, int max_rows) {
 
 template <typename T, int DP>
 int attend_join(const AttendParams &p, const AttendPlan &plan, int max_rows, void *stream) {
-  return kv_launch("kv_attend_join", dim3(plan.grid, (min(max_rows, plan.rows) + kJoinRows - 1) / kJoinRows),
-                   dim3(kJoin), 0, stream, kAfterLast, attend_join_kernel<T, DP>, p);
+  const int rounds = (min(max_rows, plan.rows) + kJoinRows - 1) / kJoinRows;
+  return kv_launch("kv_attend_join", dim3(plan.grid, min(rounds, 8)), dim3(kJoin), 0, stream, kAfterLast,
+                   attend_join_kernel<T, DP>, p);
 }
 
 template <typename T, int DP, int MT>

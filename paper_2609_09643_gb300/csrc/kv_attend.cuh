@@ -27,6 +27,24 @@ __device__ __forceinline__ int attend_key_tiles(int len, int tokens, int tile) {
   return tokens ? (len + tile - 1) / tile + 1 : 0;
 }
 
+// A segment's tiles come in the list of tiles behind kSetup places that stand
+// for its beginning (statistics, query rows, an empty pipeline), so that runs
+// of many short sessions take as long as runs of few long ones.
+constexpr int kSetup = 2;
+struct AttendSpan {
+  int seg, kt0, kt1;
+  int64_t begin;  // of the segment in the list
+};
+// What a run has of the segment that place `at` lies in; kt0 >= kt1: no tile.
+__device__ __forceinline__ AttendSpan attend_span(int64_t at, int64_t end, int64_t seq_begin, int tiles) {
+  AttendSpan s;
+  s.seg = (int)((at - seq_begin) / (tiles + kSetup));
+  s.begin = seq_begin + (int64_t)s.seg * (tiles + kSetup);
+  s.kt0 = (int)max(at - s.begin - kSetup, (int64_t)0);
+  s.kt1 = (int)max(min(end - s.begin - kSetup, (int64_t)tiles), (int64_t)0);
+  return s;
+}
+
 constexpr int kTcRows = 256;  // query rows of a CTA on the tensor cores: two tiles of 128
 template <typename T, int DP>
 int attend_tc(const AttendParams &p, int grid, void *stream);

@@ -40,7 +40,7 @@ struct TcShared {
 
 // What every role works out alike for the segment that `at` lies in.
 struct Segment {
-  int b, head, row_tile, rows, tiles, kt0, kt1, len;
+  int b, head, row_tile, rows, tiles, kt0, kt1, len;  // rows <= 0: nothing to do for this CTA
   KvRange tok;
 };
 
@@ -62,7 +62,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
   auto seq_tiles = [&](int b) -> int64_t {
     const int tokens = kv_tokens(P.t, b, P.c.status).count;
     const int row_tiles = (tokens * G + kTcRows - 1) / kTcRows;
-    return (int64_t)attend_key_tiles(kv_length(P.c, b), tokens, kTile) * ((row_tiles + groups - 1) / groups) * H;
+    return (int64_t)(attend_key_tiles(kv_length(P.c, b), tokens, kTile) + kSetup) * ((row_tiles + groups - 1) / groups) * H;
   };
   KvRun run;
   if (!kv_find_run(run, sh.run, P.c.n_seqs, gridDim.x / groups, blockIdx.x / groups, seq_tiles)) return;
@@ -103,14 +103,15 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     g.tiles = attend_key_tiles(g.len, g.tok.count, kTile);
     const int row_tiles = (g.tok.count * G + kTcRows - 1) / kTcRows;
     const int row_groups = (row_tiles + groups - 1) / groups;
-    const int seg = (int)((at - seq_begin) / g.tiles);
-    seg_begin = seq_begin + (int64_t)seg * g.tiles;
-    g.head = seg / row_groups;
-    g.row_tile = seg % row_groups * groups + rank;
-    g.rows = min(g.tok.count * G - g.row_tile * kTcRows, kTcRows);  // <= 0: this CTA has none
-    g.kt0 = (int)(at - seg_begin);
-    g.kt1 = (int)min((int64_t)g.tiles, run.end - seg_begin);
-    at = seg_begin + g.kt1;
+    const AttendSpan span = attend_span(at, run.end, seq_begin, g.tiles);
+    seg_begin = span.begin;
+    g.head = span.seg / row_groups;
+    g.row_tile = span.seg % row_groups * groups + rank;
+    g.rows = min(g.tok.count * G - g.row_tile * kTcRows, kTcRows);
+    g.kt0 = span.kt0;
+    g.kt1 = span.kt1;
+    if (g.kt0 >= g.kt1) g.rows = 0;
+    at = span.begin + kSetup + g.kt1;
   };
 
   if (warp >= kCopyWarp && warp < kIssueWarp) {
@@ -159,14 +160,14 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
         const int boxes = by_boxes ? kTile / P.k_boxes.rows : 0;
         int page = -1, off = 0;
         auto find_box = [&](int kt) {
-          if (lane < boxes) page = kv_page(P.c, g.b, kt * kTile + lane * P.k_boxes.rows, off);
+          if (lane < boxes) page = kv_page_load(P.c, g.b, kt * kTile + lane * P.k_boxes.rows, off);
         };
         if (kt < boxed) find_box(kt);
         for (; kt < boxed; kt++, tile_no++) {
           uint32_t bar;
           uint32_t dst = slot_for(bar);
           if (!ok) break;
-          const int p = page, o = off;
+          const int p = lane < boxes ? kv_page_ok(P.c, g.b, page) : -1, o = off;
           const uint32_t there = __ballot_sync(~0u, lane >= boxes || p >= 0);
           // (row 32 i + j of the tile lies in box (32 i + j) / rows)
           if (lane < 4) {
@@ -501,7 +502,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
         }
       }
       if (!whole && g.kt0 == 0 && r == 0 && q == 0)
-        P.part[blockIdx.x] = {g.b, g.head, g.row_tile, kv_run_of(run, seg_begin + g.tiles - 1)};
+        P.part[blockIdx.x] = {g.b, g.head, g.row_tile, kv_run_of(run, seg_begin + kSetup + g.tiles - 1)};
       __syncwarp();
       tmem_before_sync();  // the next segment's products overwrite O
     }

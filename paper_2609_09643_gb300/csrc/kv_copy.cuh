@@ -137,7 +137,7 @@ struct KvCopier {
     return __any_sync(~0u, odd);
   }
   // After a wait that ran out: boxes on their way may still arrive for a while.
-  __device__ __forceinline__ void give_up() {
+  static __device__ __forceinline__ void give_up() {
     for (int i = 0; i < 1000; i++) __nanosleep(1000);
   }
   __device__ __forceinline__ void arrive(uint32_t bar) {

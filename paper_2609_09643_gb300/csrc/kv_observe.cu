@@ -79,8 +79,8 @@ __global__ void __launch_bounds__(kThreads) observe_kernel(const ObserveParams P
     auto find_page = [&](int kt, int &off) -> int {
       const int slot = kt * kTile + tid;
       off = 0;
-      if (tid >= kTile || kt >= last_tile || slot >= len) return -1;
-      return kv_page(P.c, b, slot, off);
+      if (tid >= kTile || kt >= last_tile || slot >= len) return kNoSlot;
+      return kv_page_load(P.c, b, slot, off);
     };
     auto put_rows = [&](int kt, int page, int off) {
       if (tid >= kTile) return;
@@ -91,7 +91,7 @@ __global__ void __launch_bounds__(kThreads) observe_kernel(const ObserveParams P
           k = static_cast<const T *>(P.s.k_new) + (tok.first + tid) * P.s.k_token + head * P.s.k_head;
           m = (int64_t)(tok.first + tid) * H + head;
         }
-      } else if (page >= 0) {
+      } else if ((page = kv_page_ok(P.c, b, page)) >= 0) {
         k = static_cast<const T *>(P.c.k) + page * P.c.k_page + head * P.c.k_head + off * P.c.k_slot;
         m = page * P.c.m_page + head * P.c.m_head + off * P.c.m_slot;
       }

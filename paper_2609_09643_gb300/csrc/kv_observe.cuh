@@ -11,7 +11,7 @@ struct ObserveParams {
   unison_kv_step s;
   unison_kv_path path;
   int group;         // query heads of a KV head
-  int q_rows, slots;  // tensor cores: query rows that fit, key tiles on their way
+  int q_rows, q_buffers, slots;  // tensor cores: query rows that fit, how often, key tiles on their way
 };
 
 // Accepted nodes of a session.

@@ -6,7 +6,9 @@
 // weights in its registers, so nothing is exchanged between threads and no
 // atomics are needed.  A CTA keeps the query rows of one segment (session and
 // KV head) in shared memory and streams tiles of 128 keys past them.  Roles:
-//   warps 8-11      copy key tiles and, per segment, the query rows
+//   warps 8-11      find each key's account and, per segment, copy the query
+//                   rows; key tiles that are not full, row by row
+//   warp 13         full key tiles, by TMA
 //   warp 12         issues the products, 128 query rows at a time, into four
 //                   buffers of tensor memory
 //   warps 0-3, 4-7  turn the scores of a buffer into weights, in turn
@@ -16,10 +18,11 @@
 namespace unison {
 namespace {
 
-constexpr int kThreads = 416;
+constexpr int kThreads = 448;
 constexpr int kTile = 128;
-constexpr int kCopyWarp = 8, kIssueWarp = 12;
+constexpr int kCopyWarp = 8, kIssueWarp = 12, kBoxWarp = 13;
 constexpr int kBuffers = 4, kMostSlots = 6;
+constexpr int kSetup = 2;  // tiles that a segment's beginning costs
 constexpr int kNodes = UNISON_KV_MAX_TOKENS;
 // Tiles whose keys' accounts are kept in shared memory: those on their way,
 // those in tensor memory, and the two that are being finished.
@@ -28,7 +31,7 @@ constexpr int kMarkBytes = kMarks * kTile * 12;
 
 struct ObserveShared {
   KvRunShared run;
-  uint64_t k_full[kMostSlots], k_free[kMostSlots], q_full, q_free, t_full[kBuffers], t_free[kBuffers], seg_done[2],
+  uint64_t k_full[kMostSlots], k_free[kMostSlots], q_full[2], q_free[2], t_full[kBuffers], t_free[kBuffers], seg_done[2],
       part_full, part_free, idle;
   uint64_t mask[2][kNodes];  // of the accepted nodes
   float part[kTile];         // the second group's sums
@@ -53,7 +56,8 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
   __shared__ ObserveShared sh;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int D = P.c.head_dim, H = P.c.n_heads, G = P.group;
-  const uint32_t q_base = (smem_u32(smem_raw) + 1023) & ~1023u, slot_base = q_base + P.q_rows * DP * 2;
+  const uint32_t q_base = (smem_u32(smem_raw) + 1023) & ~1023u, q_bytes = P.q_rows * DP * 2,
+                 slot_base = q_base + P.q_buffers * q_bytes;
   // log-sums of the rows, of two segments, in log2 units and negated; -inf: no weight from this row
   float *const lse_base = reinterpret_cast<float *>(smem_raw + (slot_base - smem_u32(smem_raw)) + P.slots * kTileBytes);
 
@@ -68,22 +72,24 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
   };
   KvRun run;
   if (!kv_find_run(run, sh.run, P.c.n_seqs, gridDim.x, blockIdx.x, [&](int b) {
-        return (int64_t)observe_key_tiles(P, b, kTile) * H * share(b, kv_tokens(P.t, b, nullptr).count);
+        const int tiles = observe_key_tiles(P, b, kTile);
+        return tiles ? (int64_t)(tiles + kSetup) * H * share(b, kv_tokens(P.t, b, nullptr).count) : 0;
       }))
     return;
   if (tid == 0) {
     for (int i = 0; i < kMostSlots; i++) {
-      bar_init(smem_u32(&sh.k_full[i]), 4);  // copying warps
+      bar_init(smem_u32(&sh.k_full[i]), 5);  // copying warps
       bar_init(smem_u32(&sh.k_free[i]), 1);
     }
     for (int i = 0; i < kBuffers; i++) {
       bar_init(smem_u32(&sh.t_full[i]), 2);
       bar_init(smem_u32(&sh.t_free[i]), 128);
     }
-    bar_init(smem_u32(&sh.q_full), 4);
-    bar_init(smem_u32(&sh.q_free), 1);
-    bar_init(smem_u32(&sh.seg_done[0]), 256);
-    bar_init(smem_u32(&sh.seg_done[1]), 256);
+    for (int i = 0; i < 2; i++) {
+      bar_init(smem_u32(&sh.q_full[i]), 4);
+      bar_init(smem_u32(&sh.q_free[i]), 1);
+      bar_init(smem_u32(&sh.seg_done[i]), 256);
+    }
     bar_init(smem_u32(&sh.part_full), 128);
     bar_init(smem_u32(&sh.part_free), 128);
     bar_init(smem_u32(&sh.idle), 1);
@@ -99,26 +105,31 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
   int b = run.b;
   int64_t at = run.at, seq_begin = run.begin;
   // The next tiles of one head in this run: those whose share begins in it.
+  // (A head's tiles come behind kSetup shares that stand for its beginning.)
   auto next_segment = [&](Segment &g) -> bool {
     while (at < run.end) {
       g.tok = kv_tokens(P.t, b, nullptr);
       g.tiles = observe_key_tiles(P, b, kTile);
-      const int64_t each = share(b, g.tok.count), all = (int64_t)g.tiles * H;
-      const int64_t tile = (at - seq_begin + each - 1) / each;
-      const int64_t end = min((run.end - seq_begin + each - 1) / each, all);
-      if (tile < end) {
-        g.b = b;
-        g.len = kv_length(P.c, b);
-        g.rows = path_count(P, b, g.tok.count) * G;
-        g.head = (int)(tile / g.tiles);
-        g.kt0 = (int)(tile % g.tiles);
-        g.kt1 = (int)min((int64_t)g.tiles, g.kt0 + end - tile);
-        at = seq_begin + (tile + g.kt1 - g.kt0) * each;
-        return true;
+      const int64_t each = share(b, g.tok.count), per_head = g.tiles ? g.tiles + kSetup : 0;
+      const int64_t all = per_head * H;
+      const int64_t from = (at - seq_begin + each - 1) / each;
+      const int64_t to = min((run.end - seq_begin + each - 1) / each, all);
+      if (from >= to) {
+        seq_begin += all * each;
+        at = max(at, seq_begin);
+        b++;
+        continue;
       }
-      seq_begin += all * each;
-      at = max(at, seq_begin);
-      b++;
+      g.head = (int)(from / per_head);
+      const int64_t head_begin = g.head * per_head, head_end = min(head_begin + per_head, to);
+      at = seq_begin + head_end * each;
+      g.kt0 = (int)max(from - head_begin - kSetup, (int64_t)0);
+      g.kt1 = (int)max(head_end - head_begin - kSetup, (int64_t)0);
+      if (g.kt0 >= g.kt1) continue;
+      g.b = b;
+      g.len = kv_length(P.c, b);
+      g.rows = path_count(P, b, g.tok.count) * G;
+      return true;
     }
     return false;
   };
@@ -131,9 +142,10 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
     bool ok = true;
     Segment g;
     while (ok && next_segment(g)) {
-      // The segment's rows: when the last one's products have read theirs, and
-      // nobody reads the statistics of the one before any more.
-      if (seg_no > 0) ok = copier.wait(smem_u32(&sh.q_free), (seg_no - 1) & 1, &sh.dead);
+      // The segment's rows: when the products of the last one that was in their
+      // place are done, and nobody reads the statistics of the one before last.
+      const int buf = seg_no % P.q_buffers, use = seg_no / P.q_buffers;
+      if (use > 0) ok = copier.wait(smem_u32(&sh.q_free[buf]), (use - 1) & 1, &sh.dead);
       if (ok && seg_no > 1)
         ok = copier.wait(smem_u32(&sh.seg_done[seg_no & 1]), ((seg_no >> 1) - 1) & 1, &sh.dead);
       if (!ok) break;
@@ -152,7 +164,7 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
         }
         if (r < g.rows && l == -INFINITY) plain = false;
         lse[r] = l;
-        copier.rows(q_base + r0 / 128 * kTileBytes, src);
+        copier.rows(q_base + buf * q_bytes + r0 / 128 * kTileBytes, src);
       }
       if (j < kNodes) {
         const int node = j * G < g.rows ? observe_node(P, g.b, g.tok.count, j) : -1;
@@ -160,18 +172,20 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
       }
       plain = __all_sync(~0u, plain);
       if (lane == 0) sh.plain[seg_no & 1][w] = plain;
-      copier.issued(smem_u32(&sh.q_full));
+      copier.issued(smem_u32(&sh.q_full[buf]));
 
       // a tile's pages are looked up two tiles ahead, the weights there one ahead
       auto find_page = [&](int kt, int &off) -> int {
         off = 0;
-        return kt < g.tiles - 1 && kt * kTile + j < g.len ? kv_page(P.c, g.b, kt * kTile + j, off) : -1;
+        return kt < g.kt1 && kt < g.tiles - 1 && kt * kTile + j < g.len
+                   ? kv_page_load(P.c, g.b, kt * kTile + j, off) : kNoSlot;
       };
       auto account = [&](int page, int off) -> float * {
         return page < 0 ? nullptr : P.c.mass + page * P.c.m_page + g.head * P.c.m_head + off * P.c.m_slot;
       };
-      int next_off = 0, next_page = find_page(g.kt0, next_off), later_off = 0, later_page = -1;
-      if (g.kt0 + 1 < g.kt1) later_page = find_page(g.kt0 + 1, later_off);
+      int next_off = 0, later_off = 0;
+      int next_page = find_page(g.kt0, next_off), later_page = find_page(g.kt0 + 1, later_off);
+      next_page = kv_page_ok(P.c, g.b, next_page);
       float *next_m = account(next_page, next_off);
       float next_old = next_m ? *next_m : 0.f;
       const int boxed = P.k_boxes.rows ? g.len / kTile : 0;  // full tiles go by boxes
@@ -179,15 +193,15 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
         const int page = next_page, off = next_off;
         float *m = next_m;
         const float old = next_old;
-        next_page = later_page, next_off = later_off;
-        next_m = kt + 1 < g.kt1 ? account(next_page, next_off) : nullptr;
+        next_page = kv_page_ok(P.c, g.b, later_page), next_off = later_off;
+        next_m = account(next_page, next_off);
         next_old = next_m ? *next_m : 0.f;
-        if (kt + 2 < g.kt1) later_page = find_page(kt + 2, later_off);
+        later_page = find_page(kt + 2, later_off);
         const int s = item % P.slots, n = item / P.slots;
         if (n > 0) ok = copier.wait(smem_u32(&sh.k_free[s]), (n - 1) & 1, &sh.dead);
         if (!ok) break;
         item++;
-        const uint32_t dst = slot_base + s * kTileBytes, bar = smem_u32(&sh.k_full[s]);
+        const uint32_t bar = smem_u32(&sh.k_full[s]);
         const bool fresh = kt == g.tiles - 1 && j < g.tok.count && P.s.mass_new;
         if (fresh) m = P.s.mass_new + (int64_t)(g.tok.first + j) * H + g.head;
         const int mark = tile_no++ % kMarks * kTile + j;
@@ -195,14 +209,7 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
         marks_old[mark] = old;
         __syncwarp();
         if (kt < boxed) {
-          if (w == 0) {
-            // (found before, by the lane of the box's first row: in the nearest cache)
-            int p = page, o = off;
-            if (P.k_boxes.rows * lane < kTile) p = kv_page(P.c, g.b, kt * kTile + P.k_boxes.rows * lane, o);
-            tile_boxes<DP>(dst, P.k_boxes, bar, g.head, p, o);
-          } else if (lane == 0) {
-            bar_arrive(bar);
-          }
+          if (lane == 0) bar_arrive(bar);
           if (kt == g.kt0) copier.landed();
         } else {
           const T *src = nullptr;
@@ -210,14 +217,40 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
             src = static_cast<const T *>(P.s.k_new) + (g.tok.first + j) * P.s.k_token + g.head * P.s.k_head;
           else if (page >= 0)
             src = static_cast<const T *>(P.c.k) + page * P.c.k_page + g.head * P.c.k_head + off * P.c.k_slot;
-          copier.rows(dst, src);
+          copier.rows(slot_base + s * kTileBytes, src);
           copier.issued(bar);
         }
       }
       seg_no++;
     }
     copier.landed();
-    if (!ok) copier.give_up();
+  } else if (warp == kBoxWarp) {
+    // -------------------------------------------------------------- boxes
+    int item = 0;
+    bool ok = true;
+    const int boxes = P.k_boxes.rows ? kTile / P.k_boxes.rows : 0;
+    Segment g;
+    while (ok && next_segment(g)) {
+      const int boxed = boxes ? g.len / kTile : 0;
+      int page = kNoSlot, off = 0;
+      auto find_box = [&](int kt) {
+        if (lane < boxes && kt < boxed) page = kv_page_load(P.c, g.b, kt * kTile + lane * P.k_boxes.rows, off);
+      };
+      find_box(g.kt0);
+      for (int kt = g.kt0; kt < g.kt1; kt++, item++) {
+        const int s = item % P.slots, n = item / P.slots;
+        if (n > 0) ok = __all_sync(~0u, bar_wait(smem_u32(&sh.k_free[s]), (n - 1) & 1, &sh.dead));
+        if (!ok) break;
+        if (kt < boxed) {
+          const int p = lane < boxes ? kv_page_ok(P.c, g.b, page) : -1, o = off;
+          tile_boxes<DP>(slot_base + s * kTileBytes, P.k_boxes, smem_u32(&sh.k_full[s]), g.head, p, o);
+          if (kt + 1 < g.kt1) find_box(kt + 1);
+        } else if (lane == 0) {
+          bar_arrive(smem_u32(&sh.k_full[s]));
+        }
+      }
+    }
+    if (!ok) KvCopier<T, DP>::give_up();
   } else if (warp == kIssueWarp) {
     // ----------------------------------------------------------- products
     // (the whole warp goes along, one lane issues)
@@ -230,10 +263,11 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
     };
     Segment g;
     while (ok && next_segment(g)) {
+      const int qb = seg_no % P.q_buffers;
       for (int kt = g.kt0; kt < g.kt1 && ok; kt++) {
         const int s = item % P.slots;
         ok = __all_sync(~0u, bar_wait(smem_u32(&sh.k_full[s]), (item / P.slots) & 1, &sh.dead));
-        if (ok && kt == g.kt0) ok = __all_sync(~0u, bar_wait(smem_u32(&sh.q_full), seg_no & 1, &sh.dead));
+        if (ok && kt == g.kt0) ok = __all_sync(~0u, bar_wait(smem_u32(&sh.q_full[qb]), (seg_no / P.q_buffers) & 1, &sh.dead));
         item++;
         const uint32_t keys = slots + s * (kTileBytes >> 4);
         for (int r0 = 0; (r0 == 0 || r0 < g.rows) && ok; r0 += 128, job++) {
@@ -245,7 +279,7 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
           const int columns = (max(min(g.rows - r0, 128), 1) + 15) & ~15;
           const uint32_t shape = product_shape(kOperandType<T>, kTile, columns, false, false);
           if (elect_one()) {
-            const uint32_t rows = q_rows + r0 / 128 * (kTileBytes >> 4);
+            const uint32_t rows = q_rows + ((qb * q_bytes + r0 / 128 * kTileBytes) >> 4);
 #pragma unroll
             for (int d = 0; d < DP / 16; d++) {
               const uint32_t o = (d / 4 * kBlock + d % 4 * 32) >> 4;
@@ -258,7 +292,7 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
         }
         release(sh.k_free[s]);
       }
-      release(sh.q_free);
+      release(sh.q_free[qb]);
       seg_no++;
     }
     // nothing may still be at work when tensor memory is freed
@@ -328,23 +362,31 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
           int node = (i * 128 + r0) / G, head = (i * 128 + r0) % G;
 #pragma unroll 1
           for (; r0 < n; r0 += 16) {
-            uint32_t v[16];
+            uint32_t v[16], counts = n - r0 < 16 ? (1u << (n - r0)) - 1 : ~0u;
             tmem_ld16(v, from + r0);
-            tmem_wait_ld(v);
-#pragma unroll
-            for (int j = 0; j < 16; j += 2) {
-              float e[2];
-#pragma unroll
-              for (int h = 0; h < 2; h++) {
-                const float y = l[r0 + j + h];
-                const bool see = r0 + j + h < n && y != -INFINITY &&
-                                 (!last || (node < kNodes && key < 64 && mask[node] >> key & 1));
-                e[h] = see ? exp2_fast(fmaf(__uint_as_float(v[j + h]), c, y)) : 0.f;
-                if (last && ++head == G) head = 0, node++;
+            if (last) {
+#pragma unroll 1
+              for (int j = 0; j < 16; j++) {
+                if (node >= kNodes || key >= 64 || !(mask[node] >> key & 1)) counts &= ~(1u << j);
+                if (++head == G) head = 0, node++;
               }
-              sum[j >> 1 & 1] = add_pair(sum[j >> 1 & 1], pair(e[0], e[1]));
             }
             __syncwarp();
+            tmem_wait_ld(v);
+#pragma unroll
+            for (int j = 0; j < 16; j += 4) {
+              const float4 y = *reinterpret_cast<const float4 *>(l + r0 + j);
+              float e[4] = {exp2_fast(fmaf(__uint_as_float(v[j]), c, y.x)),
+                            exp2_fast(fmaf(__uint_as_float(v[j + 1]), c, y.y)),
+                            exp2_fast(fmaf(__uint_as_float(v[j + 2]), c, y.z)),
+                            exp2_fast(fmaf(__uint_as_float(v[j + 3]), c, y.w))};
+              e[0] = (counts >> j & 1) && y.x != -INFINITY ? e[0] : 0.f;
+              e[1] = (counts >> (j + 1) & 1) && y.y != -INFINITY ? e[1] : 0.f;
+              e[2] = (counts >> (j + 2) & 1) && y.z != -INFINITY ? e[2] : 0.f;
+              e[3] = (counts >> (j + 3) & 1) && y.w != -INFINITY ? e[3] : 0.f;
+              sum[0] = add_pair(sum[0], pair(e[0], e[1]));
+              sum[1] = add_pair(sum[1], pair(e[2], e[3]));
+            }
           }
           tmem_before_sync();
           bar_arrive(smem_u32(&sh.t_free[buf]));
@@ -395,7 +437,8 @@ int observe_tc(ObserveParams p, int max_rows, void *stream) {
   constexpr int kMost = 226 << 10;
   static uint64_t done = 0;
   p.q_rows = (max_rows + 127) / 128 * 128;
-  const int fixed = 1024 + p.q_rows * (DP * 2 + 8) + kMarkBytes + (int)sizeof(ObserveShared);
+  p.q_buffers = p.q_rows == 128 ? 2 : 1;  // few rows: the next segment's may come while the last one's are read
+  const int fixed = 1024 + p.q_rows * (p.q_buffers * DP * 2 + 8) + kMarkBytes + (int)sizeof(ObserveShared);
   p.slots = min(kMostSlots, (kMost - fixed) / kTileBytes);
   const int bytes = fixed - (int)sizeof(ObserveShared) + p.slots * kTileBytes;
   if (!kv_allow_smem(reinterpret_cast<const void *>(observe_tc_kernel<T, DP>), kMost - (int)sizeof(ObserveShared), &done))
