@@ -47,11 +47,9 @@ int kv_sm_count();
 // (`done`: a bit per device, kept by the caller beside the kernel).
 bool kv_allow_smem(const void *kernel, int bytes, uint64_t *done);
 
-// Queues a kernel of clusters of `cluster` CTAs.  kAfterLast instead: a kernel
-// that may be set up while the one before it on the stream ends, and calls
-// wait_for_last_kernel before it reads that one's results.  The verdict is the
-// launch's own, not an older error's.
-constexpr int kAfterLast = 0;
+// Queues a kernel of clusters of `cluster` CTAs.  It may be set up while the
+// kernel before it on the stream ends: all of these kernels begin with
+// follow_last_kernel().  The verdict is the launch's own, not an older error's.
 template <typename... P, typename... A>
 int kv_launch(const char *name, dim3 grid, dim3 block, size_t smem, void *stream, int cluster, void (*kernel)(P...),
               A &&...args) {
@@ -63,18 +61,15 @@ int kv_launch(const char *name, dim3 grid, dim3 block, size_t smem, void *stream
     lc.blockDim = block;
     lc.dynamicSmemBytes = smem;
     lc.stream = static_cast<cudaStream_t>(stream);
-    cudaLaunchAttribute at[1];
-    if (cluster == kAfterLast) {
-      at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-      at[0].val.programmaticStreamSerializationAllowed = 1;
-    } else {
-      at[0].id = cudaLaunchAttributeClusterDimension;
-      at[0].val.clusterDim.x = cluster;
-      at[0].val.clusterDim.y = 1;
-      at[0].val.clusterDim.z = 1;
-    }
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = cluster;
+    at[1].val.clusterDim.y = 1;
+    at[1].val.clusterDim.z = 1;
     lc.attrs = at;
-    lc.numAttrs = cluster == 1 ? 0 : 1;
+    lc.numAttrs = cluster > 1 ? 2 : 1;
     e = cudaLaunchKernelEx(&lc, kernel, static_cast<P>(args)...);
   }
   count_launches(1);
@@ -141,7 +136,12 @@ __device__ __forceinline__ int kv_page(const unison_kv_cache &c, int b, int slot
   return kv_page_ok(c, b, kv_page_load(c, b, slot, off));
 }
 
-__device__ __forceinline__ void wait_for_last_kernel() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// The kernel before this one is complete and its results are seen; the next one
+// may be set up from here on (it waits in the same way).
+__device__ __forceinline__ void follow_last_kernel() {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
 
 __device__ __forceinline__ uint32_t smem_u32(const void *p) {
   return static_cast<uint32_t>(__cvta_generic_to_shared(p));

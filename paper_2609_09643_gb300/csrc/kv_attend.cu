@@ -17,6 +17,7 @@ constexpr int kAttendSmem = kAttendStages<DP> *kTile *DP * 4 + MT * 16 * DP * 2;
 // the copies.
 template <typename T, int DP, int MT>
 __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) attend_kernel(const AttendParams P) {
+  follow_last_kernel();
   constexpr int kStages = kAttendStages<DP>;
   constexpr int kRows = MT * 16;
   constexpr int kGroups = 4 / MT;      // groups of warps with keys of their own
@@ -337,12 +338,12 @@ constexpr int kParts = 256;
 
 template <typename T, int DP>
 __global__ void __launch_bounds__(kJoin) attend_join_kernel(const AttendParams P) {
+  follow_last_kernel();
   constexpr int kVec = DP / 4;                            // threads of a row
   constexpr int kShares = kJoin / (kJoinRows * kVec);     // that add up different parts
   __shared__ float weight[kJoinRows][kParts];
   __shared__ float4 sums[kShares][kJoinRows][kVec];
   __shared__ float row_l[kJoinRows], row_top[kJoinRows];
-  wait_for_last_kernel();
   const AttendPart seg = P.part[blockIdx.x];
   if (seg.last < 0) return;
   const int D = P.c.head_dim, G = P.group, R = P.rows;
@@ -432,7 +433,7 @@ AttendPlan attend_plan(int head_dim, int max_rows) {
 template <typename T, int DP>
 int attend_join(const AttendParams &p, const AttendPlan &plan, int max_rows, void *stream) {
   const int rounds = (min(max_rows, plan.rows) + kJoinRows - 1) / kJoinRows;
-  return kv_launch("kv_attend_join", dim3(plan.grid, min(rounds, 8)), dim3(kJoin), 0, stream, kAfterLast,
+  return kv_launch("kv_attend_join", dim3(plan.grid, min(rounds, 8)), dim3(kJoin), 0, stream, 1,
                    attend_join_kernel<T, DP>, p);
 }
 

@@ -50,6 +50,7 @@ struct AttendTcParams : AttendParams {
 
 template <typename T, int DP>
 __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_constant__ AttendTcParams P) {
+  follow_last_kernel();
   constexpr uint32_t kTileBytes = kTile * DP * 2, kBlock = kTile * 128;
   extern __shared__ unsigned char smem_raw[];
   __shared__ TcShared<DP> sh;
@@ -77,7 +78,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     bar_init(smem_u32(&sh.idle), 1);
     for (int i = 0; i < 2; i++) {
       bar_init(smem_u32(&sh.s_full[i]), 2);
-      bar_init(smem_u32(&sh.p_full[i]), 128);
+      bar_init(smem_u32(&sh.p_full[i]), 4);  // warps
       bar_init(smem_u32(&sh.pv_done[i]), 2);
     }
     sh.dead = 0;
@@ -439,7 +440,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
         }
         tmem_wait_st();
         tmem_before_sync();
-        bar_arrive(smem_u32(&sh.p_full[q]));
+        __syncwarp();
+        if (lane == 0) bar_arrive(smem_u32(&sh.p_full[q]));
         s_no++;
       }
       if (!ok) {

@@ -18,6 +18,7 @@ struct CommitParams {
 // One CTA per session; a thread moves 16 bytes at a time.
 template <typename T>
 __global__ void __launch_bounds__(256) commit_kernel(const CommitParams P) {
+  follow_last_kernel();
   const int b = blockIdx.x, tid = threadIdx.x;
   const int H = P.c.n_heads, chunks = P.c.head_dim / 8;
   const KvRange tok = kv_tokens(P.t, b, P.c.status);
@@ -114,6 +115,7 @@ __device__ __forceinline__ int kept_count(const EvictParams &P, int b, int len) 
 // finds the same digit.  Then one pass in slot order ranks the slots that have
 // that very key, one counts and one writes the moves.
 __global__ void __launch_bounds__(kSelect) evict_select_kernel(const EvictParams P) {
+  follow_last_kernel();
   namespace cg = cooperative_groups;
   extern __shared__ uint32_t keys[];  // [hold]
   __shared__ __align__(16) uint32_t hist[2][kBins];
@@ -253,12 +255,12 @@ __global__ void __launch_bounds__(kSelect) evict_select_kernel(const EvictParams
 // moves at once, a lane each, and then copies them row by row.
 template <typename T>
 __global__ void __launch_bounds__(256) evict_move_kernel(const EvictParams P) {
+  follow_last_kernel();
   const int seg = blockIdx.x / P.per_seg, of_seg = blockIdx.x % P.per_seg, lane = threadIdx.x & 31;
   const int b = seg / P.c.n_heads, h = seg % P.c.n_heads;
   const int chunks = P.c.head_dim / 8;
   const int64_t room = (int64_t)P.c.max_pages * P.c.page_size;
   const int32_t *from = P.moves + seg * room, *into = from + room / 2;
-  wait_for_last_kernel();
   const int count = P.count[seg];
   const int warps = P.per_seg * (blockDim.x >> 5);
   const int width = 2 * chunks;
@@ -391,6 +393,6 @@ extern "C" int unison_kv_evict(const unison_kv_cache *cache, const unison_kv_cac
   const int64_t most = into ? min(room, (int64_t)into->max_pages * into->page_size) : room / 2;
   const int64_t fill = ((int64_t)kv_sm_count() * 32 + segs - 1) / (int64_t)segs;
   p.per_seg = (int)max((int64_t)1, min((most + 255) / 256, fill));
-  return kv_launch("kv_evict_move", dim3((unsigned)(segs * p.per_seg)), dim3(256), 0, cuda_stream, kAfterLast,
+  return kv_launch("kv_evict_move", dim3((unsigned)(segs * p.per_seg)), dim3(256), 0, cuda_stream, 1,
                    evict_move_kernel<uint16_t>, p);
 }

@@ -16,6 +16,7 @@ constexpr int kObserveSmem = kStages *kTile *DP * 2 + QR *DP * 2;
 // their weights without leaving its registers.
 template <typename T, int DP, int QR>
 __global__ void __launch_bounds__(kThreads) observe_kernel(const ObserveParams P) {
+  follow_last_kernel();
   constexpr int kChunks = DP / 8;
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ KvRunShared shared_run;

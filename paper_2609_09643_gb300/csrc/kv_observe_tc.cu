@@ -24,10 +24,10 @@ constexpr int kCopyWarp = 8, kIssueWarp = 12, kBoxWarp = 13;
 constexpr int kBuffers = 4, kMostSlots = 6;
 constexpr int kSetup = 2;  // tiles that a segment's beginning costs
 constexpr int kNodes = UNISON_KV_MAX_TOKENS;
-// Tiles whose keys' accounts are kept in shared memory: those on their way,
-// those in tensor memory, and the two that are being finished.
-constexpr int kMarks = 16;
-constexpr int kMarkBytes = kMarks * kTile * 12;
+// Tiles whose keys' accounts are kept in shared memory: those on their way, the
+// four that may be in tensor memory, and the one that is being looked up.
+constexpr int kMoreMarks = kBuffers + 1;
+constexpr int kMarkBytes = kTile * 12;
 
 struct ObserveShared {
   KvRunShared run;
@@ -51,6 +51,7 @@ struct ObserveTcParams : ObserveParams {
 
 template <typename T, int DP>
 __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_constant__ ObserveTcParams P) {
+  follow_last_kernel();
   constexpr uint32_t kTileBytes = kTile * DP * 2, kBlock = kTile * 128;
   extern __shared__ unsigned char smem_raw[];
   __shared__ ObserveShared sh;
@@ -62,7 +63,7 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
   float *const lse_base = reinterpret_cast<float *>(smem_raw + (slot_base - smem_u32(smem_raw)) + P.slots * kTileBytes);
 
   float **const marks_at = reinterpret_cast<float **>(lse_base + 2 * P.q_rows);  // where a key's weight goes
-  float *const marks_old = reinterpret_cast<float *>(marks_at + kMarks * kTile);  // what is there
+  float *const marks_old = reinterpret_cast<float *>(marks_at + (P.slots + kMoreMarks) * kTile);  // what is there
 
   // A tile's share of the run: its keys' way here, or the products and weights
   // of its chunks of 128 query rows, where those take longer.
@@ -83,15 +84,15 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
     }
     for (int i = 0; i < kBuffers; i++) {
       bar_init(smem_u32(&sh.t_full[i]), 2);
-      bar_init(smem_u32(&sh.t_free[i]), 128);
+      bar_init(smem_u32(&sh.t_free[i]), 4);  // warps
     }
     for (int i = 0; i < 2; i++) {
       bar_init(smem_u32(&sh.q_full[i]), 4);
       bar_init(smem_u32(&sh.q_free[i]), 1);
-      bar_init(smem_u32(&sh.seg_done[i]), 256);
+      bar_init(smem_u32(&sh.seg_done[i]), kCopyWarp);
     }
-    bar_init(smem_u32(&sh.part_full), 128);
-    bar_init(smem_u32(&sh.part_free), 128);
+    bar_init(smem_u32(&sh.part_full), 4);
+    bar_init(smem_u32(&sh.part_free), 4);
     bar_init(smem_u32(&sh.idle), 1);
     sh.dead = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -204,7 +205,7 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
         const uint32_t bar = smem_u32(&sh.k_full[s]);
         const bool fresh = kt == g.tiles - 1 && j < g.tok.count && P.s.mass_new;
         if (fresh) m = P.s.mass_new + (int64_t)(g.tok.first + j) * H + g.head;
-        const int mark = tile_no++ % kMarks * kTile + j;
+        const int mark = tile_no++ % (P.slots + kMoreMarks) * kTile + j;
         marks_at[mark] = m;
         marks_old[mark] = old;
         __syncwarp();
@@ -304,6 +305,10 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
     const int wg = warp >> 2, key = tid & 127;
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // this warp's quarter of the 128 lanes
     const float c = P.s.scale * 1.4426950408889634f;
+    auto warp_arrive = [&](uint64_t &bar) {
+      __syncwarp();
+      if (lane == 0) bar_arrive(smem_u32(&bar));
+    };
     int job = 0, seg_no = 0, tile_no = 0, shared_tiles = 0;
     bool ok = true;
     Segment g;
@@ -359,7 +364,7 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
             tmem_wait_ld();
           }
           // the others 16 at a time, each with the question whether it counts
-          int node = (i * 128 + r0) / G, head = (i * 128 + r0) % G;
+          int node = last ? (i * 128 + r0) / G : 0, head = i * 128 + r0 - node * G;
 #pragma unroll 1
           for (; r0 < n; r0 += 16) {
             uint32_t v[16], counts = n - r0 < 16 ? (1u << (n - r0)) - 1 : ~0u;
@@ -389,7 +394,7 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
             }
           }
           tmem_before_sync();
-          bar_arrive(smem_u32(&sh.t_free[buf]));
+          warp_arrive(sh.t_free[buf]);
         }
         if (!ok) break;
         float all, other;
@@ -399,24 +404,24 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
           if (wg == 1) {
             if (shared_tiles > 0) ok = bar_wait(smem_u32(&sh.part_free), (shared_tiles - 1) & 1, &sh.dead);
             if (ok) sh.part[key] = all;
-            bar_arrive(smem_u32(&sh.part_full));
+            warp_arrive(sh.part_full);
           } else {
             ok = bar_wait(smem_u32(&sh.part_full), shared_tiles & 1, &sh.dead);
             if (ok) all += sh.part[key];
-            bar_arrive(smem_u32(&sh.part_free));
+            warp_arrive(sh.part_free);
           }
           shared_tiles++;
           ok = __all_sync(~0u, ok);
           if (!ok) break;
         }
         if (writes) {
-          const int mark = tile_no % kMarks * kTile + key;
+          const int mark = tile_no % (P.slots + kMoreMarks) * kTile + key;
           float *to = marks_at[mark];
           if (to) *to = marks_old[mark] + all;
         }
       }
       if (!ok && key == 0 && P.c.status) P.c.status[g.b] = UNISON_ERR_TIMEOUT;
-      bar_arrive(smem_u32(&sh.seg_done[seg_no & 1]));
+      warp_arrive(sh.seg_done[seg_no & 1]);
       seg_no++;
     }
   }
@@ -434,14 +439,14 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
 template <typename T, int DP>
 int observe_tc(ObserveParams p, int max_rows, void *stream) {
   constexpr int kTileBytes = kTile * DP * 2;
-  constexpr int kMost = 226 << 10;
   static uint64_t done = 0;
   p.q_rows = (max_rows + 127) / 128 * 128;
   p.q_buffers = p.q_rows == 128 ? 2 : 1;  // few rows: the next segment's may come while the last one's are read
-  const int fixed = 1024 + p.q_rows * (p.q_buffers * DP * 2 + 8) + kMarkBytes + (int)sizeof(ObserveShared);
-  p.slots = min(kMostSlots, (kMost - fixed) / kTileBytes);
-  const int bytes = fixed - (int)sizeof(ObserveShared) + p.slots * kTileBytes;
-  if (!kv_allow_smem(reinterpret_cast<const void *>(observe_tc_kernel<T, DP>), kMost - (int)sizeof(ObserveShared), &done))
+  const int fixed = 1024 + p.q_rows * (p.q_buffers * DP * 2 + 8) + kMoreMarks * kMarkBytes;
+  const int most = (227 << 10) - (int)sizeof(ObserveShared) - 1024;
+  p.slots = min(kMostSlots, (most - fixed) / (kTileBytes + kMarkBytes));
+  const int bytes = fixed + p.slots * (kTileBytes + kMarkBytes);
+  if (!kv_allow_smem(reinterpret_cast<const void *>(observe_tc_kernel<T, DP>), most, &done))
     return UNISON_ERR_CUDA;
   ObserveTcParams q;
   static_cast<ObserveParams &>(q) = p;

@@ -52,6 +52,7 @@ __device__ __forceinline__ float residual(const Refused &r, float d, float y, in
 // kCertain: without q.
 template <typename T, bool kCertain>
 __global__ void __launch_bounds__(kThreads) verify_kernel(const unison_kv_tree t, const unison_kv_verify_args a) {
+  follow_last_kernel();
   namespace cg = cooperative_groups;
   __shared__ Refused refused;
   __shared__ int node_parent[UNISON_KV_MAX_TOKENS], node_token[UNISON_KV_MAX_TOKENS];

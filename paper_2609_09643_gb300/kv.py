@@ -117,7 +117,7 @@ class Cache:
         ptr = lambda x: None if x is None else x.data_ptr()  # noqa: E731
         self.tensors = (k, v, page_table, length, mass, pos, next_pos, status)  # kept while the pointers are used
         self.k, self.v, self.page_table, self.length, self.mass, self.pos, self.next_pos, self.status = self.tensors
-        self.dtype, self.device, self.n_seqs = k.dtype, k.device, n
+        self.dtype, self.device, self.n_seqs, self.on_gpu = k.dtype, k.device, n, k.is_cuda
         self.n_heads, self.head_dim = k.shape[1], k.shape[3]
         self.struct = KvCache(
             k.data_ptr(), v.data_ptr(), ptr(mass), ptr(pos), _dense(page_table, torch.int32, (n, pages), "page_table"),
@@ -126,7 +126,8 @@ class Cache:
             k.shape[2], k.shape[1], k.shape[3], DTYPE[k.dtype], 0)
         self.address = C.addressof(self.struct)
         self.scale = self.head_dim ** -0.5
-        self.scratch = {}  # bytes of workspace by the sizes that they depend on
+        self.sizes = {}    # bytes of workspace, by the call's sizes
+        self.scratch = {}  # workspaces, by stream
 
 
 class Tree:
@@ -183,6 +184,17 @@ def _queue(device, stream):
     return getattr(stream, "cuda_stream", stream)
 
 
+def _workspace(cache, n, handle):
+    """Scratch of n bytes, kept by the cache for each stream: its calls run in
+    order.  A captured call has scratch of its own, which the graph holds."""
+    if cache.on_gpu and torch._C._cuda_isCurrentStreamCapturing():
+        return torch.empty(n, dtype=torch.uint8, device=cache.device)
+    w = cache.scratch.get(handle)
+    if w is None or w.numel() < n:
+        w = cache.scratch[handle] = torch.empty(n, dtype=torch.uint8, device=cache.device)
+    return w
+
+
 def _on(stream, call, *args, **kw):
     """A call with a torch stream: what it allocates belongs to that stream."""
     with torch.cuda.stream(stream):
@@ -192,7 +204,7 @@ def _on(stream, call, *args, **kw):
 def attend(cache: Cache, tree: Tree, q, k_new, v_new, scale=None, out=None, lse=None, workspace=None, stream=None):
     """unison_kv_attend: (out [token, q head, head_dim], lse float32 [token, q
     head]).  scale defaults to head_dim ** -0.5; workspace: a uint8 tensor of
-    at least ``attend_workspace`` bytes, else one is allocated."""
+    at least ``attend_workspace`` bytes, else the cache keeps one."""
     if isinstance(stream, torch.cuda.Stream):
         return _on(stream, attend, cache, tree, q, k_new, v_new, scale, out, lse, workspace)
     n, heads = tree.n_tokens, q.shape[1]
@@ -207,13 +219,14 @@ def attend(cache: Cache, tree: Tree, q, k_new, v_new, scale=None, out=None, lse=
         lp = lse.data_ptr()
     else:
         lp = _dense(lse, torch.float32, (n, heads), "lse")
+    handle = _queue(cache.device, stream)
     if workspace is None:
-        workspace = torch.empty(attend_workspace(cache, tree, heads), dtype=torch.uint8, device=cache.device)
+        workspace = _workspace(cache, attend_workspace(cache, tree, heads), handle)
     rc = lib().unison_kv_attend(
         cache.address, tree.address,
         _STEP.pack(qp, kp, vp, op, lp, 0, qs[0], qs[1], ks[0], ks[1], vs[0], vs[1], os[0], os[1], heads,
                    cache.scale if scale is None else scale),
-        workspace.data_ptr(), workspace.numel(), _queue(cache.device, stream))
+        workspace.data_ptr(), workspace.numel(), handle)
     if rc:
         binding._check("unison_kv_attend", rc)
     return out, lse
@@ -222,9 +235,9 @@ def attend(cache: Cache, tree: Tree, q, k_new, v_new, scale=None, out=None, lse=
 def attend_workspace(cache: Cache, tree: Tree, n_q_heads: int) -> int:
     """Bytes of scratch that attend takes (a function of the sizes alone)."""
     key = tree.max_tokens, n_q_heads
-    n = cache.scratch.get(key)
+    n = cache.sizes.get(key)
     if n is None:
-        n = cache.scratch[key] = int(lib().unison_kv_attend_workspace(cache.address, tree.address, n_q_heads))
+        n = cache.sizes[key] = int(lib().unison_kv_attend_workspace(cache.address, tree.address, n_q_heads))
     return n
 
 
@@ -266,9 +279,9 @@ def commit(cache: Cache, tree: Tree, k_new, v_new, mass_new=None, path=None, n_p
 
 def evict_workspace(cache: Cache) -> int:
     """Bytes of scratch that evict takes (a function of the sizes alone)."""
-    n = cache.scratch.get("evict")
+    n = cache.sizes.get("evict")
     if n is None:
-        n = cache.scratch["evict"] = int(lib().unison_kv_evict_workspace(cache.address))
+        n = cache.sizes["evict"] = int(lib().unison_kv_evict_workspace(cache.address))
     return n
 
 
@@ -277,11 +290,12 @@ def evict(cache: Cache, keep, sink=0, recent=0, into: Cache | None = None, works
     stay, in place or, with ``into``, in another cache."""
     if isinstance(stream, torch.cuda.Stream):
         return _on(stream, evict, cache, keep, sink, recent, into, workspace)
+    handle = _queue(cache.device, stream)
     if workspace is None:
-        workspace = torch.empty(evict_workspace(cache), dtype=torch.uint8, device=cache.device)
+        workspace = _workspace(cache, evict_workspace(cache), handle)
     rc = lib().unison_kv_evict(
         cache.address, None if into is None else into.address, _dense(keep, torch.int32, (cache.n_seqs,), "keep"), sink,
-        recent, workspace.data_ptr(), workspace.numel(), _queue(cache.device, stream))
+        recent, workspace.data_ptr(), workspace.numel(), handle)
     if rc:
         binding._check("unison_kv_evict", rc)
 
