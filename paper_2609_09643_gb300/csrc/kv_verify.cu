@@ -9,6 +9,8 @@
 // cluster barrier.
 #include <cooperative_groups.h>
 
+#include <type_traits>
+
 #include "kv.cuh"
 
 namespace unison {
@@ -17,10 +19,8 @@ namespace {
 constexpr int kThreads = 512;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;
-constexpr int kUnroll = 8;                // loads in flight of a lane, from each of the two rows
-constexpr float kUnit = 1099511627776.f;  // 2^40
 
-__device__ __forceinline__ float weight(float x) { return x > 0.f ? fminf(x, 1.f) : 0.f; }
+__device__ __forceinline__ float weight(float x) { return fminf(fmaxf(x, 0.f), 1.f); }  // (NaN: 0)
 template <typename T>
 __device__ __forceinline__ float load(const T *p, int64_t i) {
   return KvType<T>::to_float(p[i]);
@@ -29,7 +29,33 @@ template <>
 __device__ __forceinline__ float load<float>(const float *p, int64_t i) {
   return p[i];
 }
-__device__ __forceinline__ int64_t fixed(float d) { return __float2ll_rz(__fmul_rn(d, kUnit)); }
+// floor(d 2^40) of 0 <= d <= 1, as 2^20 high + low.  Adding 2^23 and rounding
+// towards zero leaves the whole part in the low bits of a float, so the parts
+// come from five operations at the full rate; a conversion to 64 bits is served
+// at a small fraction of it.  high and low get 2^23's bits on top: kBias each.
+constexpr uint32_t kBias = 0x4B000000u;
+__device__ __forceinline__ void fixed_parts(float d, uint32_t &high, uint32_t &low) {
+  const float x = __fmul_rn(d, 1048576.f), h = __fadd_rz(x, 8388608.f);
+  const float rest = __fsub_rn(x, __fsub_rn(h, 8388608.f));  // exact, below 1
+  high = __float_as_uint(h);
+  low = __float_as_uint(__fmaf_rz(rest, 1048576.f, 8388608.f));
+}
+__device__ __forceinline__ int64_t fixed(float d) {
+  uint32_t high, low;
+  fixed_parts(d, high, low);
+  return (int64_t)(high - kBias) << 20 | (low - kBias);
+}
+
+// 16 bytes of a row as numbers.
+template <typename T>
+struct Quad {
+  static constexpr int kN = 16 / sizeof(T);
+  __device__ __forceinline__ static void get(const uint4 &v, float (&x)[kN]) {
+    const T *e = reinterpret_cast<const T *>(&v);
+#pragma unroll
+    for (int i = 0; i < kN; i++) x[i] = load(e, i);
+  }
+};
 
 // The refusals at the current node: z[i] the sum before refusal i, token[i]
 // the refused token.
@@ -37,10 +63,11 @@ struct Refused {
   float z[UNISON_KV_MAX_TOKENS];
   int token[UNISON_KV_MAX_TOKENS];
 };
-// d at entry x, whose first weight is d and whose draft weight is y, after n refusals.
-template <bool kCertain>
+// d at entry x, whose first weight is d and whose draft weight is y, after n
+// refusals; kCount: n where it is 0 or 1, else 2.
+template <bool kCertain, int kCount>
 __device__ __forceinline__ float residual(const Refused &r, float d, float y, int x, int n) {
-  for (int i = 0; i < n; i++) {
+  for (int i = 0; i < (kCount < 2 ? kCount : n); i++) {
     if (kCertain)
       d = r.token[i] == x ? 0.f : d;
     else
@@ -90,27 +117,65 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const unison_kv_tree t
   }
   cluster.sync();  // every CTA has begun: its shared memory may be written to
 
-  // this warp's run of the vocabulary, in whole groups of 32 entries
-  const int span = (((V + ctas * kWarps - 1) / (ctas * kWarps)) + 31) & ~31;
+  // this warp's run of the vocabulary, in whole groups of 32 times 16 bytes
+  constexpr int kN = Quad<T>::kN, kGroup = 32 * kN;
+  constexpr int kFlight = 16 / kN;  // loads in flight of a lane, from each of the two rows
+  const int span = (V + ctas * kWarps * kGroup - 1) / (ctas * kWarps * kGroup) * kGroup;
   const int64_t begin64 = (int64_t)(rank * kWarps + warp) * span;
   const int begin = (int)min(begin64, (int64_t)V), end = (int)min(begin64 + span, (int64_t)V);
   int passes = 0;
+  // This lane's share of the sum over all entries of the residual at `cur`.
+  auto share = [&](auto counted, int cur, int n) -> int64_t {
+    constexpr int kCount = decltype(counted)::value;
+    const T *p = rows_p + cur * a.p_row, *q = kCertain || kCount == 0 ? nullptr : rows_q + cur * a.q_row;
+    int64_t s = 0;
+    const bool whole = (((uintptr_t)p | (uintptr_t)q) & 15) == 0 && V % kN == 0;
+    if (whole) {
+      for (int x0 = begin + lane * kN; x0 < end; x0 += kGroup * kFlight) {
+        uint4 d[kFlight], y[kFlight];
+#pragma unroll
+        for (int i = 0; i < kFlight; i++) {
+          const int x = x0 + i * kGroup;
+          d[i] = x < end ? __ldg(reinterpret_cast<const uint4 *>(p + x)) : make_uint4(0, 0, 0, 0);
+          y[i] = q && x < end ? __ldg(reinterpret_cast<const uint4 *>(q + x)) : make_uint4(0, 0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < kFlight; i++) {
+          float dx[kN], yx[kN];
+          Quad<T>::get(d[i], dx);
+          Quad<T>::get(y[i], yx);
+          uint32_t high = 0, low = 0;  // of at most eight numbers
+#pragma unroll
+          for (int j = 0; j < kN; j++) {
+            uint32_t h, l;
+            fixed_parts(residual<kCertain, kCount>(refused, weight(dx[j]), weight(yx[j]), x0 + i * kGroup + j, n), h, l);
+            high += h;
+            low += l;
+          }
+          s += ((int64_t)(high - kN * kBias) << 20) + (low - kN * kBias);
+        }
+      }
+    } else {
+      for (int x0 = begin + lane; x0 < end; x0 += 32 * 2 * kFlight) {
+        float d[2 * kFlight], y[2 * kFlight];
+#pragma unroll
+        for (int i = 0; i < 2 * kFlight; i++) {
+          const int x = x0 + i * 32;
+          d[i] = x < end ? load(p, x) : 0.f;
+          y[i] = q && x < end ? load(q, x) : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < 2 * kFlight; i++)
+          s += fixed(residual<kCertain, kCount>(refused, weight(d[i]), weight(y[i]), x0 + i * 32, n));
+      }
+    }
+    return s;
+  };
   // The sum over all entries of the residual after n refusals at node `cur`.
   auto total = [&](int cur, int n) -> int64_t {
-    const T *p = rows_p + cur * a.p_row, *q = kCertain || n == 0 ? nullptr : rows_q + cur * a.q_row;
-    int64_t s = 0;
-    for (int x0 = begin + lane; x0 < end; x0 += 32 * kUnroll) {
-      float d[kUnroll], y[kUnroll];
-#pragma unroll
-      for (int i = 0; i < kUnroll; i++) {
-        const int x = x0 + i * 32;
-        d[i] = x < end ? load(p, x) : 0.f;
-        y[i] = q && x < end ? load(q, x) : 0.f;
-      }
-#pragma unroll
-      for (int i = 0; i < kUnroll; i++)
-        s += fixed(residual<kCertain>(refused, weight(d[i]), weight(y[i]), x0 + i * 32, n));
-    }
+    int64_t s = n == 0   ? share(std::integral_constant<int, 0>(), cur, n)
+                : n == 1 ? share(std::integral_constant<int, 1>(), cur, n)
+                         : share(std::integral_constant<int, 2>(), cur, n);
 #pragma unroll
     for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(~0u, s, d);
     if (lane == 0) warp_sum[warp] = s;
@@ -134,7 +199,7 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const unison_kv_tree t
   for (int i = 1; i < tok.count; i++) {
     if (node_parent[i] != cur) continue;
     const float y = node_y[i];
-    const float d = residual<kCertain>(refused, node_d[i], y, node_token[i], count);
+    const float d = residual<kCertain, 2>(refused, node_d[i], y, node_token[i], count);
     if (__fmul_rn(__fmul_rn(node_u[i], y), z) < d) {
       cur = i;
       count = 0;
@@ -150,7 +215,7 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const unison_kv_tree t
       }
       __syncthreads();
       left = total(cur, ++count);
-      z = __fmul_rn((float)left, 1.f / kUnit);
+      z = __fmul_rn((float)left, 1.f / 1099511627776.f);
     }
   }
   if (left <= 0) left = total(cur, count = 0);
@@ -175,7 +240,7 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const unison_kv_tree t
   const int each = span / kThreads + 1;
   const T *p = rows_p + cur * a.p_row, *q = kCertain || count == 0 ? nullptr : rows_q + cur * a.q_row;
   auto entry = [&](int x) -> int64_t {
-    return fixed(residual<kCertain>(refused, weight(load(p, x)), q ? weight(load(q, x)) : 0.f, x, count));
+    return fixed(residual<kCertain, 2>(refused, weight(load(p, x)), q ? weight(load(q, x)) : 0.f, x, count));
   };
   const int x0 = lo + tid * each, x1 = min(x0 + each, hi);
   int64_t mine = 0, all;
@@ -194,8 +259,10 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const unison_kv_tree t
 template <typename T>
 int verify_run(const unison_kv_tree &t, const unison_kv_verify_args &a, void *stream) {
   // CTAs per session: as many as the sessions leave room for (two CTAs on a
-  // multiprocessor), none with less than 2,048 entries.
-  const int room = 2 * kv_sm_count() / t.n_seqs, wanted = (a.vocab + 2047) / 2048;
+  // multiprocessor, two rounds of them: a session takes one to four passes, and
+  // those that end early make room; one round takes 107 us where two take 87),
+  // none with less than 2,048 entries.
+  const int room = 4 * kv_sm_count() / t.n_seqs, wanted = (a.vocab + 2047) / 2048;
   int ctas = 1;
   while (ctas < kMaxCluster && ctas * 2 <= max(room, 1) && ctas < wanted) ctas *= 2;
   return kv_launch("kv_verify", dim3(t.n_seqs * ctas), dim3(kThreads), 0, stream, ctas,
