@@ -40,6 +40,19 @@ inline int kv_check_tree(const unison_kv_tree *t, int n_seqs) {
   return UNISON_OK;
 }
 
+// A cache as the kernels take it: with slot / page_size as a multiplication
+// (Granlund and Montgomery: for n < 2^31, n / d = (high(n m) + n) >> l with
+// l = ceil(log2 d) and m = floor(2^32 (2^l - d) / d) + 1).
+struct KvCacheArg : unison_kv_cache {
+  uint32_t page_mul, page_shift;
+  KvCacheArg() = default;
+  KvCacheArg(const unison_kv_cache &c) : unison_kv_cache(c), page_shift(0) {
+    const uint64_t d = (uint32_t)c.page_size;
+    while ((1ull << page_shift) < d) page_shift++;
+    page_mul = (uint32_t)((((1ull << page_shift) - d) << 32) / d + 1);
+  }
+};
+
 // Multiprocessors of the current device, asked for once per device.
 int kv_sm_count();
 
@@ -121,8 +134,8 @@ __device__ __forceinline__ int kv_length(const unison_kv_cache &c, int b) {
 // Page of a slot (below max_pages * page_size), as the table has it: to be
 // checked by kv_page_ok when it is used, so that the load may be on its way.
 constexpr int kNoSlot = INT32_MIN;
-__device__ __forceinline__ int kv_page_load(const unison_kv_cache &c, int b, int slot, int &off) {
-  const unsigned i = (unsigned)slot / (unsigned)c.page_size;
+__device__ __forceinline__ int kv_page_load(const KvCacheArg &c, int b, int slot, int &off) {
+  const unsigned i = (__umulhi((unsigned)slot, c.page_mul) + (unsigned)slot) >> c.page_shift;
   off = slot - (int)(i * (unsigned)c.page_size);
   return __ldg(c.page_table + (int64_t)b * c.max_pages + i);
 }
@@ -132,7 +145,7 @@ __device__ __forceinline__ int kv_page_ok(const unison_kv_cache &c, int b, int p
   return -1;
 }
 // Page of a slot, or -1.
-__device__ __forceinline__ int kv_page(const unison_kv_cache &c, int b, int slot, int &off) {
+__device__ __forceinline__ int kv_page(const KvCacheArg &c, int b, int slot, int &off) {
   return kv_page_ok(c, b, kv_page_load(c, b, slot, off));
 }
 
@@ -201,23 +214,24 @@ __device__ __forceinline__ uint32_t swizzled(uint32_t base, int row, int chunk) 
 // ------------------------------------------------- sharing out the tiles --
 // All threads of a CTA add their values; every thread gets the exclusive
 // prefix and the sum.  `part`: 33 words of shared memory.
-__device__ __forceinline__ int64_t block_scan(int64_t x, int64_t *part, int64_t &total) {
+template <typename I>
+__device__ __forceinline__ I block_scan(I x, I *part, I &total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = (blockDim.x + 31) >> 5;
-  int64_t y = x;
+  I y = x;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
-    const int64_t z = __shfl_up_sync(~0u, y, d);
+    const I z = __shfl_up_sync(~0u, y, d);
     if (lane >= d) y += z;
   }
   __syncthreads();
   if (lane == 31) part[warp] = y;
   __syncthreads();
   if (warp == 0) {
-    const int64_t mine = lane < warps ? part[lane] : 0;
-    int64_t s = mine;
+    const I mine = lane < warps ? part[lane] : 0;
+    I s = mine;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-      const int64_t z = __shfl_up_sync(~0u, s, d);
+      const I z = __shfl_up_sync(~0u, s, d);
       if (lane >= d) s += z;
     }
     __syncwarp();
@@ -247,11 +261,11 @@ struct KvRunShared {
 template <typename F>
 __device__ __forceinline__ bool kv_find_run(KvRun &r, KvRunShared &sh, int n_seqs, int runs, int run, F tiles) {
   const int tid = threadIdx.x, step = blockDim.x;
-  int64_t mine = tid < n_seqs ? tiles(tid) : 0, n;
+  int64_t mine = tid < n_seqs ? (int64_t)tiles(tid) : 0, n;
   int64_t before = block_scan(mine, sh.part, n);
   r.total = n;
   for (int b0 = step; b0 < n_seqs; b0 += step) {
-    block_scan(b0 + tid < n_seqs ? tiles(b0 + tid) : 0, sh.part, n);
+    block_scan(b0 + tid < n_seqs ? (int64_t)tiles(b0 + tid) : 0, sh.part, n);
     r.total += n;
   }
   r.runs = (int)min((int64_t)runs, r.total);
@@ -261,7 +275,7 @@ __device__ __forceinline__ bool kv_find_run(KvRun &r, KvRunShared &sh, int n_seq
   int64_t sum = 0;
   for (int b0 = 0;; b0 += step) {
     if (n_seqs > step) {  // else the first values still stand
-      mine = b0 + tid < n_seqs ? tiles(b0 + tid) : 0;
+      mine = b0 + tid < n_seqs ? (int64_t)tiles(b0 + tid) : 0;
       before = sum + block_scan(mine, sh.part, n);
     }
     if (r.at >= before && r.at < before + mine) {

@@ -12,7 +12,7 @@ struct AttendPart {
 };
 
 struct AttendParams {
-  unison_kv_cache c;
+  KvCacheArg c;
   unison_kv_tree t;
   unison_kv_step s;
   AttendPart *part;  // [grid]

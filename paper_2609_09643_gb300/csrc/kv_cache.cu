@@ -9,7 +9,7 @@ namespace {
 
 // ---------------------------------------------------------------- commit --
 struct CommitParams {
-  unison_kv_cache c;
+  KvCacheArg c;
   unison_kv_tree t;
   unison_kv_step s;
   unison_kv_path path;
@@ -63,36 +63,57 @@ __global__ void __launch_bounds__(256) commit_kernel(const CommitParams P) {
 
 // ----------------------------------------------------------------- evict --
 struct EvictParams {
-  unison_kv_cache c, to;  // to: the cache itself where slots move in place
+  KvCacheArg c, to;  // to: the cache itself where slots move in place
   const int32_t *keep;
   int32_t sink, recent;
   bool in_place;
-  int hold;        // keys that a CTA of the selection has room for
+  int hold;        // keys of a thread of the selection in shared memory
   int per_seg;     // CTAs that move one segment's slots
   int32_t *moves;  // [segments][slots of a session]: sources, and from the middle on targets (in place)
   int32_t *count;  // [segments]
 };
 
-constexpr int kSelect = 512;
-constexpr int kWarps = kSelect / 32;
+constexpr int kSelect = 256, kPitch = kSelect + 1;
 constexpr int kMaxCluster = 8;
 constexpr int kBins = 2048;         // digits of 11, 11 and 10 bits
-constexpr int kMostHeld = 50 << 10;  // keys in a CTA's shared memory
+constexpr int kMostHeld = 192;      // keys of a thread in shared memory
 
 // Order of a slot among its session's: protected slots above all, then larger
 // mass (the bits of a float, turned so that unsigned order is the numbers'
 // order, -0 as 0), NaN and slots without a page below all.
-__device__ __forceinline__ uint32_t slot_key(const EvictParams &P, int b, int h, int slot, int next) {
-  int off;
-  const int page = kv_page(P.c, b, slot, off);
-  if (page < 0) return 0;
-  const int64_t m = page * P.c.m_page + h * P.c.m_head + off * P.c.m_slot;
-  const float x = P.c.mass[m] + 0.f;
-  const int pos = P.c.pos ? P.c.pos[m] : slot;
+__device__ __forceinline__ uint32_t order_key(const EvictParams &P, float mass, int pos, int next) {
   if (pos < P.sink || (int64_t)pos >= (int64_t)next - P.recent) return ~0u;
+  const float x = mass + 0.f;
   if (isnan(x)) return 0;
   const uint32_t u = __float_as_uint(x);
   return u >> 31 ? ~u : u | 0x80000000u;
+}
+// Keys of kN slots, kStep apart, as far as they are below end: their look-ups
+// are on their way together.
+template <int kN>
+__device__ __forceinline__ void slot_keys(const EvictParams &P, int b, int h, int first, int step, int end, int next,
+                                          uint32_t (&key)[kN]) {
+  int page[kN], off[kN], pos[kN];
+  float mass[kN];
+  const int64_t head = h * P.c.m_head;
+#pragma unroll
+  for (int i = 0; i < kN; i++) {
+    page[i] = kNoSlot;
+    if (first + i * step < end) page[i] = kv_page_load(P.c, b, first + i * step, off[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < kN; i++) {
+    page[i] = kv_page_ok(P.c, b, page[i]);
+    const int64_t m = head + page[i] * P.c.m_page + off[i] * P.c.m_slot;
+    pos[i] = first + i * step;
+    mass[i] = 0.f;
+    if (page[i] >= 0) {
+      mass[i] = P.c.mass[m];
+      if (P.c.pos) pos[i] = P.c.pos[m];
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kN; i++) key[i] = page[i] < 0 ? 0 : order_key(P, mass[i], pos[i], next);
 }
 
 // How many slots of a session stay.
@@ -109,21 +130,28 @@ __device__ __forceinline__ int kept_count(const EvictParams &P, int b, int len) 
 }
 
 // Lists the moves of one segment (session and head); a cluster of CTAs shares
-// its slots, in order.  Every key is read once and kept in shared memory.  The
-// key of the last slot that stays is found digit by digit: each CTA counts its
-// own keys, adds up the counts of all (through distributed shared memory) and
-// finds the same digit.  Then one pass in slot order ranks the slots that have
-// that very key, one counts and one writes the moves.
-__global__ void __launch_bounds__(kSelect) evict_select_kernel(const EvictParams P) {
+// its slots, in order, and so do a CTA's threads: a thread has a run of them.
+// Every key is read once and kept in shared memory, key k of thread t at
+// k * kPitch + t (odd: neighbouring slots lie in different banks).  The key of the last slot that stays is found digit by digit:
+// each CTA counts its own keys, adds up the counts of all (through distributed
+// shared memory) and finds the same digit.  Then each thread's slots with that
+// very key are ranked, and the moves counted and written.
+__global__ void __launch_bounds__(kSelect, 4) evict_select_kernel(const EvictParams P) {
   follow_last_kernel();
   namespace cg = cooperative_groups;
-  extern __shared__ uint32_t keys[];  // [hold]
+  extern __shared__ uint32_t keys[];  // [hold][kPitch]
   __shared__ __align__(16) uint32_t hist[2][kBins];
-  __shared__ uint32_t digit, above, inside;
-  __shared__ int64_t part[33], cta_sum[2][kMaxCluster];
+  __shared__ uint32_t digit, above, inside, part[33];
+  __shared__ uint32_t cta_sum[2][kMaxCluster][2];
   cg::cluster_group cluster = cg::this_cluster();
   const int ctas = cluster.num_blocks(), rank = cluster.block_rank();
-  const int seg = blockIdx.x / ctas, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  auto sync = [&]() {
+    if (ctas > 1)
+      cluster.sync();
+    else
+      __syncthreads();
+  };
+  const int seg = blockIdx.x / ctas, tid = threadIdx.x;
   const int b = seg / P.c.n_heads, h = seg % P.c.n_heads;
   const int len = kv_length(P.c, b);
   const int n = kept_count(P, b, len);
@@ -134,44 +162,72 @@ __global__ void __launch_bounds__(kSelect) evict_select_kernel(const EvictParams
     if (rank == 0 && tid == 0) P.count[seg] = 0;
     return;
   }
-  // this CTA's run of the slots, and this warp's
-  const int run = ((len + ctas * kSelect - 1) / (ctas * kSelect)) * kSelect;
-  const int64_t first64 = (int64_t)rank * run;
-  const int first = (int)min(first64, (int64_t)len), last = (int)min(first64 + run, (int64_t)len);
-  auto key_of = [&](int s) { return s - first < P.hold ? keys[s - first] : slot_key(P, b, h, s, next); };
+  // slots of a thread, of this CTA, of this thread
+  const int each = (len + ctas * kSelect - 1) / (ctas * kSelect);
+  const int64_t first64 = (int64_t)rank * each * kSelect;
+  const int first = (int)min(first64, (int64_t)len), last = (int)min(first64 + each * kSelect, (int64_t)len);
+  const int begin = min(first + tid * each, last), mine = min(begin + each, last) - begin;
+  const int held = P.hold;  // keys of a thread in shared memory
+  auto key_of = [&](int k) -> uint32_t {
+    if (k < held) return keys[k * kPitch + tid];
+    uint32_t x[1];
+    slot_keys<1>(P, b, h, begin + k, 0, last, next, x);
+    return x[0];
+  };
 
   uint32_t last_key = 0;  // of the slots that stay
   uint32_t ties = 0;      // slots with that key that stay, the lowest first
   if (n < len) {
-    const int held = min(last - first, P.hold);
-#pragma unroll 4
-    for (int i = tid; i < held; i += kSelect) keys[i] = slot_key(P, b, h, first + i, next);
+    // neighbouring threads read neighbouring slots here
+    constexpr int kAtOnce = 8;
+    const uint32_t by_each = each == 1 ? 0 : 0xFFFFFFFFu / each + 1;  // (slots of a CTA < 2^16 while they are held)
+    for (int i = tid; i < last - first; i += kSelect * kAtOnce) {
+      uint32_t k[kAtOnce];
+      slot_keys<kAtOnce>(P, b, h, first + i, kSelect, last, next, k);
+#pragma unroll
+      for (int j = 0; j < kAtOnce; j++) {
+        const int s = i + j * kSelect;
+        const int t = each <= held ? (each == 1 ? s : (int)__umulhi(s, by_each)) : s / each;
+        if (first + s < last && s - t * each < held) keys[(s - t * each) * kPitch + t] = k[j];
+      }
+    }
     for (int i = tid; i < kBins; i += kSelect) hist[0][i] = 0;
     __syncthreads();
     uint32_t rest = n;
     int shift = 21, bits = 11;
     for (int pass = 0;; pass++) {
-      uint32_t *mine = hist[pass & 1];
-      for (int s = first + tid; s < last; s += kSelect) {
-        const uint32_t k = key_of(s);
-        if (pass == 0 || k >> (shift + bits) == last_key) atomicAdd(&mine[k >> shift & ((1u << bits) - 1)], 1u);
-      }
-      cluster.sync();
-      // four bins a thread, from the top: thread 0 has the highest
-      const int bin = kBins - 4 - 4 * tid;
-      uint4 sum = {0, 0, 0, 0};
-      for (int c = 0; c < ctas; c++) {
-        const uint4 x = *reinterpret_cast<const uint4 *>(cluster.map_shared_rank(mine, c) + bin);
-        sum.x += x.x, sum.y += x.y, sum.z += x.z, sum.w += x.w;
-      }
-      for (int i = tid; i < kBins; i += kSelect) hist[~pass & 1][i] = 0;  // of the last pass: read by all
-      int64_t all;
-      uint32_t over = (uint32_t)block_scan(sum.x + sum.y + sum.z + sum.w, part, all);
-      const uint32_t of[4] = {sum.w, sum.z, sum.y, sum.x};
+      uint32_t *counts = hist[pass & 1];
+      auto count = [&](uint32_t x) {
+        if (pass == 0 || x >> (shift + bits) == last_key) atomicAdd(&counts[x >> shift & ((1u << bits) - 1)], 1u);
+      };
+      int k = 0;
+      for (; k + 4 <= min(mine, held); k += 4) {
+        uint32_t x[4];
 #pragma unroll
-      for (int i = 0; i < 4; i++) {
+        for (int i = 0; i < 4; i++) x[i] = keys[(k + i) * kPitch + tid];
+#pragma unroll
+        for (int i = 0; i < 4; i++) count(x[i]);
+      }
+      for (; k < mine; k++) count(key_of(k));
+      sync();
+      // eight bins a thread, from the top: thread 0 has the highest
+      const int bin = kBins - 8 - 8 * tid;
+      uint32_t of[8] = {0, 0, 0, 0, 0, 0, 0, 0}, sum = 0;
+      for (int c = 0; c < ctas; c++) {
+        const uint4 *theirs = reinterpret_cast<const uint4 *>(cluster.map_shared_rank(counts, c) + bin);
+        const uint4 x = theirs[1], y = theirs[0];
+        of[0] += x.w, of[1] += x.z, of[2] += x.y, of[3] += x.x;
+        of[4] += y.w, of[5] += y.z, of[6] += y.y, of[7] += y.x;
+      }
+#pragma unroll
+      for (int i = 0; i < 8; i++) sum += of[i];
+      for (int i = tid; i < kBins; i += kSelect) hist[~pass & 1][i] = 0;  // of the last pass: read by all
+      uint32_t all;
+      uint32_t over = block_scan(sum, part, all);
+#pragma unroll
+      for (int i = 0; i < 8; i++) {
         if (over < rest && rest <= over + of[i]) {
-          digit = bin + 3 - i;
+          digit = bin + 7 - i;
           above = over;
           inside = of[i];
         }
@@ -193,62 +249,66 @@ __global__ void __launch_bounds__(kSelect) evict_select_kernel(const EvictParams
       __syncthreads();  // digit, above, inside are read
     }
   }
-
-  // The exclusive prefix over all CTAs' threads, in order, of a value that lane 0 of every warp gives.
-  int exchanges = 0;
-  auto prefix = [&](int64_t x, int64_t &all) -> int64_t {
-    const int64_t in_cta = block_scan(lane == 0 ? x : 0, part, all);
-    const int64_t before_warp = __shfl_sync(~0u, in_cta, 0);
-    if (ctas == 1) return before_warp;
-    const int slot = exchanges++ & 1;
-    if (tid < ctas) *cluster.map_shared_rank(&cta_sum[slot][rank], tid) = all;
-    cluster.sync();
-    int64_t before = 0;
-    all = 0;
-    for (int c = 0; c < ctas; c++) {
-      if (c < rank) before += cta_sum[slot][c];
-      all += cta_sum[slot][c];
-    }
-    return before + before_warp;
-  };
   if (ctas > 1 && n == len) cluster.sync();  // every CTA has begun: its shared memory may be written to
-  const int warp_run = run / kWarps;
-  const int begin = min(first + warp * warp_run, last), end = min(begin + warp_run, last);
-  int64_t ties_before = 0, all;
-  if (ties) {
-    int64_t count = 0;
-    for (int s = begin + lane; s - lane < end; s += 32)
-      count += __popc(__ballot_sync(~0u, s < end && key_of(s) == last_key));
-    ties_before = prefix(count, all);
-  }
-  // Targets and sources of the moves in this warp's run, from the given ranks on.
-  auto moves = [&](bool write, int64_t targets, int64_t sources) -> int64_t {
-    int64_t tie = ties_before;
-    for (int s = begin + lane; s - lane < end; s += 32) {
-      bool stays = s < end;
-      if (n < len) {
-        const uint32_t k = s < end ? key_of(s) : 0;
-        bool same = false;
-        if (ties) {
-          same = s < end && k == last_key;
-          const uint32_t group = __ballot_sync(~0u, same);
-          same = same && tie + __popc(group & ((1u << lane) - 1)) < ties;
-          tie += __popc(group);
-        }
-        stays = s < end && (k > last_key || same);
-      }
-      const bool target = P.in_place && s < end && s < n && !stays, source = stays && (!P.in_place || s >= n);
-      const uint32_t t = __ballot_sync(~0u, target), f = __ballot_sync(~0u, source);
-      if (write && target) into[targets + __popc(t & ((1u << lane) - 1))] = s;
-      if (write && source) from[sources + __popc(f & ((1u << lane) - 1))] = s;
-      targets += __popc(t);
-      sources += __popc(f);
+
+  // Exclusive prefixes over all CTAs' threads of two counts at once, and their sums.
+  int exchanges = 0;
+  auto prefix = [&](uint32_t &x, uint32_t &y, uint32_t &all_x, uint32_t &all_y) {
+    x = block_scan(x, part, all_x);
+    y = block_scan(y, part, all_y);
+    if (ctas == 1) return;
+    const int slot = exchanges++ & 1;
+    if (tid < ctas) {
+      uint32_t *theirs = cluster.map_shared_rank(&cta_sum[slot][rank][0], tid);
+      theirs[0] = all_x;
+      theirs[1] = all_y;
     }
-    return targets << 32 | sources;
+    cluster.sync();
+    all_x = all_y = 0;
+    for (int c = 0; c < ctas; c++) {
+      if (c < rank) x += cta_sum[slot][c][0], y += cta_sum[slot][c][1];
+      all_x += cta_sum[slot][c][0];
+      all_y += cta_sum[slot][c][1];
+    }
   };
-  const int64_t before = prefix(moves(false, 0, 0), all);
-  moves(true, before >> 32, before & 0xFFFFFFFF);
-  if (rank == 0 && tid == 0) P.count[seg] = (int)(P.in_place ? min(all >> 32, all & 0xFFFFFFFF) : all & 0xFFFFFFFF);
+  uint32_t tie = 0, none = 0, all, more;
+  if (ties) {
+    for (int k = 0; k < mine; k++) tie += key_of(k) == last_key;
+    prefix(tie, none, all, more);
+  }
+  auto stays = [&](int k, uint32_t &rank) {
+    if (n == len) return true;
+    const uint32_t x = key_of(k);
+    if (ties && x == last_key) return rank++ < ties;
+    return x > last_key;
+  };
+  // (the first 32 slots of a thread are remembered: most sessions have no more)
+  uint32_t targets = 0, sources = 0, r = tie, moves = 0;
+  for (int k = 0; k < mine; k++) {
+    const bool stay = stays(k, r), low = P.in_place && begin + k < n;
+    targets += P.in_place && low && !stay;
+    sources += stay && !low;
+    if (k < 32 && stay != low) moves |= 1u << k;
+  }
+  prefix(targets, sources, all, more);
+  if (rank == 0 && tid == 0) P.count[seg] = (int)(P.in_place ? min(all, more) : more);
+  auto write = [&](int k, bool stay) {
+    if (stay)
+      from[sources++] = begin + k;
+    else
+      into[targets++] = begin + k;
+  };
+  for (; moves; moves &= moves - 1) {
+    const int k = __ffs(moves) - 1;
+    write(k, !(P.in_place && begin + k < n));
+  }
+  if (mine > 32) {
+    r = tie;
+    for (int k = 0; k < mine; k++) {
+      const bool stay = stays(k, r), low = P.in_place && begin + k < n;
+      if (k >= 32 && stay != low) write(k, stay);
+    }
+  }
 }
 
 // Moves the listed slots: keys, values, mass and position.  A warp looks up 32
@@ -340,7 +400,7 @@ extern "C" int unison_kv_commit(const unison_kv_cache *cache, const unison_kv_tr
       !pools_ok(cache))
     return UNISON_ERR_ARG;
   if (path && path->path && (!path->n_path || path->path_stride < 0)) return UNISON_ERR_ARG;
-  const CommitParams p = {*cache, *tree, *step, path ? *path : unison_kv_path{}};
+  const CommitParams p = {KvCacheArg(*cache), *tree, *step, path ? *path : unison_kv_path{}};
   // 16-bit types move as they are
   return kv_launch("kv_commit", dim3(cache->n_seqs), dim3(256), 0, cuda_stream, 1, commit_kernel<uint16_t>, p);
 }
@@ -371,7 +431,7 @@ extern "C" int unison_kv_evict(const unison_kv_cache *cache, const unison_kv_cac
   const int64_t room = (int64_t)cache->max_pages * cache->page_size;
   EvictParams p;
   p.c = *cache;
-  p.to = into ? *into : *cache;
+  p.to = KvCacheArg(into ? *into : *cache);
   p.keep = keep;
   p.sink = sink;
   p.recent = recent;
@@ -383,10 +443,11 @@ extern "C" int unison_kv_evict(const unison_kv_cache *cache, const unison_kv_cac
   const int64_t spare = (int64_t)kv_sm_count() * 4 / (int64_t)segs;
   int ctas = 1;
   while (ctas < kMaxCluster && ctas * 2 <= spare && (int64_t)ctas * 2048 < room) ctas *= 2;
-  p.hold = (int)min((room + ctas - 1) / ctas + kSelect, (int64_t)kMostHeld);
+  p.hold = (int)min((room + (int64_t)ctas * kSelect - 1) / ((int64_t)ctas * kSelect), (int64_t)kMostHeld);
+  const int bytes = p.hold * kPitch * 4;
   static uint64_t done = 0;
-  if (!kv_allow_smem(reinterpret_cast<const void *>(evict_select_kernel), kMostHeld * 4, &done)) return UNISON_ERR_CUDA;
-  rc = kv_launch("kv_evict_select", dim3((unsigned)(segs * ctas)), dim3(kSelect), p.hold * 4, cuda_stream, ctas,
+  if (!kv_allow_smem(reinterpret_cast<const void *>(evict_select_kernel), kMostHeld * kPitch * 4, &done)) return UNISON_ERR_CUDA;
+  rc = kv_launch("kv_evict_select", dim3((unsigned)(segs * ctas)), dim3(kSelect), bytes, cuda_stream, ctas,
                  evict_select_kernel, p);
   if (rc != UNISON_OK) return rc;
   // a CTA moves 256 slots at a time

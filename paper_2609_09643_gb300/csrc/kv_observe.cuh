@@ -6,7 +6,7 @@
 namespace unison {
 
 struct ObserveParams {
-  unison_kv_cache c;
+  KvCacheArg c;
   unison_kv_tree t;
   unison_kv_step s;
   unison_kv_path path;
