@@ -119,15 +119,16 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     // ------------------------------------------------------------- copies
     const int w = warp - kCopyWarp;
     KvCopier<T, DP> copier(w, lane, D, P.s.q);
-    int item = 0, tile_no = 0, seg_no = 0;
+    Ring ring;
+    int tile_no = 0, seg_no = 0;
     const bool by_boxes = P.k_boxes.rows && P.v_boxes.rows;
     bool ok = true;
     auto slot_for = [&](uint32_t &bar) -> uint32_t {  // waits until the next slot is free
-      const int s = item % kSlots<DP>, n = item / kSlots<DP>;
-      if (n > 0) ok = copier.wait(smem_u32(&sh.kv_free[s]), (n - 1) & 1, &sh.dead);
-      item++;
-      bar = smem_u32(&sh.kv_full[s]);
-      return slot_base + s * kTileBytes;
+      ok = copier.wait(smem_u32(&sh.kv_free[ring.at]), ring.turn ^ 1, &sh.dead);
+      bar = smem_u32(&sh.kv_full[ring.at]);
+      const uint32_t slot = slot_base + ring.at * kTileBytes;
+      ring.next(kSlots<DP>);
+      return slot;
     };
     while (at < run.end && ok) {
       Segment g;
@@ -234,12 +235,14 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
       const uint32_t shape_s = product_shape(kOperandType<T>, 128, kTile, false, P.s.scale < 0.f);
       const uint32_t shape_o = product_shape(kOperandType<T>, 128, DP, true, false);
       const uint32_t q_rows = smem_operand(q_base, kBlock), slots = smem_operand(slot_base, kBlock);
-      int item = 0, seg_no = 0, p_no[2] = {0, 0};
+      const uint32_t tmem = uniform(sh.tmem);
+      Ring ring;
+      int seg_no = 0, p_no[2] = {0, 0};
       bool ok = true;
       auto take = [&](int &s) -> uint32_t {  // waits for the next slot's tile
-        s = item % kSlots<DP>;
-        ok = __all_sync(~0u, bar_wait(smem_u32(&sh.kv_full[s]), (item / kSlots<DP>) & 1, &sh.dead));
-        item++;
+        s = ring.at;
+        ok = __all_sync(~0u, bar_wait(smem_u32(&sh.kv_full[s]), ring.turn, &sh.dead));
+        ring.next(kSlots<DP>);
         return slots + s * (kTileBytes >> 4);
       };
       auto scores = [&](int q, uint32_t keys) {
@@ -272,11 +275,11 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
         if (elect_one()) products_done(smem_u32(&bar));
         __syncwarp();
       };
-      while (at < run.end && ok) {
+      while (uniform(at < run.end && ok)) {
         Segment g;
         next_segment(g);
-        if (g.rows <= 0) continue;
-        const int n = g.kt1 - g.kt0, tiles = g.rows > 128 ? 2 : 1;
+        if (uniform(g.rows) <= 0) continue;
+        const int n = uniform(g.kt1 - g.kt0), tiles = uniform(g.rows) > 128 ? 2 : 1;
         int ks, vs;
         uint32_t keys = take(ks);
         if (ok) ok = __all_sync(~0u, bar_wait(smem_u32(&sh.q_full), seg_no & 1, &sh.dead));

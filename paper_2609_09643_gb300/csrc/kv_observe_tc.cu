@@ -32,9 +32,9 @@ constexpr int kMarkBytes = kTile * 12;
 struct ObserveShared {
   KvRunShared run;
   uint64_t k_full[kMostSlots], k_free[kMostSlots], q_full[2], q_free[2], t_full[kBuffers], t_free[kBuffers], seg_done[2],
-      part_full, part_free, idle;
+      part_full[2], part_free[2], idle;
   uint64_t mask[2][kNodes];  // of the accepted nodes
-  float part[kTile];         // the second group's sums
+  float part[2][kTile];      // sums of the group that does not write, of two tiles
   bool plain[2][4];          // whether every row that a copying warp read has weight to give
   uint32_t tmem;
   volatile int dead;
@@ -90,9 +90,9 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
       bar_init(smem_u32(&sh.q_full[i]), 4);
       bar_init(smem_u32(&sh.q_free[i]), 1);
       bar_init(smem_u32(&sh.seg_done[i]), kCopyWarp);
+      bar_init(smem_u32(&sh.part_full[i]), 4);
+      bar_init(smem_u32(&sh.part_free[i]), 4);
     }
-    bar_init(smem_u32(&sh.part_full), 4);
-    bar_init(smem_u32(&sh.part_free), 4);
     bar_init(smem_u32(&sh.idle), 1);
     sh.dead = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -139,7 +139,8 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
     // ------------------------------------------------------------- copies
     const int w = warp - kCopyWarp;
     KvCopier<T, DP> copier(w, lane, D, P.s.q);
-    int item = 0, seg_no = 0, tile_no = 0;
+    Ring ring, marks;
+    int seg_no = 0;
     bool ok = true;
     Segment g;
     while (ok && next_segment(g)) {
@@ -198,14 +199,15 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
         next_m = account(next_page, next_off);
         next_old = next_m ? *next_m : 0.f;
         later_page = find_page(kt + 2, later_off);
-        const int s = item % P.slots, n = item / P.slots;
-        if (n > 0) ok = copier.wait(smem_u32(&sh.k_free[s]), (n - 1) & 1, &sh.dead);
+        const int s = ring.at;
+        ok = copier.wait(smem_u32(&sh.k_free[s]), ring.turn ^ 1, &sh.dead);
         if (!ok) break;
-        item++;
+        ring.next(P.slots);
         const uint32_t bar = smem_u32(&sh.k_full[s]);
         const bool fresh = kt == g.tiles - 1 && j < g.tok.count && P.s.mass_new;
         if (fresh) m = P.s.mass_new + (int64_t)(g.tok.first + j) * H + g.head;
-        const int mark = tile_no++ % (P.slots + kMoreMarks) * kTile + j;
+        const int mark = marks.at * kTile + j;
+        marks.next(P.slots + kMoreMarks);
         marks_at[mark] = m;
         marks_old[mark] = old;
         __syncwarp();
@@ -227,7 +229,7 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
     copier.landed();
   } else if (warp == kBoxWarp) {
     // -------------------------------------------------------------- boxes
-    int item = 0;
+    Ring ring;
     bool ok = true;
     const int boxes = P.k_boxes.rows ? kTile / P.k_boxes.rows : 0;
     Segment g;
@@ -238,10 +240,11 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
         if (lane < boxes && kt < boxed) page = kv_page_load(P.c, g.b, kt * kTile + lane * P.k_boxes.rows, off);
       };
       find_box(g.kt0);
-      for (int kt = g.kt0; kt < g.kt1; kt++, item++) {
-        const int s = item % P.slots, n = item / P.slots;
-        if (n > 0) ok = __all_sync(~0u, bar_wait(smem_u32(&sh.k_free[s]), (n - 1) & 1, &sh.dead));
+      for (int kt = g.kt0; kt < g.kt1; kt++) {
+        const int s = ring.at;
+        ok = __all_sync(~0u, bar_wait(smem_u32(&sh.k_free[s]), ring.turn ^ 1, &sh.dead));
         if (!ok) break;
+        ring.next(P.slots);
         if (kt < boxed) {
           const int p = lane < boxes ? kv_page_ok(P.c, g.b, page) : -1, o = off;
           tile_boxes<DP>(slot_base + s * kTileBytes, P.k_boxes, smem_u32(&sh.k_full[s]), g.head, p, o);
@@ -256,28 +259,30 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
     // ----------------------------------------------------------- products
     // (the whole warp goes along, one lane issues)
     const uint32_t q_rows = smem_operand(q_base, kBlock), slots = smem_operand(slot_base, kBlock);
-    int item = 0, seg_no = 0, job = 0;
+    Ring ring, buffer;
+    int seg_no = 0;
     bool ok = true;
     auto release = [&](uint64_t &bar) {
       if (elect_one()) products_done(smem_u32(&bar));
       __syncwarp();
     };
+    const uint32_t tmem = uniform(sh.tmem);
     Segment g;
-    while (ok && next_segment(g)) {
-      const int qb = seg_no % P.q_buffers;
-      for (int kt = g.kt0; kt < g.kt1 && ok; kt++) {
-        const int s = item % P.slots;
-        ok = __all_sync(~0u, bar_wait(smem_u32(&sh.k_full[s]), (item / P.slots) & 1, &sh.dead));
-        if (ok && kt == g.kt0) ok = __all_sync(~0u, bar_wait(smem_u32(&sh.q_full[qb]), (seg_no / P.q_buffers) & 1, &sh.dead));
-        item++;
+    while (uniform(ok && next_segment(g))) {
+      const int qb = seg_no % P.q_buffers, n_rows = uniform(g.rows), tiles = uniform(g.kt1 - g.kt0);
+      for (int kt = 0; kt < tiles && ok; kt++) {
+        const int s = ring.at;
+        ok = __all_sync(~0u, bar_wait(smem_u32(&sh.k_full[s]), ring.turn, &sh.dead));
+        if (ok && kt == 0) ok = __all_sync(~0u, bar_wait(smem_u32(&sh.q_full[qb]), (seg_no / P.q_buffers) & 1, &sh.dead));
+        ring.next(P.slots);
         const uint32_t keys = slots + s * (kTileBytes >> 4);
-        for (int r0 = 0; (r0 == 0 || r0 < g.rows) && ok; r0 += 128, job++) {
-          const int buf = job % kBuffers;
-          if (job >= kBuffers)
-            ok = __all_sync(~0u, bar_wait(smem_u32(&sh.t_free[buf]), (job / kBuffers - 1) & 1, &sh.dead));
+        for (int r0 = 0; (r0 == 0 || r0 < n_rows) && ok; r0 += 128) {
+          const int buf = buffer.at;
+          ok = __all_sync(~0u, bar_wait(smem_u32(&sh.t_free[buf]), buffer.turn ^ 1, &sh.dead));
           if (!ok) break;
+          buffer.next(kBuffers);
           tmem_after_sync();
-          const int columns = (max(min(g.rows - r0, 128), 1) + 15) & ~15;
+          const int columns = (max(min(n_rows - r0, 128), 1) + 15) & ~15;
           const uint32_t shape = product_shape(kOperandType<T>, kTile, columns, false, false);
           if (elect_one()) {
             const uint32_t rows = q_rows + ((qb * q_bytes + r0 / 128 * kTileBytes) >> 4);
@@ -309,6 +314,7 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
       __syncwarp();
       if (lane == 0) bar_arrive(smem_u32(&bar));
     };
+    Ring marks;
     int job = 0, seg_no = 0, tile_no = 0, shared_tiles = 0;
     bool ok = true;
     Segment g;
@@ -316,10 +322,10 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
       const float *lse = lse_base + (seg_no & 1) * P.q_rows;
       const uint64_t *mask = sh.mask[seg_no & 1];
       const int chunks = max((g.rows + 127) / 128, 1);
-      for (int kt = g.kt0; kt < g.kt1; kt++, tile_no++) {
+      for (int kt = g.kt0; kt < g.kt1; kt++, tile_no++, marks.next(P.slots + kMoreMarks)) {
         const bool last = kt == g.tiles - 1;
-        // chunk by chunk in turn; a tile of one chunk is done by one group alone
-        const int first = chunks == 1 ? tile_no & 1 : 0;
+        // chunk by chunk in turn, beginning in turn where their number is odd
+        const int first = chunks & 1 ? tile_no & 1 : 0;
         const bool writes = wg == first;
         uint64_t sum[2] = {0, 0};
         for (int i = 0; i < chunks; i++, job++) {
@@ -400,22 +406,23 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
         float all, other;
         unpair(add_pair(sum[0], sum[1]), all, other);
         all += other;
-        if (chunks > 1) {  // the two groups' sums, in this order
-          if (wg == 1) {
-            if (shared_tiles > 0) ok = bar_wait(smem_u32(&sh.part_free), (shared_tiles - 1) & 1, &sh.dead);
-            if (ok) sh.part[key] = all;
-            warp_arrive(sh.part_full);
-          } else {
-            ok = bar_wait(smem_u32(&sh.part_full), shared_tiles & 1, &sh.dead);
-            if (ok) all += sh.part[key];
-            warp_arrive(sh.part_free);
-          }
+        if (chunks > 1) {  // the writer adds the other group's sum
+          const int set = shared_tiles & 1, use = shared_tiles >> 1;
           shared_tiles++;
-          ok = __all_sync(~0u, ok);
-          if (!ok) break;
+          if (!writes) {
+            if (use > 0) ok = __all_sync(~0u, bar_wait(smem_u32(&sh.part_free[set]), (use - 1) & 1, &sh.dead));
+            if (!ok) break;
+            sh.part[set][key] = all;
+            warp_arrive(sh.part_full[set]);
+          } else {
+            ok = __all_sync(~0u, bar_wait(smem_u32(&sh.part_full[set]), use & 1, &sh.dead));
+            if (!ok) break;
+            all += sh.part[set][key];
+            warp_arrive(sh.part_free[set]);
+          }
         }
         if (writes) {
-          const int mark = tile_no % (P.slots + kMoreMarks) * kTile + key;
+          const int mark = marks.at * kTile + key;
           float *to = marks_at[mark];
           if (to) *to = marks_old[mark] + all;
         }

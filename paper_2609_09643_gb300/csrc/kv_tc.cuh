@@ -33,6 +33,17 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
   *dead = 1;
   return false;
 }
+// A place in a ring of n, and the parity of the turn: what fills the place is
+// waited for with `turn`, its release by the turn before with `turn ^ 1` (true
+// at once in the first turn).  No divisions: a warp of its own takes five
+// cycles for each instruction.
+struct Ring {
+  int at = 0;
+  uint32_t turn = 0;
+  __device__ __forceinline__ void next(int n) {
+    if (++at == n) at = 0, turn ^= 1;
+  }
+};
 // What this thread wrote to shared memory, or knows to have been written there
 // (a barrier that it waited for), is seen by the products it issues next.
 __device__ __forceinline__ void fence_to_tensor() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
@@ -140,6 +151,10 @@ constexpr int kOperandType = 1;
 template <>
 constexpr int kOperandType<__half> = 0;
 
+// A value that all lanes of the warp have: told to the compiler, so that what
+// follows from it (descriptors, addresses, loops) is kept in uniform registers,
+// where the products take it from.
+__device__ __forceinline__ int uniform(int x) { return __shfl_sync(~0u, x, 0); }
 // One lane of a converged warp.
 __device__ __forceinline__ bool elect_one() {
   uint32_t one;
