@@ -324,7 +324,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) attend_kernel(con
       }
     }
     if (starts && !whole && tid == 0)
-      P.part[blockIdx.x] = {b, head, row_tile, kv_run_of(run, span.begin + kSetup + key_tiles - 1)};
+      P.part[blockIdx.x] = {kv_run_of(run, span.begin + kSetup + key_tiles - 1), head, row_tile * kRows, rows, tok.first};
   }
 }
 
@@ -346,9 +346,7 @@ __global__ void __launch_bounds__(kJoin) attend_join_kernel(const AttendParams P
   __shared__ float row_l[kJoinRows], row_top[kJoinRows];
   const AttendPart seg = P.part[blockIdx.x];
   if (seg.last < 0) return;
-  const int D = P.c.head_dim, G = P.group, R = P.rows;
-  const KvRange tok = kv_tokens(P.t, seg.b, nullptr);
-  const int rows = min(tok.count * G - seg.row_tile * R, R);
+  const int D = P.c.head_dim, G = P.group, R = P.rows, rows = seg.rows;
   const int step = P.row_groups;  // CTAs from one run to the next
   const int parts = seg.last - (int)blockIdx.x / step + 1;
   const int64_t stride = (int64_t)2 * R * (DP + 2) * step;
@@ -360,9 +358,13 @@ __global__ void __launch_bounds__(kJoin) attend_join_kernel(const AttendParams P
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int row = threadIdx.x / kVec % kJoinRows, share = threadIdx.x / (kVec * kJoinRows), col = threadIdx.x % kVec * 4;
   for (int row0 = blockIdx.y * kJoinRows; row0 < rows; row0 += gridDim.y * kJoinRows) {
-    float top = -INFINITY, l = 0.f;
-    if (warp < kJoinRows && row0 + warp < rows) {
-      for (int p = lane; p < parts; p += 32) top = fmaxf(top, part(p)[R * DP + row0 + warp]);
+    float top = -INFINITY, l = 0.f, one_m = -INFINITY, one_l = 0.f;
+    const bool weighs = warp < kJoinRows && row0 + warp < rows;
+    if (weighs) {
+      const float *q = part(lane) + R * DP + row0 + warp;
+      if (lane < parts) one_m = q[0], one_l = q[R];  // (all there is, mostly)
+      top = one_m;
+      for (int p = lane + 32; p < parts; p += 32) top = fmaxf(top, part(p)[R * DP + row0 + warp]);
 #pragma unroll
       for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
     }
@@ -371,12 +373,13 @@ __global__ void __launch_bounds__(kJoin) attend_join_kernel(const AttendParams P
     for (int p0 = 0; p0 < parts; p0 += kParts) {
       const int n = min(parts - p0, kParts);
       __syncthreads();
-      if (warp < kJoinRows && row0 + warp < rows)
+      if (weighs)
         for (int p = lane; p < n; p += 32) {
           const float *q = part(p0 + p) + R * DP + row0 + warp;
-          const float f = exp2_fast(q[0] - base);
+          const bool first = p0 + p < 32;
+          const float f = exp2_fast((first ? one_m : q[0]) - base);
           weight[warp][p] = f;
-          l += q[R] * f;
+          l += (first ? one_l : q[R]) * f;
         }
       __syncthreads();
       if (row0 + row < rows && col < D)
@@ -402,12 +405,13 @@ __global__ void __launch_bounds__(kJoin) attend_join_kernel(const AttendParams P
       }
       l = row_l[row];
       const float inv = l == 0.f ? 0.f : 1.f / l;
-      const int at = seg.row_tile * R + row0 + row, node = at / G, head = seg.head * G + at % G;
-      T *dst = static_cast<T *>(P.s.out) + (tok.first + node) * P.s.out_token + head * P.s.out_head + col;
+      const int at = seg.first_row + row0 + row, head = seg.head * G + at % G;
+      const int64_t token = seg.token + at / G;
+      T *dst = static_cast<T *>(P.s.out) + token * P.s.out_token + head * P.s.out_head + col;
       *reinterpret_cast<uint2 *>(dst) =
           make_uint2(KvType<T>::pack(sum.x * inv, sum.y * inv), KvType<T>::pack(sum.z * inv, sum.w * inv));
       if (col == 0 && P.s.lse)
-        P.s.lse[(int64_t)(tok.first + node) * P.s.n_q_heads + head] = (row_top[row] + log2f(l)) * 0.6931471805599453f;
+        P.s.lse[token * P.s.n_q_heads + head] = (row_top[row] + log2f(l)) * 0.6931471805599453f;
     }
   }
 }
@@ -433,7 +437,7 @@ AttendPlan attend_plan(int head_dim, int max_rows) {
 template <typename T, int DP>
 int attend_join(const AttendParams &p, const AttendPlan &plan, int max_rows, void *stream) {
   const int rounds = (min(max_rows, plan.rows) + kJoinRows - 1) / kJoinRows;
-  return kv_launch("kv_attend_join", dim3(plan.grid, min(rounds, 8)), dim3(kJoin), 0, stream, 1,
+  return kv_launch("kv_attend_join", dim3(plan.grid, min(rounds, plan.tc ? 16 : 8)), dim3(kJoin), 0, stream, 1,
                    attend_join_kernel<T, DP>, p);
 }
 

@@ -8,7 +8,9 @@ namespace unison {
 // What a CTA leaves to be joined: the segment (one session, KV head and row
 // tile) that begins in its run and goes on in the runs up to `last`.
 struct AttendPart {
-  int b, head, row_tile, last;  // last < 0: nothing
+  int last;                      // < 0: nothing
+  int head, first_row, rows;     // of the row tile: its first row, its rows
+  int64_t token;                 // the session's first token
 };
 
 struct AttendParams {

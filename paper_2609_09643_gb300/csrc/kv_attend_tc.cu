@@ -507,7 +507,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
         }
       }
       if (!whole && g.kt0 == 0 && r == 0 && q == 0)
-        P.part[blockIdx.x] = {g.b, g.head, g.row_tile, kv_run_of(run, seg_begin + kSetup + g.tiles - 1)};
+        P.part[blockIdx.x] = {kv_run_of(run, seg_begin + kSetup + g.tiles - 1), g.head, g.row_tile * kTcRows, g.rows, g.tok.first};
       __syncwarp();
       tmem_before_sync();  // the next segment's products overwrite O
     }

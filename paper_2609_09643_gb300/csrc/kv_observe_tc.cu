@@ -340,34 +340,23 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
           const uint32_t from = tmem + buf * 128 + lanes;
           const float *l = lse + i * 128;
           int r0 = 0;
-          if (!checked && n >= 32) {
-            // 32 scores at a time, the next ones on their way meanwhile
-            const int groups = n / 32;
-            uint32_t x[2][32];
+          if (!checked) {
             const uint64_t cc = pair(c, c);
-            tmem_ld32(x[0], from);
 #pragma unroll 1
-            for (int k = 0; k < groups; k += 2) {
+            for (; r0 + 32 <= n; r0 += 32) {
+              uint32_t v[32];
+              tmem_ld32(v, from + r0);
+              tmem_wait_ld(v);
 #pragma unroll
-              for (int h = 0; h < 2; h++) {
-                if (k + h < groups) {
-                  uint32_t(&v)[32] = x[h];
-                  tmem_wait_ld(v);
-                  tmem_ld32(x[h ^ 1], from + (r0 + 32 & 127));  // (the last one is not used)
-#pragma unroll
-                  for (int j = 0; j < 32; j += 4) {
-                    const ulonglong2 y = *reinterpret_cast<const ulonglong2 *>(l + r0 + j);
-                    float e[4];
-                    unpair(fma_pair(pair(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), cc, y.x), e[0], e[1]);
-                    unpair(fma_pair(pair(__uint_as_float(v[j + 2]), __uint_as_float(v[j + 3])), cc, y.y), e[2], e[3]);
-                    sum[0] = add_pair(sum[0], pair(exp2_fast(e[0]), exp2_fast(e[1])));
-                    sum[1] = add_pair(sum[1], pair(exp2_fast(e[2]), exp2_fast(e[3])));
-                  }
-                  r0 += 32;
-                }
+              for (int j = 0; j < 32; j += 4) {
+                const ulonglong2 y = *reinterpret_cast<const ulonglong2 *>(l + r0 + j);
+                float e[4];
+                unpair(fma_pair(pair(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), cc, y.x), e[0], e[1]);
+                unpair(fma_pair(pair(__uint_as_float(v[j + 2]), __uint_as_float(v[j + 3])), cc, y.y), e[2], e[3]);
+                sum[0] = add_pair(sum[0], pair(exp2_fast(e[0]), exp2_fast(e[1])));
+                sum[1] = add_pair(sum[1], pair(exp2_fast(e[2]), exp2_fast(e[3])));
               }
             }
-            tmem_wait_ld();
           }
           // the others 16 at a time, each with the question whether it counts
           int node = last ? (i * 128 + r0) / G : 0, head = i * 128 + r0 - node * G;
