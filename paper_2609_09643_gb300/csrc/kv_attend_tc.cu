@@ -245,36 +245,28 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
         ring.next(kSlots<DP>);
         return slots + s * (kTileBytes >> 4);
       };
+      const bool one = elect_one();
       auto scores = [&](int q, uint32_t keys) {
-        if (elect_one()) {
-          const uint32_t a = q_rows + q * (kTileBytes >> 4);
+        const uint32_t a = q_rows + q * (kTileBytes >> 4);
 #pragma unroll
-          for (int d = 0; d < DP / 16; d++) {
-            const uint32_t at = (d / 4 * kBlock + d % 4 * 32) >> 4;
-            product_ss(tmem + q * 128, a + at, keys + at, shape_s, d > 0);
-          }
-          products_done(smem_u32(&sh.s_full[q]));
-          bar_arrive(smem_u32(&sh.s_full[q]));  // hands on what the copies of the keys wrote besides (row_ok)
+        for (int d = 0; d < DP / 16; d++) {
+          const uint32_t at = (d / 4 * kBlock + d % 4 * 32) >> 4;
+          product_ss(one, tmem + q * 128, a + at, keys + at, shape_s, d > 0);
         }
-        __syncwarp();
+        products_done(one, smem_u32(&sh.s_full[q]));
+        bar_arrive_by(one, smem_u32(&sh.s_full[q]));  // hands on what the copies of the keys wrote besides (row_ok)
       };
       auto values = [&](int q, uint32_t vals, bool add) {
         ok = __all_sync(~0u, bar_wait(smem_u32(&sh.p_full[q]), p_no[q]++ & 1, &sh.dead));
         if (!ok) return;
         tmem_after_sync();
-        if (elect_one()) {
 #pragma unroll
-          for (int k = 0; k < kTile / 16; k++)
-            product_ts(tmem + 256 + q * DP, tmem + q * 128 + k * 8, vals + k * (2048 >> 4), shape_o, add || k > 0);
-          products_done(smem_u32(&sh.pv_done[q]));
-          bar_arrive(smem_u32(&sh.pv_done[q]));  // and those of the values (odd)
-        }
-        __syncwarp();
+        for (int k = 0; k < kTile / 16; k++)
+          product_ts(one, tmem + 256 + q * DP, tmem + q * 128 + k * 8, vals + k * (2048 >> 4), shape_o, add || k > 0);
+        products_done(one, smem_u32(&sh.pv_done[q]));
+        bar_arrive_by(one, smem_u32(&sh.pv_done[q]));  // and those of the values (odd)
       };
-      auto release = [&](uint64_t &bar) {
-        if (elect_one()) products_done(smem_u32(&bar));
-        __syncwarp();
-      };
+      auto release = [&](uint64_t &bar) { products_done(one, smem_u32(&bar)); };
       while (uniform(at < run.end && ok)) {
         Segment g;
         next_segment(g);

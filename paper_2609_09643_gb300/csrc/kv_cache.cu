@@ -67,6 +67,7 @@ struct EvictParams {
   const int32_t *keep;
   int32_t sink, recent;
   bool in_place;
+  bool by_four;    // mass and pos of four neighbouring slots are 16 aligned bytes
   int hold;        // keys of a thread of the selection in shared memory
   int per_seg;     // CTAs that move one segment's slots
   int32_t *moves;  // [segments][slots of a session]: sources, and from the middle on targets (in place)
@@ -82,11 +83,10 @@ constexpr int kMostHeld = 192;      // keys of a thread in shared memory
 // mass (the bits of a float, turned so that unsigned order is the numbers'
 // order, -0 as 0), NaN and slots without a page below all.
 __device__ __forceinline__ uint32_t order_key(const EvictParams &P, float mass, int pos, int next) {
-  if (pos < P.sink || (int64_t)pos >= (int64_t)next - P.recent) return ~0u;
-  const float x = mass + 0.f;
-  if (isnan(x)) return 0;
-  const uint32_t u = __float_as_uint(x);
-  return u >> 31 ? ~u : u | 0x80000000u;
+  const uint32_t u = __float_as_uint(mass + 0.f);
+  const uint32_t order = u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+  if (pos < P.sink || pos >= next) return ~0u;
+  return isnan(mass) ? 0 : order;
 }
 // Keys of kN slots, kStep apart, as far as they are below end: their look-ups
 // are on their way together.
@@ -114,6 +114,42 @@ __device__ __forceinline__ void slot_keys(const EvictParams &P, int b, int h, in
   }
 #pragma unroll
   for (int i = 0; i < kN; i++) key[i] = page[i] < 0 ? 0 : order_key(P, mass[i], pos[i], next);
+}
+
+// The same of groups of four neighbouring slots (P.by_four): one look-up and two
+// loads each.  A group's slots behind `end` lie in the same page.
+template <int kN>
+__device__ __forceinline__ void slot_keys_by_four(const EvictParams &P, int b, int h, int first, int step, int end,
+                                                  int next, uint32_t (&key)[kN][4]) {
+  int page[kN], off[kN];
+  float4 mass[kN];
+  int4 pos[kN];
+  const int64_t head = h * P.c.m_head;
+#pragma unroll
+  for (int i = 0; i < kN; i++) {
+    page[i] = kNoSlot;
+    if (first + i * step < end) page[i] = kv_page_load(P.c, b, first + i * step, off[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < kN; i++) {
+    page[i] = kv_page_ok(P.c, b, page[i]);
+    const int64_t m = head + page[i] * P.c.m_page + off[i];
+    const int s = first + i * step;
+    pos[i] = make_int4(s, s + 1, s + 2, s + 3);
+    mass[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (page[i] >= 0) {
+      mass[i] = *reinterpret_cast<const float4 *>(P.c.mass + m);
+      if (P.c.pos) pos[i] = *reinterpret_cast<const int4 *>(P.c.pos + m);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kN; i++) {
+    const bool no = page[i] < 0;
+    key[i][0] = no ? 0 : order_key(P, mass[i].x, pos[i].x, next);
+    key[i][1] = no ? 0 : order_key(P, mass[i].y, pos[i].y, next);
+    key[i][2] = no ? 0 : order_key(P, mass[i].z, pos[i].z, next);
+    key[i][3] = no ? 0 : order_key(P, mass[i].w, pos[i].w, next);
+  }
 }
 
 // How many slots of a session stay.
@@ -155,7 +191,9 @@ __global__ void __launch_bounds__(kSelect, 4) evict_select_kernel(const EvictPar
   const int b = seg / P.c.n_heads, h = seg % P.c.n_heads;
   const int len = kv_length(P.c, b);
   const int n = kept_count(P, b, len);
-  const int next = P.c.pos && P.c.next_pos ? P.c.next_pos[b] : len;
+  // positions from here on are protected
+  const int64_t from_pos = (int64_t)(P.c.pos && P.c.next_pos ? P.c.next_pos[b] : len) - P.recent;
+  const int next = (int)max(min(from_pos, (int64_t)INT32_MAX), (int64_t)INT32_MIN);
   const int64_t room = (int64_t)P.c.max_pages * P.c.page_size;
   int32_t *from = P.moves + seg * room, *into = from + room / 2;
   if (n == 0 || (P.in_place && n == len)) {  // all CTAs of the cluster
@@ -179,16 +217,33 @@ __global__ void __launch_bounds__(kSelect, 4) evict_select_kernel(const EvictPar
   uint32_t ties = 0;      // slots with that key that stay, the lowest first
   if (n < len) {
     // neighbouring threads read neighbouring slots here
-    constexpr int kAtOnce = 8;
     const uint32_t by_each = each == 1 ? 0 : 0xFFFFFFFFu / each + 1;  // (slots of a CTA < 2^16 while they are held)
-    for (int i = tid; i < last - first; i += kSelect * kAtOnce) {
-      uint32_t k[kAtOnce];
-      slot_keys<kAtOnce>(P, b, h, first + i, kSelect, last, next, k);
+    auto thread_of = [&](int s) { return each > held ? s / each : each == 1 ? s : (int)__umulhi(s, by_each); };
+    if (P.by_four) {
+      constexpr int kAtOnce = 4;
+      for (int i = tid * 4; i < last - first; i += kSelect * 4 * kAtOnce) {
+        uint32_t x[kAtOnce][4];
+        slot_keys_by_four<kAtOnce>(P, b, h, first + i, kSelect * 4, last, next, x);
 #pragma unroll
-      for (int j = 0; j < kAtOnce; j++) {
-        const int s = i + j * kSelect;
-        const int t = each <= held ? (each == 1 ? s : (int)__umulhi(s, by_each)) : s / each;
-        if (first + s < last && s - t * each < held) keys[(s - t * each) * kPitch + t] = k[j];
+        for (int j = 0; j < kAtOnce; j++) {
+          int s = i + j * kSelect * 4, t = thread_of(s), k = s - t * each;
+#pragma unroll
+          for (int e = 0; e < 4; e++, s++) {
+            if (first + s < last && k < held) keys[k * kPitch + t] = x[j][e];
+            if (++k == each) k = 0, t++;
+          }
+        }
+      }
+    } else {
+      constexpr int kAtOnce = 8;
+      for (int i = tid; i < last - first; i += kSelect * kAtOnce) {
+        uint32_t x[kAtOnce];
+        slot_keys<kAtOnce>(P, b, h, first + i, kSelect, last, next, x);
+#pragma unroll
+        for (int j = 0; j < kAtOnce; j++) {
+          const int s = i + j * kSelect, t = thread_of(s), k = s - t * each;
+          if (first + s < last && k < held) keys[k * kPitch + t] = x[j];
+        }
       }
     }
     for (int i = tid; i < kBins; i += kSelect) hist[0][i] = 0;
@@ -436,6 +491,8 @@ extern "C" int unison_kv_evict(const unison_kv_cache *cache, const unison_kv_cac
   p.sink = sink;
   p.recent = recent;
   p.in_place = into == nullptr;
+  p.by_four = cache->m_slot == 1 && cache->page_size % 4 == 0 && (cache->m_page | cache->m_head) % 4 == 0 &&
+              kv_aligned(cache->mass, 16) && kv_aligned(cache->pos, 16);
   p.moves = static_cast<int32_t *>(workspace);
   p.count = p.moves + segs * room;
   // CTAs per segment: as many as the segments leave room for (four CTAs on a
@@ -450,9 +507,12 @@ extern "C" int unison_kv_evict(const unison_kv_cache *cache, const unison_kv_cac
   rc = kv_launch("kv_evict_select", dim3((unsigned)(segs * ctas)), dim3(kSelect), bytes, cuda_stream, ctas,
                  evict_select_kernel, p);
   if (rc != UNISON_OK) return rc;
-  // a CTA moves 256 slots at a time
+  // A CTA moves 256 slots at a time.  Enough CTAs for all at once where a cache
+  // is copied (16 sessions' 8,192 slots: 179 us, with a fifth of the CTAs 192);
+  // few where a session at its budget drops a handful (8 slots of 64 sessions:
+  // 10 us, with five times the CTAs 16).
   const int64_t most = into ? min(room, (int64_t)into->max_pages * into->page_size) : room / 2;
-  const int64_t fill = ((int64_t)kv_sm_count() * 32 + segs - 1) / (int64_t)segs;
+  const int64_t fill = ((int64_t)kv_sm_count() * (into ? 32 : 6) + segs - 1) / (int64_t)segs;
   p.per_seg = (int)max((int64_t)1, min((most + 255) / 256, fill));
   return kv_launch("kv_evict_move", dim3((unsigned)(segs * p.per_seg)), dim3(256), 0, cuda_stream, 1,
                    evict_move_kernel<uint16_t>, p);

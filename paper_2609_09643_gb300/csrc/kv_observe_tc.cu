@@ -262,10 +262,8 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
     Ring ring, buffer;
     int seg_no = 0;
     bool ok = true;
-    auto release = [&](uint64_t &bar) {
-      if (elect_one()) products_done(smem_u32(&bar));
-      __syncwarp();
-    };
+    const bool one = elect_one();
+    auto release = [&](uint64_t &bar) { products_done(one, smem_u32(&bar)); };
     const uint32_t tmem = uniform(sh.tmem);
     Segment g;
     while (uniform(ok && next_segment(g))) {
@@ -284,17 +282,14 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
           tmem_after_sync();
           const int columns = (max(min(n_rows - r0, 128), 1) + 15) & ~15;
           const uint32_t shape = product_shape(kOperandType<T>, kTile, columns, false, false);
-          if (elect_one()) {
-            const uint32_t rows = q_rows + ((qb * q_bytes + r0 / 128 * kTileBytes) >> 4);
+          const uint32_t rows = q_rows + ((qb * q_bytes + r0 / 128 * kTileBytes) >> 4);
 #pragma unroll
-            for (int d = 0; d < DP / 16; d++) {
-              const uint32_t o = (d / 4 * kBlock + d % 4 * 32) >> 4;
-              product_ss(tmem + buf * 128, keys + o, rows + o, shape, d > 0);
-            }
-            products_done(smem_u32(&sh.t_full[buf]));
-            bar_arrive(smem_u32(&sh.t_full[buf]));  // hands on what the copies wrote besides
+          for (int d = 0; d < DP / 16; d++) {
+            const uint32_t o = (d / 4 * kBlock + d % 4 * 32) >> 4;
+            product_ss(one, tmem + buf * 128, keys + o, rows + o, shape, d > 0);
           }
-          __syncwarp();
+          products_done(one, smem_u32(&sh.t_full[buf]));
+          bar_arrive_by(one, smem_u32(&sh.t_full[buf]));  // hands on what the copies wrote besides
         }
         release(sh.k_free[s]);
       }

@@ -161,25 +161,38 @@ __device__ __forceinline__ bool elect_one() {
   asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xFFFFFFFF;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(one));
   return one != 0;
 }
-// d (+)= a b, both in shared memory; 16 elements of the sum.  By one thread.
-__device__ __forceinline__ void product_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t shape, bool add) {
+// d (+)= a b, both in shared memory; 16 elements of the sum.  The whole warp
+// comes here and the lane with `one` issues: without a branch, the operands'
+// descriptors stay in uniform registers.
+__device__ __forceinline__ void product_ss(bool one, uint32_t d, uint32_t a, uint32_t b, uint32_t shape, bool add) {
   asm volatile(
-      "{\n .reg .pred p;\n .reg .b64 a, b;\n setp.ne.b32 p, %4, 0;\n mov.b64 a, {%1, %5};\n mov.b64 b, {%2, %5};\n"
-      " tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n}\n" ::"r"(d),
-      "r"(a), "r"(b), "r"(shape), "r"((uint32_t)add), "r"(kOperandHigh)
+      "{\n .reg .pred p, q;\n .reg .b64 a, b;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %6, 0;\n"
+      " mov.b64 a, {%1, %5};\n mov.b64 b, {%2, %5};\n"
+      " @q tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n}\n" ::"r"(d),
+      "r"(a), "r"(b), "r"(shape), "r"((uint32_t)add), "r"(kOperandHigh), "r"((uint32_t)one)
       : "memory");
 }
 // The same with a in tensor memory.
-__device__ __forceinline__ void product_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t shape, bool add) {
+__device__ __forceinline__ void product_ts(bool one, uint32_t d, uint32_t a, uint32_t b, uint32_t shape, bool add) {
   asm volatile(
-      "{\n .reg .pred p;\n .reg .b64 b;\n setp.ne.b32 p, %4, 0;\n mov.b64 b, {%2, %5};\n"
-      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n}\n" ::"r"(d),
-      "r"(a), "r"(b), "r"(shape), "r"((uint32_t)add), "r"(kOperandHigh)
+      "{\n .reg .pred p, q;\n .reg .b64 b;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %6, 0;\n"
+      " mov.b64 b, {%2, %5};\n"
+      " @q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n}\n" ::"r"(d),
+      "r"(a), "r"(b), "r"(shape), "r"((uint32_t)add), "r"(kOperandHigh), "r"((uint32_t)one)
       : "memory");
 }
-// The barrier gets one arrival when all products of this thread so far are done.
-__device__ __forceinline__ void products_done(uint32_t bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+// The barrier gets one arrival when all products of that lane so far are done.
+__device__ __forceinline__ void products_done(bool one, uint32_t bar) {
+  asm volatile(
+      "{\n .reg .pred q;\n setp.ne.b32 q, %1, 0;\n"
+      " @q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}\n" ::"r"(bar),
+      "r"((uint32_t)one)
+      : "memory");
+}
+__device__ __forceinline__ void bar_arrive_by(bool one, uint32_t bar) {
+  asm volatile("{\n .reg .pred q;\n setp.ne.b32 q, %1, 0;\n @q mbarrier.arrive.shared::cta.b64 _, [%0];\n}\n" ::"r"(bar),
+               "r"((uint32_t)one)
+               : "memory");
 }
 
 // Address of a 16-byte chunk in such an operand of rows * 128-byte blocks.
