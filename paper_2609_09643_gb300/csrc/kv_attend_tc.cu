@@ -148,9 +148,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
       copier.issued(smem_u32(&sh.q_full));
       int kt = g.kt0;
       const int boxed = by_boxes ? min(g.kt1, g.len / kTile) : kt;  // full tiles go by boxes
+      if (kt < boxed) copier.landed();
       if (w > 0) {
         // (the other warps keep step: a barrier's parity tells only its last phase)
-        if (kt < boxed) copier.landed();
         for (; kt < boxed && ok; kt++, tile_no++)
           for (int part = 0; part < 2; part++) {
             uint32_t bar;
@@ -159,34 +159,27 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
             if (lane == 0) bar_arrive(bar);
           }
       } else {
-        const int boxes = by_boxes ? kTile / P.k_boxes.rows : 0;
-        int page = -1, off = 0;
-        auto find_box = [&](int kt) {
-          if (lane < boxes) page = kv_page_load(P.c, g.b, kt * kTile + lane * P.k_boxes.rows, off);
-        };
-        if (kt < boxed) find_box(kt);
+        const int rows = P.k_boxes.rows, box = lane / (DP / 64);
+        BoxPages pages;
+        pages.reset();
         for (; kt < boxed; kt++, tile_no++) {
+          int p, o;
+          pages.get(P.c, g.b, kt, rows, g.len, box, p, o);
           uint32_t bar;
           uint32_t dst = slot_for(bar);
           if (!ok) break;
-          const int p = lane < boxes ? kv_page_ok(P.c, g.b, page) : -1, o = off;
-          const uint32_t there = __ballot_sync(~0u, lane >= boxes || p >= 0);
-          // (row 32 i + j of the tile lies in box (32 i + j) / rows)
-          if (lane < 4) {
-            uint32_t word = ~0u;
-            if (there != ~0u) {
-              word = 0;
-              for (int j = 0; j < 32; j++) word |= (there >> ((lane * 32 + j) / P.k_boxes.rows) & 1) << j;
-            }
-            sh.row_ok[tile_no & 7][lane] = word;
+          // which of the tile's rows have a page: row r is in box r / rows
+          const bool gap = __any_sync(~0u, box * rows < kTile && p < 0);
+          for (int i = 0; i < 4; i++) {
+            const int at = gap ? (i * 32 + lane) / rows * (DP / 64) : 0;
+            const uint32_t word = gap ? __ballot_sync(~0u, __shfl_sync(~0u, p, at) >= 0) : ~0u;
+            if (lane == 0) sh.row_ok[tile_no & 7][i] = word;
           }
           __syncwarp();
           tile_boxes<DP>(dst, P.k_boxes, bar, g.head, p, o);
-          if (kt + 1 < boxed) find_box(kt + 1);
           dst = slot_for(bar);
           if (!ok) break;
           tile_boxes<DP>(dst, P.v_boxes, bar, g.head, p, o);
-          if (kt == g.kt0) copier.landed();
         }
       }
       // the other tiles, row by row

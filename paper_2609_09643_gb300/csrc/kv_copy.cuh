@@ -39,17 +39,35 @@ __device__ __forceinline__ void box_copy(uint32_t dst, const KvBoxes &x, uint32_
       : "memory");
 }
 
-// All boxes of a full tile, by one warp: lane i knows the page that box i lies
-// in, and the slot of that page that it begins with.  The warp's arrival at the
-// tile's barrier announces the bytes.
+// All boxes of a full tile, by one warp.  The pages of the next boxes are looked
+// up 32 at a time, a lane each, so that most tiles wait for no look-up.
+struct BoxPages {
+  int page, off, first;  // of box first + lane of the session
+  __device__ __forceinline__ void reset() { first = INT32_MIN / 2; }
+  // The page, and the slot of it, that lane i's box of the tile begins with:
+  // box * rows is below `end` slots.
+  __device__ __forceinline__ void get(const KvCacheArg &c, int b, int tile, int rows, int end, int box, int &p, int &o) {
+    const int per_tile = kTileRows / rows, wanted = tile * per_tile;
+    if (wanted < first || wanted + per_tile > first + 32) {
+      first = wanted;
+      const int slot = (wanted + (int)(threadIdx.x & 31)) * rows;
+      page = kNoSlot;
+      off = 0;
+      if (slot < end) page = kv_page_ok(c, b, kv_page_load(c, b, slot, off));
+    }
+    p = __shfl_sync(~0u, page, wanted - first + box);
+    o = __shfl_sync(~0u, off, wanted - first + box);
+  }
+};
+// Sends them: lane i has column block i % (DP / 64) of box i / (DP / 64), which
+// begins in page p at slot o.  The warp's arrival at the tile's barrier
+// announces the bytes.
 template <int DP>
-__device__ __forceinline__ void tile_boxes(uint32_t dst, const KvBoxes &x, uint32_t bar, int head, int page, int off) {
+__device__ __forceinline__ void tile_boxes(uint32_t dst, const KvBoxes &x, uint32_t bar, int head, int p, int o) {
   constexpr int kHalves = DP / 64;
-  const int lane = threadIdx.x & 31;
+  const int lane = threadIdx.x & 31, box = lane / kHalves, col = lane % kHalves * 64;
   if (lane == 0) bar_expect(bar, kTileRows * DP * 2);
   __syncwarp();
-  const int box = lane / kHalves, col = lane % kHalves * 64;
-  const int p = __shfl_sync(~0u, page, box), o = __shfl_sync(~0u, off, box);
   if (box * x.rows < kTileRows)
     box_copy(dst + col * (kTileRows * 2) + box * x.rows * 128, x, bar, col, o, head, p);
   __syncwarp();

@@ -231,27 +231,23 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
     // -------------------------------------------------------------- boxes
     Ring ring;
     bool ok = true;
-    const int boxes = P.k_boxes.rows ? kTile / P.k_boxes.rows : 0;
+    const int box = lane / (DP / 64);
+    BoxPages pages;
     Segment g;
     while (ok && next_segment(g)) {
-      const int boxed = boxes ? g.len / kTile : 0;
-      int page = kNoSlot, off = 0;
-      auto find_box = [&](int kt) {
-        if (lane < boxes && kt < boxed) page = kv_page_load(P.c, g.b, kt * kTile + lane * P.k_boxes.rows, off);
-      };
-      find_box(g.kt0);
+      const int boxed = P.k_boxes.rows ? g.len / kTile : 0;
+      pages.reset();
       for (int kt = g.kt0; kt < g.kt1; kt++) {
         const int s = ring.at;
+        int p = -1, o = 0;
+        if (kt < boxed) pages.get(P.c, g.b, kt, P.k_boxes.rows, g.len, box, p, o);
         ok = __all_sync(~0u, bar_wait(smem_u32(&sh.k_free[s]), ring.turn ^ 1, &sh.dead));
         if (!ok) break;
         ring.next(P.slots);
-        if (kt < boxed) {
-          const int p = lane < boxes ? kv_page_ok(P.c, g.b, page) : -1, o = off;
+        if (kt < boxed)
           tile_boxes<DP>(slot_base + s * kTileBytes, P.k_boxes, smem_u32(&sh.k_full[s]), g.head, p, o);
-          if (kt + 1 < g.kt1) find_box(kt + 1);
-        } else if (lane == 0) {
+        else if (lane == 0)
           bar_arrive(smem_u32(&sh.k_full[s]));
-        }
       }
     }
     if (!ok) KvCopier<T, DP>::give_up();

@@ -161,6 +161,41 @@ def test_attend_absent_pages_and_bad_values_are_reported(kv):
     assert math.isclose(float(lse[0, 0]), s.max() + math.log(w.sum()), abs_tol=1e-4)
 
 
+def _without_page(m, b, page):
+    """Session b loses a page: its slots count as absent, for the kernels by the
+    table, for the reference by leaving them out."""
+    ref_m = Made.__new__(Made)
+    ref_m.__dict__.update(m.__dict__)
+    m.page_table[b, page] = -1
+    ref_m.table = m.table.copy()
+    ref_m.table[b, page:-1] = m.table[b, page + 1:]
+    ref_m.lens = list(m.lens)
+    ref_m.lens[b] -= m.page
+    return ref_m
+
+
+@pytest.mark.parametrize("page", [8, 16, 32, 64, 128, 256, 24])
+@pytest.mark.parametrize("group,d,layout", [(16, 128, "hnd"), (2, 64, "nhd")])
+def test_absent_pages_in_the_middle(kv, page, group, d, layout):
+    """A page that is missing inside tiles that are full otherwise, for attention
+    of many and of few rows and for the observed weight."""
+    m = Made([1500, 700], [9, 5], hkv=3, group=group, d=d, page=page, layout=layout, seed=page)
+    start = m.mass.clone()
+    r = _without_page(m, 0, 2)
+    out, lse = kv.attend(m.cache(kv), m.tree(kv), m.q, m.k_new, m.v_new)
+    want, want_lse, tol, tol_lse = ref.attend(r)
+    assert np.max(np.abs(f64(out) - want) / (tol + 1e-30)) <= 1
+    assert np.max(np.abs(f64(lse) - want_lse) / tol_lse) <= 1
+    kv.observe(m.cache(kv), m.tree(kv), m.q, lse, m.k_new)
+    added, bound, _, _ = ref.observe(r, lse)
+    for b in range(2):
+        s = np.arange(r.lens[b])
+        at = (r.table[b, s // page], slice(None), s % page)
+        got = (f64(m.mass) - f64(start))[at]
+        assert np.all(np.abs(got - added[b]) <= bound[b] + 2.0 ** -22 * np.abs(f64(m.mass)[at]))
+    assert m.status.tolist() == [-4, 0]
+
+
 def test_attend_same_bits_again_and_in_a_graph(kv):
     m = Made([3000, 17, 900], [8, 1, 30], group=4, d=128, seed=14)
     cache, tree = m.cache(kv), m.tree(kv)
