@@ -624,3 +624,28 @@ def test_a_whole_step_without_synchronisation_and_in_a_graph(kv):
                        for x in ("k", "v", "mass", "pos", "length", "next_pos", "status")])
     assert all(torch.equal(a, b) for a, b in zip(*states))
     assert states[0][4].tolist() == [200, 40, 5] and states[0][6].tolist() == [0, 0, 0]
+
+
+def test_the_serving_example(kv):
+    """examples/serving_step.py: budgets hold, positions are distinct, demoted
+    sessions arrive with their most attended tokens."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "serving_step.py")
+    spec = importlib.util.spec_from_file_location("serving_step", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    r = example.main(sessions=5, steps=6, prompt_tokens=300, budget=256, quiet=True)
+    fast, far = r["fast"], r["far"]
+    assert fast.length.tolist() == [256] * 5
+    assert [n > 0 for n in far.length.tolist()] == [b in r["victims"] for b in range(5)]
+    assert fast.status.tolist() == [0] * 5 and far.status.tolist() == [0] * 5
+    assert fast.next_pos.tolist() == (300 + r["told"]).tolist()
+    assert bool(torch.isfinite(r["out"].float()).all())
+    slot = torch.arange(256, device="cuda")
+    for b in range(5):
+        page = fast.page_table[b].long()[slot // 64]
+        pos = fast.pos[page, :, slot % 64]
+        for h in range(pos.shape[1]):
+            assert pos[:, h].unique().numel() == 256
+            assert set(range(4)) <= set(pos[:, h].tolist())  # the sink stayed
