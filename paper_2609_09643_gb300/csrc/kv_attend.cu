@@ -425,7 +425,7 @@ struct AttendPlan {
 AttendPlan attend_plan(int head_dim, int max_rows) {
   AttendPlan p;
   p.dp = head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256;
-  p.tc = max_rows > 64 && p.dp <= 128;
+  p.tc = max_rows > 32 && p.dp <= 128;
   p.rows = p.tc ? kTcRows : max_rows <= 16 ? 16 : max_rows <= 32 ? 32 : 64;
   // CTAs that go through the same keys with row tiles of their own
   p.row_groups = p.tc ? min((max_rows + kTcRows - 1) / kTcRows, 4) : 1;
@@ -458,9 +458,12 @@ int attend_rows(const AttendParams &p, const AttendPlan &plan, int max_rows, voi
       return rc == UNISON_OK ? attend_join<T, DP>(p, plan, max_rows, stream) : rc;
     }
   }
-  rc = plan.rows == 16   ? attend_run<T, DP, 1>(p, plan, stream)
-       : plan.rows == 32 ? attend_run<T, DP, 2>(p, plan, stream)
-                         : attend_run<T, DP, 4>(p, plan, stream);
+  if (plan.rows == 16)
+    rc = attend_run<T, DP, 1>(p, plan, stream);
+  else if (DP <= 128 || plan.rows == 32)
+    rc = attend_run<T, DP, 2>(p, plan, stream);
+  else
+    rc = attend_run<T, DP, DP <= 128 ? 2 : 4>(p, plan, stream);
   return rc == UNISON_OK ? attend_join<T, DP>(p, plan, max_rows, stream) : rc;
 }
 

@@ -31,9 +31,11 @@ constexpr int kTcSmem = 1024 + kTcRows *DP * 2 + kSlots<DP> *kTile *DP * 2;
 template <int DP>
 struct TcShared {
   KvRunShared run;
-  uint64_t kv_full[kSlots<DP>], kv_free[kSlots<DP>], q_full, q_free, s_full[2], p_full[2], pv_done[2], idle;
+  uint64_t kv_full[kSlots<DP>], kv_free[kSlots<DP>], q_full, q_free, s_full[2], p_full[2], pv_done[2], half_full,
+      half_free, idle;
   uint32_t row_ok[8][4];  // which keys of a tile exist
   bool odd[4][4];         // whether new values that a copying warp read hold infinities or NaN, of four segments
+  float half[2][128];     // maxima and sums of a single query tile's second half of the keys
   uint32_t tmem;
   volatile int dead;
 };
@@ -43,6 +45,22 @@ struct Segment {
   int b, head, row_tile, rows, tiles, kt0, kt1, len;  // rows <= 0: nothing to do for this CTA
   KvRange tok;
 };
+
+// The order in which a run's tiles of keys (0) and values (1) go through the ring,
+// n tiles: K0 V0 K1 V1 .. where two query tiles share them, K0 K1 V0 K2 V1 .. where
+// one query tile takes the key tiles in two turns.
+__device__ __forceinline__ int item_of(int j, int n, bool turns, int &tile) {
+  if (!turns || n == 1) {
+    tile = j >> 1;
+    return j & 1;
+  }
+  if (j == 0 || j == 2 * n - 1) {
+    tile = j ? n - 1 : 0;
+    return j ? 1 : 0;
+  }
+  tile = j & 1 ? (j + 1) >> 1 : (j >> 1) - 1;
+  return ~j & 1;
+}
 
 struct AttendTcParams : AttendParams {
   KvBoxes k_boxes, v_boxes;
@@ -76,6 +94,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     bar_init(smem_u32(&sh.q_full), 4);
     bar_init(smem_u32(&sh.q_free), 1);
     bar_init(smem_u32(&sh.idle), 1);
+    bar_init(smem_u32(&sh.half_full), 4);
+    bar_init(smem_u32(&sh.half_free), 4);
     for (int i = 0; i < 2; i++) {
       bar_init(smem_u32(&sh.s_full[i]), 2);
       bar_init(smem_u32(&sh.p_full[i]), 4);  // warps
@@ -122,6 +142,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     Ring ring;
     int tile_no = 0, seg_no = 0;
     const bool by_boxes = P.k_boxes.rows && P.v_boxes.rows;
+    BoxSender<DP> sender(w ? P.v_boxes : P.k_boxes);
     bool ok = true;
     auto slot_for = [&](uint32_t &bar) -> uint32_t {  // waits until the next slot is free
       ok = copier.wait(smem_u32(&sh.kv_free[ring.at]), ring.turn ^ 1, &sh.dead);
@@ -146,77 +167,83 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
         copier.rows(q_base + q * kTileBytes, src);
       }
       copier.issued(smem_u32(&sh.q_full));
-      int kt = g.kt0;
-      const int boxed = by_boxes ? min(g.kt1, g.len / kTile) : kt;  // full tiles go by boxes
-      if (kt < boxed) copier.landed();
-      if (w > 0) {
-        // (the other warps keep step: a barrier's parity tells only its last phase)
-        for (; kt < boxed && ok; kt++, tile_no++)
-          for (int part = 0; part < 2; part++) {
-            uint32_t bar;
-            slot_for(bar);
-            if (!ok) break;
-            if (lane == 0) bar_arrive(bar);
-          }
-      } else {
-        const int rows = P.k_boxes.rows, box = lane / (DP / 64);
-        BoxPages pages;
-        pages.reset();
-        for (; kt < boxed; kt++, tile_no++) {
-          int p, o;
-          pages.get(P.c, g.b, kt, rows, g.len, box, p, o);
-          uint32_t bar;
-          uint32_t dst = slot_for(bar);
-          if (!ok) break;
-          // which of the tile's rows have a page: row r is in box r / rows
-          const bool gap = __any_sync(~0u, box * rows < kTile && p < 0);
-          for (int i = 0; i < 4; i++) {
-            const int at = gap ? (i * 32 + lane) / rows * (DP / 64) : 0;
-            const uint32_t word = gap ? __ballot_sync(~0u, __shfl_sync(~0u, p, at) >= 0) : ~0u;
-            if (lane == 0) sh.row_ok[tile_no & 7][i] = word;
-          }
-          __syncwarp();
-          tile_boxes<DP>(dst, P.k_boxes, bar, g.head, p, o);
-          dst = slot_for(bar);
-          if (!ok) break;
-          tile_boxes<DP>(dst, P.v_boxes, bar, g.head, p, o);
-        }
-      }
-      // the other tiles, row by row
-      for (; kt < g.kt1 && ok; kt++, tile_no++) {
-        const int j = w * 32 + lane;  // this lane's row: a slot of a page, or a new token
-        const bool last = kt == last_tile, fresh = last && j < g.tok.count;
-        int page = -1, off = 0;
-        if (!last && kt * kTile + j < g.len) page = kv_page(P.c, g.b, kt * kTile + j, off);
-        const uint32_t there = __ballot_sync(~0u, fresh || page >= 0);
-        for (int part = 0; part < 2 && ok; part++) {  // keys, values
-          const T *src = nullptr;
-          if (fresh)
-            src = part ? static_cast<const T *>(P.s.v_new) + (g.tok.first + j) * P.s.v_token + g.head * P.s.v_head
-                       : static_cast<const T *>(P.s.k_new) + (g.tok.first + j) * P.s.k_token + g.head * P.s.k_head;
-          else if (page >= 0)
-            src = part ? static_cast<const T *>(P.c.v) + page * P.c.v_page + g.head * P.c.v_head + off * P.c.v_slot
-                       : static_cast<const T *>(P.c.k) + page * P.c.k_page + g.head * P.c.k_head + off * P.c.k_slot;
-          uint32_t bar;
+      const int n = g.kt1 - g.kt0, j = w * 32 + lane;  // j: this lane's row of a tile
+      const int boxed = by_boxes ? g.len / kTile : 0;  // full tiles go by boxes
+      sender.reset();
+      int page[2], off[2], next_page = kNoSlot, next_off = 0;  // of this lane's row in the last two tiles, the next
+      for (int item = 0; item < 2 * n; item++) {
+        int tile;
+        const int part = item_of(item, n, g.rows <= 128, tile), kt = g.kt0 + tile;
+        uint32_t bar;
+        if (kt < boxed) {  // the first warp sends the keys, the second one the values
+          if (item == 0) copier.landed();
+          const bool sends = w == part;
+          if (sends) sender.look_up(P.c, g.b, kt, g.len);
           const uint32_t dst = slot_for(bar);
           if (!ok) break;
-          copier.rows(dst, src);
-          if (part == 0) {
-            if (lane == 0) sh.row_ok[tile_no & 7][w] = there;
-            copier.issued(bar);
-          } else if (!last) {
-            copier.issued(bar);
+          if (!sends) {
+            // (every warp keeps step: a barrier's parity tells only its last phase)
+            if (lane == 0) bar_arrive(bar);
           } else {
-            // A new token that a row does not see must not reach it as 0 * inf:
-            // such values become 0 here and are put back, row by row, at the end.
-            copier.issued(0);
-            copier.landed();
-            const bool odd = copier.zero_odd_values(dst);
-            if (lane == 0) sh.odd[seg_no & 3][w] = odd;
-            copier.arrive(bar);
+            if (part == 0) {
+              if (!sender.gap) {
+                if (lane < 4) sh.row_ok[(tile_no + tile) & 7][lane] = ~0u;
+              } else {
+                for (int i = 0; i < 4; i++) {
+                  const uint32_t word = sender.present(kt, i);
+                  if (lane == 0) sh.row_ok[(tile_no + tile) & 7][i] = word;
+                }
+              }
+              __syncwarp();
+            }
+            sender.send(kt, dst, bar, g.head);
           }
+          if (copier.waiting[0] | copier.waiting[1]) copier.issued(0);
+          continue;
+        }
+        // row by row
+        const bool last = kt == last_tile, fresh = last && j < g.tok.count;
+        auto look_up = [&](int kt, int &o) -> int {
+          o = 0;
+          return kt < last_tile && kt * kTile + j < g.len ? kv_page_load(P.c, g.b, kt * kTile + j, o) : kNoSlot;
+        };
+        if (part == 0) {
+          if (tile == 0 || kt == boxed) next_page = look_up(kt, next_off);
+          const int p = kv_page_ok(P.c, g.b, next_page);
+          if (tile & 1)
+            page[1] = p, off[1] = next_off;
+          else
+            page[0] = p, off[0] = next_off;
+          next_page = look_up(kt + 1, next_off);
+        }
+        const int p = tile & 1 ? page[1] : page[0], o = tile & 1 ? off[1] : off[0];
+        const T *src = nullptr;
+        if (fresh)
+          src = part ? static_cast<const T *>(P.s.v_new) + (g.tok.first + j) * P.s.v_token + g.head * P.s.v_head
+                     : static_cast<const T *>(P.s.k_new) + (g.tok.first + j) * P.s.k_token + g.head * P.s.k_head;
+        else if (p >= 0)
+          src = part ? static_cast<const T *>(P.c.v) + p * P.c.v_page + g.head * P.c.v_head + o * P.c.v_slot
+                     : static_cast<const T *>(P.c.k) + p * P.c.k_page + g.head * P.c.k_head + o * P.c.k_slot;
+        const uint32_t there = __ballot_sync(~0u, src != nullptr);
+        const uint32_t dst = slot_for(bar);
+        if (!ok) break;
+        copier.rows(dst, src);
+        if (part == 0) {
+          if (lane == 0) sh.row_ok[(tile_no + tile) & 7][w] = there;
+          copier.issued(bar);
+        } else if (!last) {
+          copier.issued(bar);
+        } else {
+          // A new token that a row does not see must not reach it as 0 * inf:
+          // such values become 0 here and are put back, row by row, at the end.
+          copier.issued(0);
+          copier.landed();
+          const bool odd = copier.zero_odd_values(dst);
+          if (lane == 0) sh.odd[seg_no & 3][w] = odd;
+          copier.arrive(bar);
         }
       }
+      tile_no += n;
       seg_no++;
     }
     copier.landed();
@@ -239,15 +266,16 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
         return slots + s * (kTileBytes >> 4);
       };
       const bool one = elect_one();
-      auto scores = [&](int q, uint32_t keys) {
+      // Scores of slot `to` from query tile q; weights of slot q with the values.
+      auto scores = [&](int to, int q, uint32_t keys) {
         const uint32_t a = q_rows + q * (kTileBytes >> 4);
 #pragma unroll
         for (int d = 0; d < DP / 16; d++) {
           const uint32_t at = (d / 4 * kBlock + d % 4 * 32) >> 4;
-          product_ss(one, tmem + q * 128, a + at, keys + at, shape_s, d > 0);
+          product_ss(one, tmem + to * 128, a + at, keys + at, shape_s, d > 0);
         }
-        products_done(one, smem_u32(&sh.s_full[q]));
-        bar_arrive_by(one, smem_u32(&sh.s_full[q]));  // hands on what the copies of the keys wrote besides (row_ok)
+        products_done(one, smem_u32(&sh.s_full[to]));
+        bar_arrive_by(one, smem_u32(&sh.s_full[to]));  // hands on what the copies of the keys wrote besides (row_ok)
       };
       auto values = [&](int q, uint32_t vals, bool add) {
         ok = __all_sync(~0u, bar_wait(smem_u32(&sh.p_full[q]), p_no[q]++ & 1, &sh.dead));
@@ -269,23 +297,48 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
         uint32_t keys = take(ks);
         if (ok) ok = __all_sync(~0u, bar_wait(smem_u32(&sh.q_full), seg_no & 1, &sh.dead));
         if (!ok) break;
-        for (int q = 0; q < tiles; q++) scores(q, keys);
-        release(sh.kv_free[ks]);
-        if (n == 1) release(sh.q_free);
-        for (int i = 0; i < n && ok; i++) {
-          const uint32_t vals = take(vs);
-          for (int q = 0; q < tiles && ok; q++) {
-            values(q, vals, i > 0);
-            if (!ok) break;
-            if (q == tiles - 1) release(sh.kv_free[vs]);
-            if (i + 1 < n) {
-              if (q == 0) keys = take(ks);
+        if (tiles == 2) {  // two query tiles share the keys
+          for (int q = 0; q < 2; q++) scores(q, q, keys);
+          release(sh.kv_free[ks]);
+          if (n == 1) release(sh.q_free);
+          for (int i = 0; i < n && ok; i++) {
+            const uint32_t vals = take(vs);
+            for (int q = 0; q < 2 && ok; q++) {
+              values(q, vals, i > 0);
               if (!ok) break;
-              scores(q, keys);
-              if (q == tiles - 1) {
-                release(sh.kv_free[ks]);
-                if (i + 2 == n) release(sh.q_free);
+              if (q == 1) release(sh.kv_free[vs]);
+              if (i + 1 < n) {
+                if (q == 0) keys = take(ks);
+                if (!ok) break;
+                scores(q, q, keys);
+                if (q == 1) {
+                  release(sh.kv_free[ks]);
+                  if (i + 2 == n) release(sh.q_free);
+                }
               }
+            }
+          }
+        } else {  // one query tile: key tiles in turn to the two slots
+          scores(0, 0, keys);
+          release(sh.kv_free[ks]);
+          if (n > 1) {
+            keys = take(ks);
+            if (!ok) break;
+            scores(1, 0, keys);
+            release(sh.kv_free[ks]);
+          }
+          if (n <= 2) release(sh.q_free);
+          for (int i = 0; i < n && ok; i++) {
+            const uint32_t vals = take(vs);
+            if (ok) values(i & 1, vals, i > 1);
+            if (!ok) break;
+            release(sh.kv_free[vs]);
+            if (i + 2 < n) {
+              keys = take(ks);
+              if (!ok) break;
+              scores(i & 1, 0, keys);
+              release(sh.kv_free[ks]);
+              if (i + 3 == n) release(sh.q_free);
             }
           }
         }
@@ -304,27 +357,32 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     // (the sign is in the products; not 0, so that -inf stays -inf)
     const float c = fmaxf(fabsf(P.s.scale) * 1.4426950408889634f, 1.2e-38f);
     int s_no = 0, seg_no = 0, tile_no = 0;  // products seen, segments, key tiles of this CTA
+    int halves = 0;                          // segments that the slots joined
+    bool owed = false;                       // slot 1: its half of the last one may still be read
     bool ok = true;
     while (at < run.end && ok) {
       Segment g;
       next_segment(g);
       if (g.rows <= 0) continue;
       const int mine = seg_no++;
-      if (q * 128 >= g.rows) {  // the segment has no such tile
-        tile_no += g.kt1 - g.kt0;
-        continue;
-      }
-      const int row = g.row_tile * kTcRows + q * 128 + r, node = row / G;
-      const bool used = q * 128 + r < g.rows;
+      // Two query tiles: one for each slot.  One: the slots take its key tiles in
+      // turn, as two halves that are joined at the end.
+      const bool turns = g.rows <= 128;
+      const int n = g.kt1 - g.kt0, begin = turns ? g.kt0 + q : g.kt0, step = turns ? 2 : 1;
+      const int tiles_before = tile_no;
+      tile_no += n;
+      if (begin >= g.kt1) continue;
+      const int tr = turns ? r : q * 128 + r, row = g.row_tile * kTcRows + tr, node = row / G;
+      const bool used = tr < g.rows;
       const uint64_t mask = !used ? 0 : P.t.mask ? P.t.mask[g.tok.first + node] : ~0ull >> (63 - node);
       float m = -INFINITY, l = 0.f;
-      for (int kt = g.kt0; kt < g.kt1; kt++, tile_no++) {
+      for (int kt = begin; kt < g.kt1; kt += step) {
         ok = __all_sync(~0u, bar_wait(smem_u32(&sh.s_full[q]), s_no & 1, &sh.dead));
         if (!ok) break;
         tmem_after_sync();
         uint32_t see[4];
 #pragma unroll
-        for (int i = 0; i < 4; i++) see[i] = sh.row_ok[tile_no & 7][i];
+        for (int i = 0; i < 4; i++) see[i] = sh.row_ok[(tiles_before + kt - g.kt0) & 7][i];
         if (kt == g.tiles - 1) {
           see[0] &= (uint32_t)mask;
           see[1] &= (uint32_t)(mask >> 32);
@@ -336,7 +394,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
         // registers until the tile's maximum is known.  (Two passes cost 700
         // cycles of a tile's 2,400 here.)
         bool done = false;
-        if (!hidden && kt > g.kt0) {
+        if (!hidden && kt > begin) {
           const float base = m == -INFINITY ? 0.f : m;
           const uint64_t bb = pair(-base, -base);
           uint64_t sum[2] = {0, 0};
@@ -385,8 +443,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
 #pragma unroll
             for (int j = 0; j < 32; j++) t = fmaxf(t, __uint_as_float(x[0][j]));
           }
-          const float to = kt == g.kt0 || t * c > m + kSlack ? t * c : m;
-          if (kt > g.kt0 && __any_sync(~0u, to != m)) {
+          const float to = kt == begin || t * c > m + kSlack ? t * c : m;
+          if (kt > begin && __any_sync(~0u, to != m)) {
             const float f = m == to ? 1.f : exp2_fast(m - to);
             ok = __all_sync(~0u, bar_wait(smem_u32(&sh.pv_done[q]), (s_no - 1) & 1, &sh.dead));
             if (!ok) break;
@@ -428,6 +486,11 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
         }
         tmem_wait_st();
         tmem_before_sync();
+        if (owed) {  // these weights' product overwrites the slot's sums
+          ok = __all_sync(~0u, bar_wait(smem_u32(&sh.half_free), (halves - 1) & 1, &sh.dead));
+          if (!ok) break;
+          owed = false;
+        }
         __syncwarp();
         if (lane == 0) bar_arrive(smem_u32(&sh.p_full[q]));
         s_no++;
@@ -440,18 +503,47 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
       ok = __all_sync(~0u, bar_wait(smem_u32(&sh.pv_done[q]), (s_no - 1) & 1, &sh.dead));
       if (!ok) break;
       tmem_after_sync();
+      const bool join = turns && n > 1;
+      float f0 = 1.f, f1 = 0.f;
+      if (join) {
+        if (q == 1) {
+          sh.half[0][r] = m;
+          sh.half[1][r] = l;
+          tmem_before_sync();
+          __syncwarp();
+          if (lane == 0) bar_arrive(smem_u32(&sh.half_full));
+          halves++;
+          owed = true;
+          continue;
+        }
+        ok = __all_sync(~0u, bar_wait(smem_u32(&sh.half_full), halves++ & 1, &sh.dead));
+        if (!ok) break;
+        tmem_after_sync();
+        const float m1 = sh.half[0][r], l1 = sh.half[1][r], top = fmaxf(m, m1), base = top == -INFINITY ? 0.f : top;
+        f0 = exp2_fast(m - base);
+        f1 = exp2_fast(m1 - base);
+        l = l * f0 + l1 * f1;
+        m = top;
+      }
       const bool whole = g.kt0 == 0 && g.kt1 == g.tiles;
       const bool *flags = sh.odd[mine & 3];
       const bool odd = g.kt1 == g.tiles && (flags[0] || flags[1] || flags[2] || flags[3]);
       const float inv = l == 0.f ? 0.f : 1.f / l;
       float *part = P.partial + ((int64_t)blockIdx.x * 2 + (g.kt0 == 0 ? 1 : 0)) * (kTcRows * (DP + 2));
-      const int pr = q * 128 + r;
       T *dst = static_cast<T *>(P.s.out) + (g.tok.first + node) * P.s.out_token + (g.head * G + row % G) * P.s.out_head;
 #pragma unroll 1
       for (int d0 = 0; d0 < DP; d0 += 32) {
         uint32_t o[32];
         tmem_ld32(o, o_addr + d0);
         tmem_wait_ld(o);
+        if (join) {
+          uint32_t o1[32];
+          tmem_ld32(o1, o_addr + DP + d0);
+          tmem_wait_ld(o1);
+#pragma unroll
+          for (int i = 0; i < 32; i++)
+            o[i] = __float_as_uint(__uint_as_float(o[i]) * f0 + __uint_as_float(o1[i]) * f1);
+        }
         if (used && odd) {
           const uint64_t see = mask & (~0ull >> (64 - g.tok.count));
           for (int j = 0; j < g.tok.count; j++) {
@@ -479,14 +571,14 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
         } else if (used) {
 #pragma unroll
           for (int i = 0; i < 32; i += 4)
-            *reinterpret_cast<uint4 *>(part + pr * DP + d0 + i) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+            *reinterpret_cast<uint4 *>(part + tr * DP + d0 + i) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
         }
         __syncwarp();  // the next load is one instruction of the whole warp
       }
       if (used) {
         if (!whole) {
-          part[kTcRows * DP + pr] = m;
-          part[kTcRows * (DP + 1) + pr] = l;
+          part[kTcRows * DP + tr] = m;
+          part[kTcRows * (DP + 1) + tr] = l;
         } else if (P.s.lse) {
           P.s.lse[(int64_t)(g.tok.first + node) * P.s.n_q_heads + g.head * G + row % G] = (m + log2f(l)) * 0.6931471805599453f;
         }
@@ -495,6 +587,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
         P.part[blockIdx.x] = {kv_run_of(run, seg_begin + kSetup + g.tiles - 1), g.head, g.row_tile * kTcRows, g.rows, g.tok.first};
       __syncwarp();
       tmem_before_sync();  // the next segment's products overwrite O
+      if (join && lane == 0) bar_arrive(smem_u32(&sh.half_free));
     }
   }
   __syncwarp();

@@ -39,39 +39,59 @@ __device__ __forceinline__ void box_copy(uint32_t dst, const KvBoxes &x, uint32_
       : "memory");
 }
 
-// All boxes of a full tile, by one warp.  The pages of the next boxes are looked
-// up 32 at a time, a lane each, so that most tiles wait for no look-up.
-struct BoxPages {
-  int page, off, first;  // of box first + lane of the session
+// All boxes of full tiles, by one warp: lane i has column block i % (DP / 64) of
+// box i / (DP / 64) of the tile.  The pages of the next boxes are looked up 32
+// at a time, a lane each, so that most tiles wait for no look-up.  (A warp of
+// its own takes five to eight cycles an instruction, and a tile's bytes arrive
+// in 1,400: what is the same for every tile is worked out once.)
+template <int DP>
+struct BoxSender {
+  static constexpr int kHalves = DP / 64;
+  const KvBoxes &x;
+  int rows, per_tile;     // of a box; boxes of a tile
+  int box, col, to;       // of this lane: the latter in the tile
+  bool sends;
+  int page, off, first;   // of box first + lane of the session
+  bool gap;               // whether one of those has no page
+
+  __device__ __forceinline__ BoxSender(const KvBoxes &boxes) : x(boxes) {
+    const int lane = threadIdx.x & 31;
+    rows = x.rows;
+    per_tile = rows ? kTileRows / rows : 0;
+    box = lane / kHalves;
+    col = lane % kHalves * 64;
+    sends = box < per_tile;
+    to = col * (kTileRows * 2) + box * rows * 128;
+  }
   __device__ __forceinline__ void reset() { first = INT32_MIN / 2; }
-  // The page, and the slot of it, that lane i's box of the tile begins with:
-  // box * rows is below `end` slots.
-  __device__ __forceinline__ void get(const KvCacheArg &c, int b, int tile, int rows, int end, int box, int &p, int &o) {
-    const int per_tile = kTileRows / rows, wanted = tile * per_tile;
+  // Look-ups for a tile of the session; `end`: its slots.
+  __device__ __forceinline__ void look_up(const KvCacheArg &c, int b, int tile, int end) {
+    const int wanted = tile * per_tile;
     if (wanted < first || wanted + per_tile > first + 32) {
       first = wanted;
       const int slot = (wanted + (int)(threadIdx.x & 31)) * rows;
       page = kNoSlot;
       off = 0;
       if (slot < end) page = kv_page_ok(c, b, kv_page_load(c, b, slot, off));
+      gap = __any_sync(~0u, page < 0 && slot < end);
     }
-    p = __shfl_sync(~0u, page, wanted - first + box);
-    o = __shfl_sync(~0u, off, wanted - first + box);
+  }
+  // Which of the tile's rows 32 i .. 32 i + 31 have a page.
+  __device__ __forceinline__ uint32_t present(int tile, int i) const {
+    if (!gap) return ~0u;
+    const int of = tile * per_tile - first + (i * 32 + (int)(threadIdx.x & 31)) / rows;
+    return __ballot_sync(~0u, __shfl_sync(~0u, page, of) >= 0);
+  }
+  // Sends the tile.  The warp's arrival at its barrier announces the bytes.
+  __device__ __forceinline__ void send(int tile, uint32_t dst, uint32_t bar, int head) const {
+    const int of = tile * per_tile - first + box;
+    const int p = __shfl_sync(~0u, page, of & 31), o = __shfl_sync(~0u, off, of & 31);
+    if ((threadIdx.x & 31) == 0) bar_expect(bar, kTileRows * DP * 2);
+    __syncwarp();
+    if (sends) box_copy(dst + to, x, bar, col, o, head, p);
+    __syncwarp();
   }
 };
-// Sends them: lane i has column block i % (DP / 64) of box i / (DP / 64), which
-// begins in page p at slot o.  The warp's arrival at the tile's barrier
-// announces the bytes.
-template <int DP>
-__device__ __forceinline__ void tile_boxes(uint32_t dst, const KvBoxes &x, uint32_t bar, int head, int p, int o) {
-  constexpr int kHalves = DP / 64;
-  const int lane = threadIdx.x & 31, box = lane / kHalves, col = lane % kHalves * 64;
-  if (lane == 0) bar_expect(bar, kTileRows * DP * 2);
-  __syncwarp();
-  if (box * x.rows < kTileRows)
-    box_copy(dst + col * (kTileRows * 2) + box * x.rows * 128, x, bar, col, o, head, p);
-  __syncwarp();
-}
 
 // A copying warp.  Each item (a tile, or the query rows) ends with one arrival
 // of the warp at the item's barrier: two items later, when the copies have

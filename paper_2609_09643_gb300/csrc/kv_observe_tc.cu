@@ -231,21 +231,19 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
     // -------------------------------------------------------------- boxes
     Ring ring;
     bool ok = true;
-    const int box = lane / (DP / 64);
-    BoxPages pages;
+    BoxSender<DP> sender(P.k_boxes);
     Segment g;
     while (ok && next_segment(g)) {
       const int boxed = P.k_boxes.rows ? g.len / kTile : 0;
-      pages.reset();
+      sender.reset();
       for (int kt = g.kt0; kt < g.kt1; kt++) {
         const int s = ring.at;
-        int p = -1, o = 0;
-        if (kt < boxed) pages.get(P.c, g.b, kt, P.k_boxes.rows, g.len, box, p, o);
+        if (kt < boxed) sender.look_up(P.c, g.b, kt, g.len);
         ok = __all_sync(~0u, bar_wait(smem_u32(&sh.k_free[s]), ring.turn ^ 1, &sh.dead));
         if (!ok) break;
         ring.next(P.slots);
         if (kt < boxed)
-          tile_boxes<DP>(slot_base + s * kTileBytes, P.k_boxes, smem_u32(&sh.k_full[s]), g.head, p, o);
+          sender.send(kt, slot_base + s * kTileBytes, smem_u32(&sh.k_full[s]), g.head);
         else if (lane == 0)
           bar_arrive(smem_u32(&sh.k_full[s]));
       }
