@@ -608,8 +608,8 @@ int attend_tc(const AttendParams &p, int grid, void *stream) {
   if (!kv_allow_smem(kernel, kTcSmem<DP>, &done)) return UNISON_ERR_CUDA;
   AttendTcParams q;
   static_cast<AttendParams &>(q) = p;
-  kv_boxes(q.k_boxes, p.c, p.c.k, p.c.k_page, p.c.k_head, p.c.k_slot);
-  kv_boxes(q.v_boxes, p.c, p.c.v, p.c.v_page, p.c.v_head, p.c.v_slot);
+  kv_boxes(q.k_boxes, p.c, p.c.k, p.c.k_page, p.c.k_head, p.c.k_slot, 16);
+  kv_boxes(q.v_boxes, p.c, p.c.v, p.c.v_page, p.c.v_head, p.c.v_slot, 16);
   return kv_launch("kv_attend", dim3(grid), dim3(kThreads), kTcSmem<DP>, stream, 1, attend_tc_kernel<T, DP>, q);
 }
 

@@ -23,11 +23,13 @@ Encode encoder() {
 }
 }  // namespace
 
-void kv_boxes(KvBoxes &x, const unison_kv_cache &c, const void *pool, int64_t page, int64_t head, int64_t slot) {
+void kv_boxes(KvBoxes &x, const unison_kv_cache &c, const void *pool, int64_t page, int64_t head, int64_t slot,
+              int least) {
   x.rows = 0;
-  // a tile is whole pages of a multiple of eight slots, or a page whole tiles
-  const int ps = c.page_size;
-  const int rows = ps % kTileRows == 0 ? kTileRows : kTileRows % ps == 0 && ps % 8 == 0 ? ps : 0;
+  // A box is the largest power of two of slots that divides a page, up to 128: no
+  // box lies in two pages, and its rows are whole repeats of the swizzle.
+  const int ps = c.page_size, two = ps & -ps;
+  const int rows = two >= least ? (two < kTileRows ? two : kTileRows) : 0;
   if (c.n_heads == 1) head = slot * ps;  // an axis of one: its stride means nothing
   x.head_first = head < slot;
   if (c.n_pages == 1) page = x.head_first ? slot * ps : head * c.n_heads;

@@ -1,12 +1,18 @@
 // Tiles of paged rows on their way into the tensor cores' operands, for the
 // four copying warps of a CTA.
 //
-// Full tiles of caches whose pages divide a tile (or the other way round) go by
-// TMA: one warp sends the boxes, and the hardware reports the bytes to the
-// tile's barrier.  Every other tile (the last one of
-// a session, its new tokens, odd page sizes or strides) and the query rows go
-// by 16-byte copies, which can leave out single rows.  (128 keys of 128
-// elements cost the warps about 2,000 cycles by copies, and next to nothing by TMA.)
+// Full tiles of caches whose page size is a multiple of 16 go by TMA: one warp
+// sends the boxes, and the hardware reports the bytes to the tile's barrier.
+// Every other tile (the last one of a session, its new tokens, other page sizes
+// or odd strides) and the query rows go by 16-byte copies, which can leave out
+// single rows.  128 keys of 128 elements cost the warps about 2,000 cycles by
+// copies and next to nothing by TMA; but a box takes the hardware 90 cycles,
+// however small.  16 sessions of 16k keys, 8 KV heads, in pages of 8 / 16 / 64
+// slots: attention of 64 rows 251 / 200 / 180 us by boxes, 194 by copies (head
+// size 128), 171 / 143 / 124 and 156 (64); observation of 8 to 64 rows 168 /
+// 113 / 113 and 113 by copies.  So boxes have 16 slots or more, except where
+// query rows leave place for two tiles only: 512 rows' observation, few of them
+// accepted, takes 168 by boxes of 8 and 350 by copies, which are not early enough.
 #pragma once
 
 #include <cuda.h>
@@ -23,8 +29,10 @@ struct KvBoxes {
   int rows;         // of a box, 0: not by TMA
   bool head_first;  // heads lie closer together than slots
 };
-// On the host; rows = 0 where the pool does not allow it.
-void kv_boxes(KvBoxes &x, const unison_kv_cache &c, const void *pool, int64_t page, int64_t head, int64_t slot);
+// On the host; rows = 0 where the pool does not allow boxes of `least` slots
+// (8, or a multiple of it).
+void kv_boxes(KvBoxes &x, const unison_kv_cache &c, const void *pool, int64_t page, int64_t head, int64_t slot,
+              int least);
 
 __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {  // an arrival that announces bytes
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");

@@ -22,7 +22,6 @@ constexpr int kThreads = 448;
 constexpr int kTile = 128;
 constexpr int kCopyWarp = 8, kIssueWarp = 12, kBoxWarp = 13;
 constexpr int kBuffers = 4, kMostSlots = 6;
-constexpr int kSetup = 2;  // tiles that a segment's beginning costs
 constexpr int kNodes = UNISON_KV_MAX_TOKENS;
 // Tiles whose keys' accounts are kept in shared memory: those on their way, the
 // four that may be in tensor memory, and the one that is being looked up.
@@ -65,16 +64,25 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
   float **const marks_at = reinterpret_cast<float **>(lse_base + 2 * P.q_rows);  // where a key's weight goes
   float *const marks_old = reinterpret_cast<float *>(marks_at + (P.slots + kMoreMarks) * kTile);  // what is there
 
-  // A tile's share of the run: its keys' way here, or the products and weights
-  // of its chunks of 128 query rows, where those take longer.
-  auto share = [&](int b, int tokens) {
-    const int chunks = (path_count(P, b, tokens) * G + 127) / 128;
-    return max(4, 3 * chunks);
+  // A tile's share of the run, in units of 33 ns: its keys' way here, or the
+  // products and weights of its chunks of 128 query rows, where those take
+  // longer.  (16 sessions of 16k keys, 8 KV heads, head size 128: 115 us with 8
+  // rows, 126 with 128, 174 with 136, 188 with 256, 258 with 384, 328 with 512;
+  // head size 64: 83, 102, 164, 178, 252, 312.  Beside sessions of many rows,
+  // which leave them the memory, few rows take a fifth less.)
+  const int keys_way = DP == 64 ? 20 : P.slots > 2 || P.k_boxes.rows > 8 ? 26 : P.k_boxes.rows ? 40 : 80;
+  auto share = [&](int rows) {
+    return rows <= 128 ? keys_way + rows / 32 : max(keys_way, 16 + 9 * ((rows + 127) / 128) + rows / 14);
   };
+  // A head's beginning (its query rows, an empty pipeline) and the tiles that are
+  // not full, in tiles.
+  auto setup = [&](int rows) { return max((160 + rows / 4) / share(rows), 1); };
   KvRun run;
   if (!kv_find_run(run, sh.run, P.c.n_seqs, gridDim.x, blockIdx.x, [&](int b) {
         const int tiles = observe_key_tiles(P, b, kTile);
-        return tiles ? (int64_t)(tiles + kSetup) * H * share(b, kv_tokens(P.t, b, nullptr).count) : 0;
+        if (!tiles) return (int64_t)0;
+        const int rows = path_count(P, b, kv_tokens(P.t, b, nullptr).count) * G;
+        return (int64_t)(tiles + setup(rows)) * H * share(rows);
       }))
     return;
   if (tid == 0) {
@@ -106,12 +114,14 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
   int b = run.b;
   int64_t at = run.at, seq_begin = run.begin;
   // The next tiles of one head in this run: those whose share begins in it.
-  // (A head's tiles come behind kSetup shares that stand for its beginning.)
+  // (A head's tiles come behind the shares that stand for its beginning.)
   auto next_segment = [&](Segment &g) -> bool {
     while (at < run.end) {
       g.tok = kv_tokens(P.t, b, nullptr);
       g.tiles = observe_key_tiles(P, b, kTile);
-      const int64_t each = share(b, g.tok.count), per_head = g.tiles ? g.tiles + kSetup : 0;
+      g.rows = path_count(P, b, g.tok.count) * G;
+      const int each = share(g.rows), before = setup(g.rows);
+      const int64_t per_head = g.tiles ? g.tiles + before : 0;
       const int64_t all = per_head * H;
       const int64_t from = (at - seq_begin + each - 1) / each;
       const int64_t to = min((run.end - seq_begin + each - 1) / each, all);
@@ -124,12 +134,11 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
       g.head = (int)(from / per_head);
       const int64_t head_begin = g.head * per_head, head_end = min(head_begin + per_head, to);
       at = seq_begin + head_end * each;
-      g.kt0 = (int)max(from - head_begin - kSetup, (int64_t)0);
-      g.kt1 = (int)max(head_end - head_begin - kSetup, (int64_t)0);
+      g.kt0 = (int)max(from - head_begin - before, (int64_t)0);
+      g.kt1 = (int)max(head_end - head_begin - before, (int64_t)0);
       if (g.kt0 >= g.kt1) continue;
       g.b = b;
       g.len = kv_length(P.c, b);
-      g.rows = path_count(P, b, g.tok.count) * G;
       return true;
     }
     return false;
@@ -435,7 +444,9 @@ int observe_tc(ObserveParams p, int max_rows, void *stream) {
     return UNISON_ERR_CUDA;
   ObserveTcParams q;
   static_cast<ObserveParams &>(q) = p;
-  kv_boxes(q.k_boxes, p.c, p.c.k, p.c.k_page, p.c.k_head, p.c.k_slot);
+  // Boxes of eight slots where shared memory holds few tiles on their way
+  // (kv_copy.cuh has the figures).
+  kv_boxes(q.k_boxes, p.c, p.c.k, p.c.k_page, p.c.k_head, p.c.k_slot, p.slots > 2 ? 16 : 8);
   return kv_launch("kv_observe", dim3(kv_sm_count()), dim3(kThreads), max(bytes, 120 << 10), stream, 1,
                    observe_tc_kernel<T, DP>, q);
 }
