@@ -28,7 +28,9 @@
  * outside the pool, a length beyond the page table, offsets that do not
  * ascend) are never followed: lengths and offsets are clamped, a slot without
  * a page counts as absent, and, where the cache has a status array, the
- * session's word receives UNISON_ERR_RANGE.  The calls never clear it.
+ * session's word receives UNISON_ERR_RANGE.  The calls never clear it.  Waits
+ * inside the kernels are bounded; one that gives up (no input makes it) leaves
+ * UNISON_ERR_TIMEOUT there, and that session's results are undefined.
  */
 #ifndef UNISON_KV_H
 #define UNISON_KV_H

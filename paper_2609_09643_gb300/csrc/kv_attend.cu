@@ -1,4 +1,13 @@
-// Attention of drafted tokens over the paged cache (unison_kv_attend).
+// Attention of drafted tokens over the paged cache (unison_kv_attend): the
+// variant for few query rows, and the join of what both variants split.
+//
+//   S = scale q . k,  m = max S,  l = sum exp(S - m),  out = sum exp(S - m) v / l
+//
+// in one pass over the keys: when a tile raises the maximum, l and the sums so
+// far are scaled by exp(old m - new m).  Two halves of the keys are joined in
+// the same way, so the keys may be shared out at will: the call's key tiles are
+// one list, every CTA takes an equal run of it, whatever the sessions' lengths
+// are, and a second kernel joins what lies in several runs.
 #include "kv_attend.cuh"
 
 namespace unison {
@@ -12,9 +21,18 @@ constexpr int kAttendStages = DP <= 128 ? 3 : 2;
 template <int DP, int MT>
 constexpr int kAttendSmem = kAttendStages<DP> *kTile *DP * 4 + MT * 16 * DP * 2;
 
-// Reads of one tile's rows are planned two tiles ahead of their use: first the
-// page ids (into a register), then the rows' addresses (shared memory), then
-// the copies.
+// Up to 32 query rows per KV head (64 with head sizes above 128, row tile by row
+// tile): every key meets too few rows for the products to matter, so memory
+// bounds it, and the keys go through shared memory by 16-byte copies, which take
+// any page size and stride alike.  The query heads of a KV head share its keys;
+// the four warps split the rows (MT) and then a tile's keys.  Reads of one
+// tile's rows are planned two tiles ahead of their use: first the page ids (into
+// a register), then the rows' addresses (shared memory), then the copies.
+// Weights are rounded to the cache's type, as the products' operands have to be;
+// their sum l is of the weights before that.
+// One token x 4 heads over 64 sessions of 512 to 32k keys (8 KV heads of 128,
+// 2.07 GB): 303 us, 6.8 TB/s; 8 tokens over two sessions of 128k keys (1.07 GB):
+// 165 us, 6.5 TB/s; one token of one session of 2,100 keys: 8 us.
 template <typename T, int DP, int MT>
 __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) attend_kernel(const AttendParams P) {
   follow_last_kernel();
@@ -299,7 +317,8 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) attend_kernel(con
       }
       const int row = row_tile * kRows + r, node = row / G;
       if (kt1 == key_tiles && odd_values) {
-        const uint64_t mask = (P.t.mask ? P.t.mask[tok.first + node] : ~0ull >> (63 - node)) & (~0ull >> (64 - tok.count));
+        const uint64_t mask =
+            (P.t.mask ? P.t.mask[tok.first + node] : ~0ull >> (63 - node)) & (~0ull >> (64 - tok.count));
         for (int j = 0; j < tok.count; j++) {
           if (!(mask >> j & 1)) continue;
           const T *v = static_cast<const T *>(P.s.v_new) + (tok.first + j) * P.s.v_token + head * P.s.v_head + d;
@@ -310,7 +329,8 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) attend_kernel(con
       }
       if (whole) {
         const float inv = l == 0.f ? 0.f : 1.f / l;
-        T *dst = static_cast<T *>(P.s.out) + (tok.first + node) * P.s.out_token + (head * G + row % G) * P.s.out_head + d;
+        T *dst = static_cast<T *>(P.s.out) + (tok.first + node) * P.s.out_token +
+                 (head * G + row % G) * P.s.out_head + d;
         *reinterpret_cast<uint32_t *>(dst) = KvType<T>::pack(x * inv, y * inv);
         if (d == 0 && P.s.lse)
           P.s.lse[(int64_t)(tok.first + node) * P.s.n_q_heads + head * G + row % G] =
@@ -324,7 +344,8 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) attend_kernel(con
       }
     }
     if (starts && !whole && tid == 0)
-      P.part[blockIdx.x] = {kv_run_of(run, span.begin + kSetup + key_tiles - 1), head, row_tile * kRows, rows, tok.first};
+      P.part[blockIdx.x] = {kv_run_of(run, span.begin + kSetup + key_tiles - 1), head, row_tile * kRows, rows,
+                            tok.first};
   }
 }
 
@@ -332,6 +353,9 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) attend_kernel(con
 // the other kernel and four rows.  The parts' statistics become weights in
 // shared memory, in rounds of kParts; the threads of a row then add up 16 bytes
 // of it each, from parts of their own where there are threads to spare.
+// Bound by its loads' latency: 4 us after one short session, 7 us after two of
+// 128k keys (a segment lies in up to 19 runs), 27 us for 304 parts of 256 rows
+// (40 MB).
 constexpr int kJoin = 256;
 constexpr int kJoinRows = 4;
 constexpr int kParts = 256;
@@ -356,7 +380,8 @@ __global__ void __launch_bounds__(kJoin) attend_join_kernel(const AttendParams P
   auto part = [&](int p) { return p ? rest + p * stride : first; };
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int row = threadIdx.x / kVec % kJoinRows, share = threadIdx.x / (kVec * kJoinRows), col = threadIdx.x % kVec * 4;
+  const int row = threadIdx.x / kVec % kJoinRows, share = threadIdx.x / (kVec * kJoinRows),
+            col = threadIdx.x % kVec * 4;
   for (int row0 = blockIdx.y * kJoinRows; row0 < rows; row0 += gridDim.y * kJoinRows) {
     float top = -INFINITY, l = 0.f, one_m = -INFINITY, one_l = 0.f;
     const bool weighs = warp < kJoinRows && row0 + warp < rows;
@@ -422,6 +447,12 @@ struct AttendPlan {
   uint64_t bytes;
 };
 
+// Variants, by the query rows per KV head (16 sessions of 16k keys, 8 KV heads):
+//   up to 32 the one above: 176 us for 32 rows of 128 elements (the other one:
+//            186), 114 of 64 (148)
+//   more     tensor cores with sums in tensor memory: 180 us for 48 rows of 128
+//            (342 here, row tile by row tile), 125 of 64 (158); 185 and 126 for 128
+// Head sizes above 128 do not fit the latter's tensor memory.
 AttendPlan attend_plan(int head_dim, int max_rows) {
   AttendPlan p;
   p.dp = head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256;
@@ -458,12 +489,10 @@ int attend_rows(const AttendParams &p, const AttendPlan &plan, int max_rows, voi
       return rc == UNISON_OK ? attend_join<T, DP>(p, plan, max_rows, stream) : rc;
     }
   }
-  if (plan.rows == 16)
-    rc = attend_run<T, DP, 1>(p, plan, stream);
-  else if (DP <= 128 || plan.rows == 32)
-    rc = attend_run<T, DP, 2>(p, plan, stream);
-  else
-    rc = attend_run<T, DP, DP <= 128 ? 2 : 4>(p, plan, stream);
+  constexpr int kMostTiles = DP <= 128 ? 2 : 4;  // of 16 rows
+  rc = plan.rows == 16   ? attend_run<T, DP, 1>(p, plan, stream)
+       : plan.rows == 32 ? attend_run<T, DP, 2>(p, plan, stream)
+                         : attend_run<T, DP, kMostTiles>(p, plan, stream);
   return rc == UNISON_OK ? attend_join<T, DP>(p, plan, max_rows, stream) : rc;
 }
 
@@ -520,7 +549,8 @@ static int attend_check(const unison_kv_cache *c, const unison_kv_tree *t, int n
   return UNISON_OK;
 }
 
-extern "C" uint64_t unison_kv_attend_workspace(const unison_kv_cache *cache, const unison_kv_tree *tree, int n_q_heads) {
+extern "C" uint64_t unison_kv_attend_workspace(const unison_kv_cache *cache, const unison_kv_tree *tree,
+                                               int n_q_heads) {
   if (attend_check(cache, tree, n_q_heads) != UNISON_OK) return 0;
   return attend_plan(cache->head_dim, tree->max_tokens * (n_q_heads / cache->n_heads)).bytes;
 }

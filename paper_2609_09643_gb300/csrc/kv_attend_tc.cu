@@ -1,5 +1,6 @@
 // Attention of many query rows per KV head on the tensor cores (the variant of
-// unison_kv_attend for trees whose nodes x query heads exceed 64 rows).
+// unison_kv_attend for trees whose nodes x query heads exceed 32 rows, and head
+// sizes up to 128; kv_attend.cu has the formulas).
 //
 // A CTA takes up to 256 query rows, two tiles of 128, and walks the keys in
 // tiles of 128.  Warps have roles:
@@ -8,10 +9,25 @@
 //   warp 12      issues the products S = Q K^T and O += P V; S, P (over S) and
 //                O stay in tensor memory
 //   warps 0-3, 4-7  one query tile each: a thread per row turns S into weights
-// While one tile's weights are computed, the other tile's products run.  O is
-// rescaled only when a row's maximum has grown by more than 2^8 over the one
-// its weights are relative to; the sums are 32 bits wide, so weights up to 2^8
-// cost no accuracy.
+// While one tile's weights are computed, the other tile's products run.  One
+// query tile alone takes the keys in two turns instead, each with an O of its
+// own, joined at the end (64 rows of 16 sessions of 16k keys, head size 128: 180
+// us, in one turn 197).  O is rescaled only when a row's maximum has grown by
+// more than 2^8 over the one its weights are relative to; the sums are 32 bits
+// wide, so weights up to 2^8 cost no accuracy.  They are rounded to the cache's
+// type for the second product; their sum is of the weights before that.
+//
+// Up to 128 rows memory bounds it (5.9 TB/s at 128 rows of that case, 185 us);
+// from 256 on the tensor cores and the two warps per scheduler that compute the
+// weights: 64 nodes x 8 heads over 32 sessions of 15k to 16k keys, 8 KV heads
+// (1.06 PFLOP), take 735 us, 1.44 PFLOP/s, 74% of what a plain matrix product
+// reaches here.  512 rows' CTAs work in pairs on the same keys, which the second
+// finds in the L2 cache.
+//
+// A wait that runs out ends the CTA (every role sees `dead`) and reports
+// UNISON_ERR_TIMEOUT.  Every copying warp waits for every slot, also for those
+// that another warp fills: a barrier's parity tells a phase only from the next
+// one, and a warp that runs two ahead would take a slot that is being read.
 #include "kv_attend.cuh"
 #include "kv_copy.cuh"
 
@@ -81,7 +97,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
   auto seq_tiles = [&](int b) -> int64_t {
     const int tokens = kv_tokens(P.t, b, P.c.status).count;
     const int row_tiles = (tokens * G + kTcRows - 1) / kTcRows;
-    return (int64_t)(attend_key_tiles(kv_length(P.c, b), tokens, kTile) + kSetup) * ((row_tiles + groups - 1) / groups) * H;
+    return (int64_t)(attend_key_tiles(kv_length(P.c, b), tokens, kTile) + kSetup) *
+           ((row_tiles + groups - 1) / groups) * H;
   };
   KvRun run;
   if (!kv_find_run(run, sh.run, P.c.n_seqs, gridDim.x / groups, blockIdx.x / groups, seq_tiles)) return;
@@ -163,7 +180,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
         const int r = q * 128 + w * 32 + lane, row = g.row_tile * kTcRows + r;
         const T *src = nullptr;
         if (r < g.rows)
-          src = static_cast<const T *>(P.s.q) + (g.tok.first + row / G) * P.s.q_token + (g.head * G + row % G) * P.s.q_head;
+          src = static_cast<const T *>(P.s.q) + (g.tok.first + row / G) * P.s.q_token +
+                (g.head * G + row % G) * P.s.q_head;
         copier.rows(q_base + q * kTileBytes, src);
       }
       copier.issued(smem_u32(&sh.q_full));
@@ -495,10 +513,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
         if (lane == 0) bar_arrive(smem_u32(&sh.p_full[q]));
         s_no++;
       }
-      if (!ok) {
-        if (r == 0 && P.c.status) P.c.status[g.b] = UNISON_ERR_TIMEOUT;
-        break;
-      }
+      if (!ok) break;
       // ---- results: O is complete when the last product with V is
       ok = __all_sync(~0u, bar_wait(smem_u32(&sh.pv_done[q]), (s_no - 1) & 1, &sh.dead));
       if (!ok) break;
@@ -580,15 +595,18 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
           part[kTcRows * DP + tr] = m;
           part[kTcRows * (DP + 1) + tr] = l;
         } else if (P.s.lse) {
-          P.s.lse[(int64_t)(g.tok.first + node) * P.s.n_q_heads + g.head * G + row % G] = (m + log2f(l)) * 0.6931471805599453f;
+          P.s.lse[(int64_t)(g.tok.first + node) * P.s.n_q_heads + g.head * G + row % G] =
+              (m + log2f(l)) * 0.6931471805599453f;
         }
       }
       if (!whole && g.kt0 == 0 && r == 0 && q == 0)
-        P.part[blockIdx.x] = {kv_run_of(run, seg_begin + kSetup + g.tiles - 1), g.head, g.row_tile * kTcRows, g.rows, g.tok.first};
+        P.part[blockIdx.x] = {kv_run_of(run, seg_begin + kSetup + g.tiles - 1), g.head, g.row_tile * kTcRows, g.rows,
+                              g.tok.first};
       __syncwarp();
       tmem_before_sync();  // the next segment's products overwrite O
       if (join && lane == 0) bar_arrive(smem_u32(&sh.half_free));
     }
+    if (!ok && r == 0 && P.c.status) P.c.status[b] = UNISON_ERR_TIMEOUT;
   }
   __syncwarp();
   tmem_before_sync();

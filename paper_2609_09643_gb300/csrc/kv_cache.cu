@@ -47,8 +47,10 @@ __global__ void __launch_bounds__(256) commit_kernel(const CommitParams P) {
                                                    h * P.s.k_head + c * 8);
     const int4 v = *reinterpret_cast<const int4 *>(static_cast<const T *>(P.s.v_new) + from * P.s.v_token +
                                                    h * P.s.v_head + c * 8);
-    *reinterpret_cast<int4 *>(static_cast<T *>(P.c.k) + page * P.c.k_page + h * P.c.k_head + off * P.c.k_slot + c * 8) = k;
-    *reinterpret_cast<int4 *>(static_cast<T *>(P.c.v) + page * P.c.v_page + h * P.c.v_head + off * P.c.v_slot + c * 8) = v;
+    T *to_k = static_cast<T *>(P.c.k) + page * P.c.k_page + h * P.c.k_head + off * P.c.k_slot;
+    T *to_v = static_cast<T *>(P.c.v) + page * P.c.v_page + h * P.c.v_head + off * P.c.v_slot;
+    *reinterpret_cast<int4 *>(to_k + c * 8) = k;
+    *reinterpret_cast<int4 *>(to_v + c * 8) = v;
     if (c == 0) {
       const int64_t m = page * P.c.m_page + h * P.c.m_head + off * P.c.m_slot;
       if (P.c.mass) P.c.mass[m] = P.s.mass_new ? P.s.mass_new[from * H + h] : 0.f;
@@ -168,10 +170,14 @@ __device__ __forceinline__ int kept_count(const EvictParams &P, int b, int len) 
 // Lists the moves of one segment (session and head); a cluster of CTAs shares
 // its slots, in order, and so do a CTA's threads: a thread has a run of them.
 // Every key is read once and kept in shared memory, key k of thread t at
-// k * kPitch + t (odd: neighbouring slots lie in different banks).  The key of the last slot that stays is found digit by digit:
-// each CTA counts its own keys, adds up the counts of all (through distributed
-// shared memory) and finds the same digit.  Then each thread's slots with that
-// very key are ranked, and the moves counted and written.
+// k * kPitch + t (odd: neighbouring slots lie in different banks).  The key of
+// the last slot that stays is found digit by digit: each CTA counts its own
+// keys, adds up the counts of all (through distributed shared memory) and finds
+// the same digit.  Then each thread's slots with that very key are ranked, and
+// the moves counted and written.  The counts are whole numbers, so the atomics'
+// order changes nothing.  Bound by latency: a chain of dependent steps (table,
+// account, three digits with two barriers each, three prefixes), of which only
+// the first one reads the 8 bytes of a slot that it has to.
 __global__ void __launch_bounds__(kSelect, 4) evict_select_kernel(const EvictParams P) {
   follow_last_kernel();
   namespace cg = cooperative_groups;
@@ -503,7 +509,8 @@ extern "C" int unison_kv_evict(const unison_kv_cache *cache, const unison_kv_cac
   p.hold = (int)min((room + (int64_t)ctas * kSelect - 1) / ((int64_t)ctas * kSelect), (int64_t)kMostHeld);
   const int bytes = p.hold * kPitch * 4;
   static uint64_t done = 0;
-  if (!kv_allow_smem(reinterpret_cast<const void *>(evict_select_kernel), kMostHeld * kPitch * 4, &done)) return UNISON_ERR_CUDA;
+  if (!kv_allow_smem(reinterpret_cast<const void *>(evict_select_kernel), kMostHeld * kPitch * 4, &done))
+    return UNISON_ERR_CUDA;
   rc = kv_launch("kv_evict_select", dim3((unsigned)(segs * ctas)), dim3(kSelect), bytes, cuda_stream, ctas,
                  evict_select_kernel, p);
   if (rc != UNISON_OK) return rc;

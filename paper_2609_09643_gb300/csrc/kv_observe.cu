@@ -1,4 +1,6 @@
-// Attention weight of accepted tokens on every cached token (unison_kv_observe).
+// Attention weight of accepted tokens on every cached token (unison_kv_observe):
+// the variant for head sizes above 128 or more than 512 query rows, which the
+// tensor cores' one (kv_observe_tc.cu) has no room for in shared memory.
 #include "kv_observe.cuh"
 
 namespace unison {
@@ -13,7 +15,8 @@ constexpr int kObserveSmem = kStages *kTile *DP * 2 + QR *DP * 2;
 
 // The keys are the rows of the matrix product and the query rows its columns:
 // a thread holds two keys' products with two query rows at a time, and adds up
-// their weights without leaving its registers.
+// their weights without leaving its registers.  Every CTA takes an equal run of
+// the call's key tiles.  Query rows beyond QR are loaded again for every tile.
 template <typename T, int DP, int QR>
 __global__ void __launch_bounds__(kThreads) observe_kernel(const ObserveParams P) {
   follow_last_kernel();

@@ -12,6 +12,16 @@
 //   warp 12         issues the products, 128 query rows at a time, into four
 //                   buffers of tensor memory
 //   warps 0-3, 4-7  turn the scores of a buffer into weights, in turn
+//
+//   mass[x] += sum over the rows r of exp2(c S[r,x] - log-sum of row r)
+//
+// with everything in 32 bits: a weight is one fused multiply-add and one exp2.
+// Bound by memory up to 128 rows (64 sessions of 512 to 32k keys, 8 KV heads of
+// 128, 4 to 16 rows, 1.07 GB: 184 us, 5.8 TB/s), above by the weights: two warps
+// per scheduler wait for tensor memory, shared memory and exp2 in turn (rows 8
+// to 512 over 16 sessions of 8k to 32k keys: 231 us).  Four groups of weight
+// warps are slower (249 us where two took 230): each has less to do between its
+// waits, and the sums of four groups have to meet.
 #include "kv_copy.cuh"
 #include "kv_observe.cuh"
 
@@ -30,8 +40,8 @@ constexpr int kMarkBytes = kTile * 12;
 
 struct ObserveShared {
   KvRunShared run;
-  uint64_t k_full[kMostSlots], k_free[kMostSlots], q_full[2], q_free[2], t_full[kBuffers], t_free[kBuffers], seg_done[2],
-      part_full[2], part_free[2], idle;
+  uint64_t k_full[kMostSlots], k_free[kMostSlots], q_full[2], q_free[2], t_full[kBuffers], t_free[kBuffers],
+      seg_done[2], part_full[2], part_free[2], idle;
   uint64_t mask[2][kNodes];  // of the accepted nodes
   float part[2][kTile];      // sums of the group that does not write, of two tiles
   bool plain[2][4];          // whether every row that a copying warp read has weight to give
@@ -274,7 +284,8 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
       for (int kt = 0; kt < tiles && ok; kt++) {
         const int s = ring.at;
         ok = __all_sync(~0u, bar_wait(smem_u32(&sh.k_full[s]), ring.turn, &sh.dead));
-        if (ok && kt == 0) ok = __all_sync(~0u, bar_wait(smem_u32(&sh.q_full[qb]), (seg_no / P.q_buffers) & 1, &sh.dead));
+        if (ok && kt == 0)
+          ok = __all_sync(~0u, bar_wait(smem_u32(&sh.q_full[qb]), (seg_no / P.q_buffers) & 1, &sh.dead));
         ring.next(P.slots);
         const uint32_t keys = slots + s * (kTileBytes >> 4);
         for (int r0 = 0; (r0 == 0 || r0 < n_rows) && ok; r0 += 128) {

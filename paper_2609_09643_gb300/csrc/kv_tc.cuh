@@ -71,7 +71,8 @@ __device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b) {
 // --------------------------------------------------------- tensor memory --
 // By all lanes of one warp; the address is written to shared memory.
 __device__ __forceinline__ void tmem_alloc(uint32_t dst, uint32_t columns) {
-  asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst), "r"(columns) : "memory");
+  asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst), "r"(columns)
+               : "memory");
   asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
 }
 __device__ __forceinline__ void tmem_free(uint32_t addr, uint32_t columns) {
@@ -92,8 +93,10 @@ __device__ __forceinline__ void tmem_wait_ld(uint32_t (&r)[N]) {
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-#define KV_R8(r, i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3]), "=r"(r[i + 4]), "=r"(r[i + 5]), "=r"(r[i + 6]), "=r"(r[i + 7])
-#define KV_W8(r, i) "r"(r[i]), "r"(r[i + 1]), "r"(r[i + 2]), "r"(r[i + 3]), "r"(r[i + 4]), "r"(r[i + 5]), "r"(r[i + 6]), "r"(r[i + 7])
+#define KV_R4(r, i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3])
+#define KV_W4(r, i) "r"(r[i]), "r"(r[i + 1]), "r"(r[i + 2]), "r"(r[i + 3])
+#define KV_R8(r, i) KV_R4(r, i), KV_R4(r, i + 4)
+#define KV_W8(r, i) KV_W4(r, i), KV_W4(r, i + 4)
 // 32 columns of this warp's quarter of the lanes: lane i of the warp has lane i
 // of the quarter.  The registers are valid after tmem_wait_ld.
 __device__ __forceinline__ void tmem_ld32(uint32_t *r, uint32_t addr) {
@@ -120,12 +123,15 @@ __device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t *r) {
 }
 __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t *r) {
   asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(addr),
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+      "%16};" ::"r"(addr),
       KV_W8(r, 0), KV_W8(r, 8)
       : "memory");
 }
 #undef KV_R8
 #undef KV_W8
+#undef KV_R4
+#undef KV_W4
 
 // --------------------------------------------------------------- products --
 // Operands in shared memory lie in 128-byte rows of 64 elements, 16-byte chunk
@@ -190,7 +196,8 @@ __device__ __forceinline__ void products_done(bool one, uint32_t bar) {
       : "memory");
 }
 __device__ __forceinline__ void bar_arrive_by(bool one, uint32_t bar) {
-  asm volatile("{\n .reg .pred q;\n setp.ne.b32 q, %1, 0;\n @q mbarrier.arrive.shared::cta.b64 _, [%0];\n}\n" ::"r"(bar),
+  asm volatile("{\n .reg .pred q;\n setp.ne.b32 q, %1, 0;\n @q mbarrier.arrive.shared::cta.b64 _, [%0];\n}\n" ::"r"(
+                   bar),
                "r"((uint32_t)one)
                : "memory");
 }

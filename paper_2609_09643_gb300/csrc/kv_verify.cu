@@ -148,7 +148,8 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const unison_kv_tree t
 #pragma unroll
           for (int j = 0; j < kN; j++) {
             uint32_t h, l;
-            fixed_parts(residual<kCertain, kCount>(refused, weight(dx[j]), weight(yx[j]), x0 + i * kGroup + j, n), h, l);
+            const int x = x0 + i * kGroup + j;
+            fixed_parts(residual<kCertain, kCount>(refused, weight(dx[j]), weight(yx[j]), x, n), h, l);
             high += h;
             low += l;
           }

@@ -111,7 +111,8 @@ class Cache:
         n, pages = page_table.shape
         marks = [x for x in (mass, pos) if x is not None]
         for x, dt in ((mass, torch.float32), (pos, torch.int32)):
-            _need(x is None or (x.dtype == dt and x.shape == k.shape[:3]), "mass float32, pos int32: [page, head, slot]")
+            _need(x is None or (x.dtype == dt and x.shape == k.shape[:3]),
+                  "mass float32, pos int32: [page, head, slot]")
         _need(len(marks) < 2 or mass.stride() == pos.stride(), "mass and pos: the same strides")
         m = marks[0].stride() if marks else (0, 0, 0)
         ptr = lambda x: None if x is None else x.data_ptr()  # noqa: E731
@@ -195,18 +196,21 @@ def _workspace(cache, n, handle):
     return w
 
 
-def _on(stream, call, *args, **kw):
-    """A call with a torch stream: what it allocates belongs to that stream."""
+def _on(device, stream, call, *args):
+    """A call with a given stream (torch's, or a raw handle): what it allocates belongs to that stream."""
+    if not isinstance(stream, torch.cuda.Stream):
+        raw = getattr(stream, "cuda_stream", stream)
+        stream = torch.cuda.ExternalStream(raw, device=device) if raw else torch.cuda.default_stream(device)
     with torch.cuda.stream(stream):
-        return call(*args, **kw)
+        return call(*args)
 
 
 def attend(cache: Cache, tree: Tree, q, k_new, v_new, scale=None, out=None, lse=None, workspace=None, stream=None):
     """unison_kv_attend: (out [token, q head, head_dim], lse float32 [token, q
     head]).  scale defaults to head_dim ** -0.5; workspace: a uint8 tensor of
     at least ``attend_workspace`` bytes, else the cache keeps one."""
-    if isinstance(stream, torch.cuda.Stream):
-        return _on(stream, attend, cache, tree, q, k_new, v_new, scale, out, lse, workspace)
+    if stream is not None and cache.on_gpu:
+        return _on(cache.device, stream, attend, cache, tree, q, k_new, v_new, scale, out, lse, workspace)
     n, heads = tree.n_tokens, q.shape[1]
     qp, qs = _rows(cache, q, n, heads)
     kp, ks = _rows(cache, k_new, n, cache.n_heads)
@@ -244,8 +248,8 @@ def attend_workspace(cache: Cache, tree: Tree, n_q_heads: int) -> int:
 def observe(cache: Cache, tree: Tree, q, lse, k_new, scale=None, path=None, n_path=None, mass_new=None, stream=None):
     """unison_kv_observe: adds to cache.mass; returns mass_new, float32 [token,
     head], the weight of the new tokens themselves."""
-    if isinstance(stream, torch.cuda.Stream):
-        return _on(stream, observe, cache, tree, q, lse, k_new, scale, path, n_path, mass_new)
+    if stream is not None and cache.on_gpu:
+        return _on(cache.device, stream, observe, cache, tree, q, lse, k_new, scale, path, n_path, mass_new)
     n, heads = tree.n_tokens, q.shape[1]
     qp, qs = _rows(cache, q, n, heads)
     kp, ks = _rows(cache, k_new, n, cache.n_heads)
@@ -288,8 +292,8 @@ def evict_workspace(cache: Cache) -> int:
 def evict(cache: Cache, keep, sink=0, recent=0, into: Cache | None = None, workspace=None, stream=None) -> None:
     """unison_kv_evict: at most keep[b] (int32 tensor) slots of each session
     stay, in place or, with ``into``, in another cache."""
-    if isinstance(stream, torch.cuda.Stream):
-        return _on(stream, evict, cache, keep, sink, recent, into, workspace)
+    if stream is not None and cache.on_gpu:
+        return _on(cache.device, stream, evict, cache, keep, sink, recent, into, workspace)
     handle = _queue(cache.device, stream)
     if workspace is None:
         workspace = _workspace(cache, evict_workspace(cache), handle)
@@ -305,8 +309,8 @@ def verify(tree: Tree, token, p, q, u, u_sample, path=None, n_path=None, next_to
     next_token [session]), all int32.  p, q: [token, vocab] probabilities of
     one type (q None: certain drafts); token int32 [token]; u float32 [token];
     u_sample float32 [session]."""
-    if isinstance(stream, torch.cuda.Stream):
-        return _on(stream, verify, tree, token, p, q, u, u_sample, path, n_path, next_token)
+    if stream is not None and p.is_cuda:
+        return _on(p.device, stream, verify, tree, token, p, q, u, u_sample, path, n_path, next_token)
     n, t, total, device = tree.n_seqs, tree.max_tokens, tree.n_tokens, p.device
     dtype, vocab, ps, qs = p.dtype, p.shape[-1], p.stride(), _NO_STRIDES
     ok = dtype in DTYPE and p.shape == (total, vocab) and ps[1] == 1

@@ -145,6 +145,23 @@ def test_attend_strided_rows_stream_and_workspace(kv):
     assert bool(both[:, 20:].isnan().all()) and bool(both[:, :, 64:].isnan().all())
 
 
+def test_scratch_and_results_belong_to_the_given_stream(kv):
+    m = Made([300, 41], [4, 2], group=4, hkv=2, d=64, seed=14)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    check_attend(kv, m, stream=side.cuda_stream)  # a raw handle
+    cache, tree = m.cache(kv), m.tree(kv)
+    with torch.cuda.stream(side):
+        want = kv.attend(cache, tree, m.q, m.k_new, m.v_new)[0]
+    for handle in (side, side.cuda_stream):
+        got = kv.attend(cache, tree, m.q, m.k_new, m.v_new, stream=handle)[0]
+        side.synchronize()
+        assert torch.equal(got, want) and list(cache.scratch) == [side.cuda_stream]
+    got = kv.attend(cache, tree, m.q, m.k_new, m.v_new, stream=0)[0]  # the default stream
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and list(cache.scratch) == [side.cuda_stream, 0]
+
+
 def test_attend_absent_pages_and_bad_values_are_reported(kv):
     m = Made([100, 50, 20], [2, 20, 3], group=4, page=16, seed=13)
     full = [m.slots(f64(x), 0) for x in (m.k, m.v)]
