@@ -15,7 +15,9 @@ struct CommitParams {
   unison_kv_path path;
 };
 
-// One CTA per session; a thread moves 16 bytes at a time.
+// One CTA per session; a thread moves 16 bytes at a time.  Bound by latency (two
+// dependent look-ups and a copy): 5 us for 64 sessions of up to eight tokens, 8
+// KV heads of 128.
 template <typename T>
 __global__ void __launch_bounds__(256) commit_kernel(const CommitParams P) {
   follow_last_kernel();
@@ -177,7 +179,8 @@ __device__ __forceinline__ int kept_count(const EvictParams &P, int b, int len) 
 // the moves counted and written.  The counts are whole numbers, so the atomics'
 // order changes nothing.  Bound by latency: a chain of dependent steps (table,
 // account, three digits with two barriers each, three prefixes), of which only
-// the first one reads the 8 bytes of a slot that it has to.
+// the first one reads the 8 bytes of a slot that it has to.  64 sessions x 8
+// heads of 4,100 slots: 17 us; 16 x 8 of 8k to 32k: 35 us.
 __global__ void __launch_bounds__(kSelect, 4) evict_select_kernel(const EvictParams P) {
   follow_last_kernel();
   namespace cg = cooperative_groups;
@@ -212,11 +215,24 @@ __global__ void __launch_bounds__(kSelect, 4) evict_select_kernel(const EvictPar
   const int first = (int)min(first64, (int64_t)len), last = (int)min(first64 + each * kSelect, (int64_t)len);
   const int begin = min(first + tid * each, last), mine = min(begin + each, last) - begin;
   const int held = P.hold;  // keys of a thread in shared memory
-  auto key_of = [&](int k) -> uint32_t {
-    if (k < held) return keys[k * kPitch + tid];
-    uint32_t x[1];
-    slot_keys<1>(P, b, h, begin + k, 0, last, next, x);
-    return x[0];
+  // f(k, key) for this thread's slots; the keys come from shared memory four at a time.
+  auto each_key = [&](auto f) {
+    int k = 0;
+    for (; k + 4 <= min(mine, held); k += 4) {
+      uint32_t x[4];
+#pragma unroll
+      for (int i = 0; i < 4; i++) x[i] = keys[(k + i) * kPitch + tid];
+#pragma unroll
+      for (int i = 0; i < 4; i++) f(k + i, x[i]);
+    }
+    for (; k < mine; k++) {
+      uint32_t x[1] = {0};
+      if (k < held)
+        x[0] = keys[k * kPitch + tid];
+      else if (n < len)
+        slot_keys<1>(P, b, h, begin + k, 0, last, next, x);
+      f(k, x[0]);
+    }
   };
 
   uint32_t last_key = 0;  // of the slots that stay
@@ -258,27 +274,27 @@ __global__ void __launch_bounds__(kSelect, 4) evict_select_kernel(const EvictPar
     int shift = 21, bits = 11;
     for (int pass = 0;; pass++) {
       uint32_t *counts = hist[pass & 1];
-      auto count = [&](uint32_t x) {
+      each_key([&](int, uint32_t x) {
         if (pass == 0 || x >> (shift + bits) == last_key) atomicAdd(&counts[x >> shift & ((1u << bits) - 1)], 1u);
-      };
-      int k = 0;
-      for (; k + 4 <= min(mine, held); k += 4) {
-        uint32_t x[4];
-#pragma unroll
-        for (int i = 0; i < 4; i++) x[i] = keys[(k + i) * kPitch + tid];
-#pragma unroll
-        for (int i = 0; i < 4; i++) count(x[i]);
-      }
-      for (; k < mine; k++) count(key_of(k));
+      });
       sync();
       // eight bins a thread, from the top: thread 0 has the highest
       const int bin = kBins - 8 - 8 * tid;
       uint32_t of[8] = {0, 0, 0, 0, 0, 0, 0, 0}, sum = 0;
-      for (int c = 0; c < ctas; c++) {
-        const uint4 *theirs = reinterpret_cast<const uint4 *>(cluster.map_shared_rank(counts, c) + bin);
-        const uint4 x = theirs[1], y = theirs[0];
-        of[0] += x.w, of[1] += x.z, of[2] += x.y, of[3] += x.x;
-        of[4] += y.w, of[5] += y.z, of[6] += y.y, of[7] += y.x;
+      for (int c0 = 0; c0 < ctas; c0 += 4) {
+        uint4 x[4], y[4];
+#pragma unroll
+        for (int c = 0; c < 4; c++) {
+          const uint4 *theirs =
+              reinterpret_cast<const uint4 *>(cluster.map_shared_rank(counts, min(c0 + c, ctas - 1)) + bin);
+          x[c] = theirs[1], y[c] = theirs[0];
+        }
+#pragma unroll
+        for (int c = 0; c < 4; c++) {
+          if (c0 + c >= ctas) break;
+          of[0] += x[c].w, of[1] += x[c].z, of[2] += x[c].y, of[3] += x[c].x;
+          of[4] += y[c].w, of[5] += y[c].z, of[6] += y[c].y, of[7] += y[c].x;
+        }
       }
 #pragma unroll
       for (int i = 0; i < 8; i++) sum += of[i];
@@ -334,23 +350,22 @@ __global__ void __launch_bounds__(kSelect, 4) evict_select_kernel(const EvictPar
   };
   uint32_t tie = 0, none = 0, all, more;
   if (ties) {
-    for (int k = 0; k < mine; k++) tie += key_of(k) == last_key;
+    each_key([&](int, uint32_t x) { tie += x == last_key; });
     prefix(tie, none, all, more);
   }
-  auto stays = [&](int k, uint32_t &rank) {
+  auto stays = [&](uint32_t x, uint32_t &rank) {
     if (n == len) return true;
-    const uint32_t x = key_of(k);
     if (ties && x == last_key) return rank++ < ties;
     return x > last_key;
   };
   // (the first 32 slots of a thread are remembered: most sessions have no more)
   uint32_t targets = 0, sources = 0, r = tie, moves = 0;
-  for (int k = 0; k < mine; k++) {
-    const bool stay = stays(k, r), low = P.in_place && begin + k < n;
+  each_key([&](int k, uint32_t x) {
+    const bool stay = stays(x, r), low = P.in_place && begin + k < n;
     targets += P.in_place && low && !stay;
     sources += stay && !low;
     if (k < 32 && stay != low) moves |= 1u << k;
-  }
+  });
   prefix(targets, sources, all, more);
   if (rank == 0 && tid == 0) P.count[seg] = (int)(P.in_place ? min(all, more) : more);
   auto write = [&](int k, bool stay) {
@@ -365,15 +380,18 @@ __global__ void __launch_bounds__(kSelect, 4) evict_select_kernel(const EvictPar
   }
   if (mine > 32) {
     r = tie;
-    for (int k = 0; k < mine; k++) {
-      const bool stay = stays(k, r), low = P.in_place && begin + k < n;
+    each_key([&](int k, uint32_t x) {
+      const bool stay = stays(x, r), low = P.in_place && begin + k < n;
       if (k >= 32 && stay != low) write(k, stay);
-    }
+    });
   }
 }
 
 // Moves the listed slots: keys, values, mass and position.  A warp looks up 32
-// moves at once, a lane each, and then copies them row by row.
+// moves at once, a lane each, and then copies them row by row, eight loads of 16
+// bytes of a lane on their way.  Bound by memory where many slots move (16
+// sessions' 8,192 slots into another cache, 8 KV heads of 128: 1.09 GB in 175 us,
+// 6.2 TB/s), by latency where few do (6 us).
 template <typename T>
 __global__ void __launch_bounds__(256) evict_move_kernel(const EvictParams P) {
   follow_last_kernel();
@@ -501,9 +519,11 @@ extern "C" int unison_kv_evict(const unison_kv_cache *cache, const unison_kv_cac
               kv_aligned(cache->mass, 16) && kv_aligned(cache->pos, 16);
   p.moves = static_cast<int32_t *>(workspace);
   p.count = p.moves + segs * room;
-  // CTAs per segment: as many as the segments leave room for (four CTAs on a
-  // multiprocessor), none with less than 2,048 slots.
-  const int64_t spare = (int64_t)kv_sm_count() * 4 / (int64_t)segs;
+  // CTAs per segment: as many as the segments leave room for (two CTAs on a
+  // multiprocessor, though four fit: clusters then wait for places; of sessions
+  // of 8k to 32k slots 64 segments take 33 us against 73, 128 take 39 against 45,
+  // and one CTA each 35 and 53), none with less than 2,048 slots.
+  const int64_t spare = (int64_t)kv_sm_count() * 2 / (int64_t)segs;
   int ctas = 1;
   while (ctas < kMaxCluster && ctas * 2 <= spare && (int64_t)ctas * 2048 < room) ctas *= 2;
   p.hold = (int)min((room + (int64_t)ctas * kSelect - 1) / ((int64_t)ctas * kSelect), (int64_t)kMostHeld);

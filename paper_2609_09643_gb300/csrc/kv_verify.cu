@@ -7,6 +7,12 @@
 // has a run of the vocabulary, each of its warps a run of that.  A pass over
 // the rows is one stream of loads, one exchange of the CTAs' sums and one
 // cluster barrier.
+//
+// Bound by the chain of passes: each refusal wants the sum that the last one
+// left, and a session's next pass cannot begin before.  128 sessions' trees of 32
+// nodes over 128,000 entries of 32 bits (one to four passes mostly, from the L2
+// cache after the first): 63 us, while reading every row that is wanted once
+// would take 19.  One session's chain of five over 32,000 entries: 6 us.
 #include <cooperative_groups.h>
 
 #include <type_traits>
