@@ -368,16 +368,22 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
             }
           }
           // the others 16 at a time, each with the question whether it counts
-          int node = last ? (i * 128 + r0) / G : 0, head = i * 128 + r0 - node * G;
+          const int node = (i * 128 + r0) / G;
+          int head = i * 128 + r0 - node * G;
+          uint64_t sees = 0;  // the accepted nodes from this one on that see this new token
+          if (last && key < 64) {
+            for (int j = 0; j < kNodes; j++) sees |= (mask[j] >> key & 1) << j;
+            sees >>= min(node, kNodes - 1);
+          }
 #pragma unroll 1
           for (; r0 < n; r0 += 16) {
             uint32_t v[16], counts = n - r0 < 16 ? (1u << (n - r0)) - 1 : ~0u;
             tmem_ld16(v, from + r0);
             if (last) {
-#pragma unroll 1
+#pragma unroll
               for (int j = 0; j < 16; j++) {
-                if (node >= kNodes || key >= 64 || !(mask[node] >> key & 1)) counts &= ~(1u << j);
-                if (++head == G) head = 0, node++;
+                if (!(sees & 1)) counts &= ~(1u << j);
+                if (++head == G) head = 0, sees >>= 1;
               }
             }
             __syncwarp();
