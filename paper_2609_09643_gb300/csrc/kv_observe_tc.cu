@@ -17,11 +17,14 @@
 //
 // with everything in 32 bits: a weight is one fused multiply-add and one exp2.
 // Bound by memory up to 128 rows (64 sessions of 512 to 32k keys, 8 KV heads of
-// 128, 4 to 16 rows, 1.07 GB: 184 us, 5.8 TB/s), above by the weights: two warps
-// per scheduler wait for tensor memory, shared memory and exp2 in turn (rows 8
-// to 512 over 16 sessions of 8k to 32k keys: 231 us).  Four groups of weight
-// warps are slower (249 us where two took 230): each has less to do between its
-// waits, and the sums of four groups have to meet.
+// 128, 4 to 16 rows, 1.07 GB: 180 us, 5.9 TB/s), above by the warps that turn
+// scores into weights (rows 8 to 512 over 16 sessions of 8k to 32k keys: 209 us).
+// They take 1,000 cycles for a chunk of 128 x 128: 622 with nothing but the loads
+// and two warps per scheduler (exp2 at 32 a cycle: 512), the rest between chunks
+// and tiles (barriers, the sums' exchange).  So what is asked once a segment is
+// not asked once a chunk (512 rows took 328 us then).  Not faster: four groups
+// of weight warps (249 us where two took 230), scores read as matrix fragments
+// so that a log-sum serves four weights, the next scores on their way meanwhile.
 #include "kv_copy.cuh"
 #include "kv_observe.cuh"
 
@@ -77,12 +80,12 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
   // A tile's share of the run, in units of 33 ns: its keys' way here, or the
   // products and weights of its chunks of 128 query rows, where those take
   // longer.  (16 sessions of 16k keys, 8 KV heads, head size 128: 115 us with 8
-  // rows, 126 with 128, 174 with 136, 188 with 256, 258 with 384, 328 with 512;
-  // head size 64: 83, 102, 164, 178, 252, 312.  Beside sessions of many rows,
+  // rows, 121 with 128, 154 with 136, 166 with 256, 221 with 384, 279 with 512;
+  // head size 64: 82, 88, 145, 160, 209, 258.  Beside sessions of many rows,
   // which leave them the memory, few rows take a fifth less.)
   const int keys_way = DP == 64 ? 20 : P.slots > 2 || P.k_boxes.rows > 8 ? 26 : P.k_boxes.rows ? 40 : 80;
   auto share = [&](int rows) {
-    return rows <= 128 ? keys_way + rows / 32 : max(keys_way, 16 + 9 * ((rows + 127) / 128) + rows / 14);
+    return rows <= 128 ? keys_way + rows / 32 : max(keys_way, 14 + 11 * ((rows + 127) / 128) + rows / 25);
   };
   // A head's beginning (its query rows, an empty pipeline) and the tiles that are
   // not full, in tiles.
@@ -324,28 +327,31 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
       if (lane == 0) bar_arrive(smem_u32(&bar));
     };
     Ring marks;
-    int job = 0, seg_no = 0, tile_no = 0, shared_tiles = 0;
+    int jobs = 0, seg_no = 0, tile_no = 0, shared_tiles = 0;
     bool ok = true;
     Segment g;
     while (ok && next_segment(g)) {
       const float *lse = lse_base + (seg_no & 1) * P.q_rows;
       const uint64_t *mask = sh.mask[seg_no & 1];
       const int chunks = max((g.rows + 127) / 128, 1);
+      int plain = -1;  // whether every row has weight to give, -1: not read yet
       for (int kt = g.kt0; kt < g.kt1; kt++, tile_no++, marks.next(P.slots + kMoreMarks)) {
         const bool last = kt == g.tiles - 1;
         // chunk by chunk in turn, beginning in turn where their number is odd
         const int first = chunks & 1 ? tile_no & 1 : 0;
         const bool writes = wg == first;
         uint64_t sum[2] = {0, 0};
-        for (int i = 0; i < chunks; i++, job++) {
-          if (((i + first) & 1) != wg) continue;
-          const int buf = job % kBuffers;
+        for (int i = wg ^ first; i < chunks; i += 2) {
+          const int job = jobs + i, buf = job % kBuffers;
           ok = __all_sync(~0u, bar_wait(smem_u32(&sh.t_full[buf]), (job / kBuffers) & 1, &sh.dead));
           if (!ok) break;
           tmem_after_sync();
           const int n = min(g.rows - i * 128, 128);
-          const bool *plain = sh.plain[seg_no & 1];
-          const bool checked = last || !(plain[0] && plain[1] && plain[2] && plain[3]);
+          if (plain < 0) {
+            const bool *all = sh.plain[seg_no & 1];
+            plain = all[0] && all[1] && all[2] && all[3];
+          }
+          const bool checked = last || !plain;
           const uint32_t from = tmem + buf * 128 + lanes;
           const float *l = lse + i * 128;
           int r0 = 0;
@@ -367,46 +373,49 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
               }
             }
           }
-          // the others 16 at a time, each with the question whether it counts
-          const int node = (i * 128 + r0) / G;
-          int head = i * 128 + r0 - node * G;
-          uint64_t sees = 0;  // the accepted nodes from this one on that see this new token
-          if (last && key < 64) {
-            for (int j = 0; j < kNodes; j++) sees |= (mask[j] >> key & 1) << j;
-            sees >>= min(node, kNodes - 1);
-          }
-#pragma unroll 1
-          for (; r0 < n; r0 += 16) {
-            uint32_t v[16], counts = n - r0 < 16 ? (1u << (n - r0)) - 1 : ~0u;
-            tmem_ld16(v, from + r0);
-            if (last) {
-#pragma unroll
-              for (int j = 0; j < 16; j++) {
-                if (!(sees & 1)) counts &= ~(1u << j);
-                if (++head == G) head = 0, sees >>= 1;
-              }
+          if (r0 < n) {
+            // the others 16 at a time, each with the question whether it counts
+            const int node = (i * 128 + r0) / G;
+            int head = i * 128 + r0 - node * G;
+            uint64_t sees = 0;  // the accepted nodes from this one on that see this new token
+            if (last && key < 64) {
+              for (int j = 0; j < kNodes; j++) sees |= (mask[j] >> key & 1) << j;
+              sees >>= min(node, kNodes - 1);
             }
-            __syncwarp();
-            tmem_wait_ld(v);
+#pragma unroll 1
+            for (; r0 < n; r0 += 16) {
+              uint32_t v[16], counts = n - r0 < 16 ? (1u << (n - r0)) - 1 : ~0u;
+              tmem_ld16(v, from + r0);
+              if (last) {
 #pragma unroll
-            for (int j = 0; j < 16; j += 4) {
-              const float4 y = *reinterpret_cast<const float4 *>(l + r0 + j);
-              float e[4] = {exp2_fast(fmaf(__uint_as_float(v[j]), c, y.x)),
-                            exp2_fast(fmaf(__uint_as_float(v[j + 1]), c, y.y)),
-                            exp2_fast(fmaf(__uint_as_float(v[j + 2]), c, y.z)),
-                            exp2_fast(fmaf(__uint_as_float(v[j + 3]), c, y.w))};
-              e[0] = (counts >> j & 1) && y.x != -INFINITY ? e[0] : 0.f;
-              e[1] = (counts >> (j + 1) & 1) && y.y != -INFINITY ? e[1] : 0.f;
-              e[2] = (counts >> (j + 2) & 1) && y.z != -INFINITY ? e[2] : 0.f;
-              e[3] = (counts >> (j + 3) & 1) && y.w != -INFINITY ? e[3] : 0.f;
-              sum[0] = add_pair(sum[0], pair(e[0], e[1]));
-              sum[1] = add_pair(sum[1], pair(e[2], e[3]));
+                for (int j = 0; j < 16; j++) {
+                  if (!(sees & 1)) counts &= ~(1u << j);
+                  if (++head == G) head = 0, sees >>= 1;
+                }
+              }
+              __syncwarp();
+              tmem_wait_ld(v);
+#pragma unroll
+              for (int j = 0; j < 16; j += 4) {
+                const float4 y = *reinterpret_cast<const float4 *>(l + r0 + j);
+                float e[4] = {exp2_fast(fmaf(__uint_as_float(v[j]), c, y.x)),
+                              exp2_fast(fmaf(__uint_as_float(v[j + 1]), c, y.y)),
+                              exp2_fast(fmaf(__uint_as_float(v[j + 2]), c, y.z)),
+                              exp2_fast(fmaf(__uint_as_float(v[j + 3]), c, y.w))};
+                e[0] = (counts >> j & 1) && y.x != -INFINITY ? e[0] : 0.f;
+                e[1] = (counts >> (j + 1) & 1) && y.y != -INFINITY ? e[1] : 0.f;
+                e[2] = (counts >> (j + 2) & 1) && y.z != -INFINITY ? e[2] : 0.f;
+                e[3] = (counts >> (j + 3) & 1) && y.w != -INFINITY ? e[3] : 0.f;
+                sum[0] = add_pair(sum[0], pair(e[0], e[1]));
+                sum[1] = add_pair(sum[1], pair(e[2], e[3]));
+              }
             }
           }
           tmem_before_sync();
           warp_arrive(sh.t_free[buf]);
         }
         if (!ok) break;
+        jobs += chunks;
         float all, other;
         unpair(add_pair(sum[0], sum[1]), all, other);
         all += other;
