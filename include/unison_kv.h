@@ -55,7 +55,7 @@ enum { UNISON_KV_BF16 = 0, UNISON_KV_FP16 = 1, UNISON_KV_FP32 = 2 };
  * Strides are in elements, of the page, head and slot axes; the head_dim axis
  * is contiguous.  k and v start on 16-byte boundaries, their strides are
  * multiples of 8.  head_dim: a multiple of 8, 8 .. 256; n_heads: KV heads;
- * dtype: UNISON_KV_BF16 or _FP16; page_size >= 1; max_pages * page_size < 2^31 - 64.
+ * dtype: UNISON_KV_BF16 or _FP16; page_size >= 1; max_pages * page_size < 2^31 - 2^16.
  * A call that does not use an array takes NULL for it. */
 typedef struct {
   void *k;

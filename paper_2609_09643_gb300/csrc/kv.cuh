@@ -26,7 +26,7 @@ inline int kv_check_cache(const unison_kv_cache *c) {
     return UNISON_ERR_RANGE;
   if (c->head_dim < 8 || c->head_dim > 256 || c->head_dim % 8) return UNISON_ERR_RANGE;
   if (c->dtype != UNISON_KV_BF16 && c->dtype != UNISON_KV_FP16) return UNISON_ERR_ARG;
-  if ((int64_t)c->max_pages * c->page_size >= (1ll << 31) - 64) return UNISON_ERR_RANGE;
+  if ((int64_t)c->max_pages * c->page_size >= (1ll << 31) - (1 << 16)) return UNISON_ERR_RANGE;  // tiles round up
   if (c->n_seqs > 0 && (!c->length || (c->max_pages > 0 && !c->page_table))) return UNISON_ERR_ARG;
   return UNISON_OK;
 }

@@ -82,11 +82,11 @@ def _need(ok, what):
         raise ValueError(what)
 
 
-def _dense(x, dtype, shape, what):
+def _dense(x, dtype, shape, what, device):
     if x is None:
         return None
-    if x.dtype is not dtype or x.shape != shape or not x.is_contiguous():
-        raise ValueError(f"{what}: a contiguous {dtype} tensor of shape {shape} is wanted")
+    if x.dtype is not dtype or x.shape != shape or not x.is_contiguous() or x.device != device:
+        raise ValueError(f"{what}: a contiguous {dtype} tensor of shape {shape} on {device} is wanted")
     return x.data_ptr()
 
 
@@ -106,13 +106,15 @@ class Cache:
     def __init__(self, k, v, page_table, length, mass=None, pos=None, next_pos=None, status=None):
         _need(k.dim() == 4 and k.shape == v.shape, "k, v: [page, head, slot, head_dim] of the same shape")
         _need(k.dtype == v.dtype and k.dtype in (torch.bfloat16, torch.float16), "k, v: bfloat16 or float16")
+        device = k.device
+        _need(v.device == device, "k, v: on one device")
         _need(k.stride(3) == 1 and v.stride(3) == 1, "k, v: the last axis is contiguous")
         _need(page_table.dim() == 2, "page_table: [session, page]")
         n, pages = page_table.shape
         marks = [x for x in (mass, pos) if x is not None]
         for x, dt in ((mass, torch.float32), (pos, torch.int32)):
-            _need(x is None or (x.dtype == dt and x.shape == k.shape[:3]),
-                  "mass float32, pos int32: [page, head, slot]")
+            _need(x is None or (x.dtype == dt and x.shape == k.shape[:3] and x.device == device),
+                  "mass float32, pos int32: [page, head, slot], on the device of k")
         _need(len(marks) < 2 or mass.stride() == pos.stride(), "mass and pos: the same strides")
         m = marks[0].stride() if marks else (0, 0, 0)
         ptr = lambda x: None if x is None else x.data_ptr()  # noqa: E731
@@ -121,10 +123,12 @@ class Cache:
         self.dtype, self.device, self.n_seqs, self.on_gpu = k.dtype, k.device, n, k.is_cuda
         self.n_heads, self.head_dim = k.shape[1], k.shape[3]
         self.struct = KvCache(
-            k.data_ptr(), v.data_ptr(), ptr(mass), ptr(pos), _dense(page_table, torch.int32, (n, pages), "page_table"),
-            _dense(length, torch.int32, (n,), "length"), _dense(next_pos, torch.int32, (n,), "next_pos"),
-            _dense(status, torch.int32, (n,), "status"), *k.stride()[:3], *v.stride()[:3], *m, n, pages, k.shape[0],
-            k.shape[2], k.shape[1], k.shape[3], DTYPE[k.dtype], 0)
+            k.data_ptr(), v.data_ptr(), ptr(mass), ptr(pos),
+            _dense(page_table, torch.int32, (n, pages), "page_table", device),
+            _dense(length, torch.int32, (n,), "length", device),
+            _dense(next_pos, torch.int32, (n,), "next_pos", device),
+            _dense(status, torch.int32, (n,), "status", device), *k.stride()[:3], *v.stride()[:3], *m, n, pages,
+            k.shape[0], k.shape[2], k.shape[1], k.shape[3], DTYPE[k.dtype], 0)
         self.address = C.addressof(self.struct)
         self.scale = self.head_dim ** -0.5
         self.sizes = {}    # bytes of workspace, by the call's sizes
@@ -144,9 +148,10 @@ class Tree:
         _need(n is not None, "n_tokens is wanted where neither mask nor parent tells it")
         self.tensors = (offsets, mask, parent)
         self.n_seqs, self.n_tokens, self.max_tokens = offsets.shape[0] - 1, n, max_tokens
-        self.struct = KvTree(_dense(offsets, torch.int32, (self.n_seqs + 1,), "offsets"),
-                             _dense(mask, torch.int64, (n,), "mask"), _dense(parent, torch.int32, (n,), "parent"),
-                             self.n_seqs, n, max_tokens, 0)
+        self.device = offsets.device
+        self.struct = KvTree(_dense(offsets, torch.int32, (self.n_seqs + 1,), "offsets", self.device),
+                             _dense(mask, torch.int64, (n,), "mask", self.device),
+                             _dense(parent, torch.int32, (n,), "parent", self.device), self.n_seqs, n, max_tokens, 0)
         self.address = C.addressof(self.struct)
 
 
@@ -163,8 +168,9 @@ _NO_STRIDES = (0, 0, 0)
 def _rows(cache, x, n, heads):
     """(pointer, strides) of a step's tensor [n, heads, head_dim] of the cache's type, its last axis contiguous."""
     s = x.stride()
-    if x.dtype is not cache.dtype or x.shape != (n, heads, cache.head_dim) or s[2] != 1:
-        raise ValueError(f"step tensors: {cache.dtype} [{n}, {heads}, {cache.head_dim}], last axis contiguous")
+    if x.dtype is not cache.dtype or x.shape != (n, heads, cache.head_dim) or s[2] != 1 or x.device != cache.device:
+        raise ValueError(f"step tensors: {cache.dtype} [{n}, {heads}, {cache.head_dim}] on {cache.device}, "
+                         "last axis contiguous")
     return x.data_ptr(), s
 
 
@@ -173,9 +179,15 @@ def _path(tree, path, n_path):
         return None
     s = path.stride()
     if path.dtype is not torch.int32 or path.dim() != 2 or path.shape[0] != tree.n_seqs or s[1] != 1 or \
-            path.shape[1] < tree.max_tokens:
-        raise ValueError("path: int32 [session, max_tokens]")
-    return _PATH.pack(path.data_ptr(), _dense(n_path, torch.int32, (tree.n_seqs,), "n_path"), s[0])
+            path.shape[1] < tree.max_tokens or path.device != tree.device:
+        raise ValueError("path: int32 [session, max_tokens] on the tree's device")
+    return _PATH.pack(path.data_ptr(), _dense(n_path, torch.int32, (tree.n_seqs,), "n_path", tree.device), s[0])
+
+
+def _on_gpu(cache, *others):
+    """The kernels follow pointers: none to the host, none to another device."""
+    if not cache.on_gpu and cache.n_seqs or any(x.device != cache.device for x in others if x is not None):
+        raise ValueError(f"cache, tree and workspace: on one CUDA device ({cache.device})")
 
 
 def _queue(device, stream):
@@ -222,7 +234,8 @@ def attend(cache: Cache, tree: Tree, q, k_new, v_new, scale=None, out=None, lse=
         lse = torch.empty(n, heads, dtype=torch.float32, device=cache.device)
         lp = lse.data_ptr()
     else:
-        lp = _dense(lse, torch.float32, (n, heads), "lse")
+        lp = _dense(lse, torch.float32, (n, heads), "lse", cache.device)
+    _on_gpu(cache, tree, workspace)
     handle = _queue(cache.device, stream)
     if workspace is None:
         workspace = _workspace(cache, attend_workspace(cache, tree, heads), handle)
@@ -253,13 +266,14 @@ def observe(cache: Cache, tree: Tree, q, lse, k_new, scale=None, path=None, n_pa
     n, heads = tree.n_tokens, q.shape[1]
     qp, qs = _rows(cache, q, n, heads)
     kp, ks = _rows(cache, k_new, n, cache.n_heads)
-    lp = _dense(lse, torch.float32, (n, heads), "lse")
+    lp = _dense(lse, torch.float32, (n, heads), "lse", cache.device)
+    _on_gpu(cache, tree)
     if mass_new is None:
         mass_new = torch.empty(n, cache.n_heads, dtype=torch.float32, device=cache.device)
     rc = lib().unison_kv_observe(
         cache.address, tree.address,
-        _STEP.pack(qp, kp, 0, 0, lp, _dense(mass_new, torch.float32, (n, cache.n_heads), "mass_new"), qs[0], qs[1],
-                   ks[0], ks[1], 0, 0, 0, 0, heads, cache.scale if scale is None else scale),
+        _STEP.pack(qp, kp, 0, 0, lp, _dense(mass_new, torch.float32, (n, cache.n_heads), "mass_new", cache.device),
+                   qs[0], qs[1], ks[0], ks[1], 0, 0, 0, 0, heads, cache.scale if scale is None else scale),
         _path(tree, path, n_path), _queue(cache.device, stream))
     if rc:
         binding._check("unison_kv_observe", rc)
@@ -272,7 +286,8 @@ def commit(cache: Cache, tree: Tree, k_new, v_new, mass_new=None, path=None, n_p
     n = tree.n_tokens
     kp, ks = _rows(cache, k_new, n, cache.n_heads)
     vp, vs = _rows(cache, v_new, n, cache.n_heads)
-    mp = _dense(mass_new, torch.float32, (n, cache.n_heads), "mass_new")
+    mp = _dense(mass_new, torch.float32, (n, cache.n_heads), "mass_new", cache.device)
+    _on_gpu(cache, tree)
     rc = lib().unison_kv_commit(
         cache.address, tree.address,
         _STEP.pack(0, kp, vp, 0, 0, mp or 0, 0, 0, ks[0], ks[1], vs[0], vs[1], 0, 0, 0, 0.0),
@@ -294,12 +309,13 @@ def evict(cache: Cache, keep, sink=0, recent=0, into: Cache | None = None, works
     stay, in place or, with ``into``, in another cache."""
     if stream is not None and cache.on_gpu:
         return _on(cache.device, stream, evict, cache, keep, sink, recent, into, workspace)
+    kp = _dense(keep, torch.int32, (cache.n_seqs,), "keep", cache.device)
+    _on_gpu(cache, into, workspace)
     handle = _queue(cache.device, stream)
     if workspace is None:
         workspace = _workspace(cache, evict_workspace(cache), handle)
-    rc = lib().unison_kv_evict(
-        cache.address, None if into is None else into.address, _dense(keep, torch.int32, (cache.n_seqs,), "keep"), sink,
-        recent, workspace.data_ptr(), workspace.numel(), handle)
+    rc = lib().unison_kv_evict(cache.address, None if into is None else into.address, kp, sink, recent,
+                               workspace.data_ptr(), workspace.numel(), handle)
     if rc:
         binding._check("unison_kv_evict", rc)
 
@@ -318,6 +334,8 @@ def verify(tree: Tree, token, p, q, u, u_sample, path=None, n_path=None, next_to
         qs = q.stride()
         ok = ok and q.dtype is dtype and q.shape == (total, vocab) and qs[1] == 1
     _need(ok, "p, q: [token, vocab] of one type, last axis contiguous")
+    _need(tree.device == device and (q is None or q.device == device) and (p.is_cuda or n == 0),
+          "p, q and the tree: on one CUDA device")
     if path is None:
         path = torch.empty(n, t, dtype=torch.int32, device=device)
     if n_path is None:
@@ -325,15 +343,16 @@ def verify(tree: Tree, token, p, q, u, u_sample, path=None, n_path=None, next_to
     if next_token is None:
         next_token = torch.empty(n, dtype=torch.int32, device=device)
     s = path.stride()
-    _need(path.dtype is torch.int32 and path.dim() == 2 and path.shape[0] == n and path.shape[1] >= t and s[1] == 1,
-          "path: int32 [session, max_tokens]")
+    _need(path.dtype is torch.int32 and path.dim() == 2 and path.shape[0] == n and path.shape[1] >= t and s[1] == 1 and
+          path.device == device, "path: int32 [session, max_tokens] on the device of p")
     rc = lib().unison_kv_verify(
         tree.address,
         _VERIFY.pack(p.data_ptr(), 0 if q is None else q.data_ptr(), ps[0], qs[0],
-                     _dense(token, torch.int32, (total,), "token"), _dense(u, torch.float32, (total,), "u"),
-                     _dense(u_sample, torch.float32, (n,), "u_sample"), path.data_ptr(),
-                     _dense(n_path, torch.int32, (n,), "n_path"), _dense(next_token, torch.int32, (n,), "next_token"),
-                     s[0], vocab, DTYPE[dtype]),
+                     _dense(token, torch.int32, (total,), "token", device),
+                     _dense(u, torch.float32, (total,), "u", device),
+                     _dense(u_sample, torch.float32, (n,), "u_sample", device), path.data_ptr(),
+                     _dense(n_path, torch.int32, (n,), "n_path", device),
+                     _dense(next_token, torch.int32, (n,), "next_token", device), s[0], vocab, DTYPE[dtype]),
         _queue(device, stream))
     if rc:
         binding._check("unison_kv_verify", rc)

@@ -184,3 +184,36 @@ def test_empty_batches_do_nothing(kv):
     kv.evict(cache, torch.zeros(0, dtype=torch.int32), stream=0)
     i = torch.zeros(0, dtype=torch.int32)
     kv.verify(tree, i, torch.zeros(0, 10), None, torch.zeros(0), torch.zeros(0), stream=0)
+
+
+def test_room_of_a_page_table_is_limited(kv):
+    cache = _made().cache(kv)
+    cache.struct.page_size = 1 << 15
+    for pages, fits in (((1 << 16) - 3, True), ((1 << 16) - 2, False)):
+        cache.struct.max_pages = pages
+        assert (kv.lib().unison_kv_evict_workspace(cache.address) > 0) == fits
+
+
+def test_binding_refuses_the_host_and_other_devices(kv):
+    """Kernels follow pointers, so a tensor elsewhere is refused before any launch."""
+    m = _made()
+    cache, tree = m.cache(kv), m.tree(kv)
+    p, i = torch.zeros(m.total, 10), torch.zeros(m.total, dtype=torch.int32)
+    lse, keep = torch.zeros(m.total, m.q.shape[1]), torch.zeros(2, dtype=torch.int32)
+    for call in (lambda: kv.attend(cache, tree, m.q, m.k_new, m.v_new, stream=0),
+                 lambda: kv.observe(cache, tree, m.q, lse, m.k_new, stream=0),
+                 lambda: kv.commit(cache, tree, m.k_new, m.v_new, stream=0),
+                 lambda: kv.evict(cache, keep, stream=0),
+                 lambda: kv.verify(tree, i, p, p, torch.zeros(m.total), torch.zeros(2), stream=0)):
+        with pytest.raises(ValueError, match="CUDA"):
+            call()
+    there = lambda x: torch.empty_like(x, device="meta")  # noqa: E731
+    for call in (lambda: kv.Cache(m.k, there(m.v), m.page_table, m.length),
+                 lambda: kv.Cache(m.k, m.v, there(m.page_table), m.length),
+                 lambda: kv.Cache(m.k, m.v, m.page_table, there(m.length)),
+                 lambda: kv.Cache(m.k, m.v, m.page_table, m.length, mass=there(m.mass)),
+                 lambda: kv.Tree(m.offsets, 3, mask=there(m.mask)),
+                 lambda: kv.attend(cache, tree, there(m.q), m.k_new, m.v_new, stream=0),
+                 lambda: kv.evict(cache, there(keep), stream=0)):
+        with pytest.raises(ValueError, match="device| on "):
+            call()
