@@ -49,7 +49,7 @@ struct TcShared {
   KvRunShared run;
   uint64_t kv_full[kSlots<DP>], kv_free[kSlots<DP>], q_full, q_free, s_full[2], p_full[2], pv_done[2], half_full,
       half_free, idle;
-  uint32_t row_ok[8][4];  // which keys of a tile exist
+  alignas(16) uint32_t row_ok[8][4];  // which keys of a tile exist
   bool odd[4][4];         // whether new values that a copying warp read hold infinities or NaN, of four segments
   float half[2][128];     // maxima and sums of a single query tile's second half of the keys
   uint32_t tmem;
@@ -398,14 +398,12 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
         ok = __all_sync(~0u, bar_wait(smem_u32(&sh.s_full[q]), s_no & 1, &sh.dead));
         if (!ok) break;
         tmem_after_sync();
-        uint32_t see[4];
-#pragma unroll
-        for (int i = 0; i < 4; i++) see[i] = sh.row_ok[(tiles_before + kt - g.kt0) & 7][i];
+        uint4 see = *reinterpret_cast<const uint4 *>(sh.row_ok[(tiles_before + kt - g.kt0) & 7]);
+        const bool hidden = (see.x & see.y & see.z & see.w) != ~0u;  // the last tile: always (64 tokens at most)
         if (kt == g.tiles - 1) {
-          see[0] &= (uint32_t)mask;
-          see[1] &= (uint32_t)(mask >> 32);
+          see.x &= (uint32_t)mask;
+          see.y &= (uint32_t)(mask >> 32);
         }
-        const bool hidden = !__all_sync(~0u, (see[0] & see[1] & see[2] & see[3]) == ~0u);
         const uint64_t cc = pair(c, c);
         uint32_t x[2][32];
         // One pass where the last reference still serves: the weights wait in
@@ -451,7 +449,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
             for (int i = 0; i < 32; i++)
               if (!(word >> i & 1)) v[i] = 0xFF800000u;  // -inf
           };
-          auto word_of = [&](int i) { return i == 0 ? see[0] : i == 1 ? see[1] : i == 2 ? see[2] : see[3]; };
+          auto word_of = [&](int i) { return i == 0 ? see.x : i == 1 ? see.y : i == 2 ? see.z : see.w; };
           float t = -INFINITY;
 #pragma unroll 1
           for (int i = 0; i < 4; i++) {
