@@ -349,16 +349,21 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) attend_kernel(con
   }
 }
 
-// Joins the parts of the segments that lie in several runs: one CTA per CTA of
-// the other kernel and four rows.  The parts' statistics become weights in
-// shared memory, in rounds of kParts; the threads of a row then add up 16 bytes
-// of it each, from parts of their own where there are threads to spare.
-// Bound by its loads' latency: 4 us after one short session, 7 us after two of
-// 128k keys (a segment lies in up to 19 runs), 27 us for 304 parts of 256 rows
-// (40 MB).
+// Joins the parts of the segments that lie in several runs, each by the CTAs of
+// the run that it begins in.
+//   up to kFewParts  a warp for each row: it asks for the parts' statistics and
+//                    for the row in all of them at once
+//   more             four rows at a time: the parts' statistics become weights in
+//                    shared memory, in rounds of kParts; the threads of a row
+//                    then add up 16 bytes of it each, from parts of their own
+//                    where there are threads to spare
+// Bound by its loads' latency: 15 us for 304 parts of 256 rows (40 MB; 27 four
+// rows at a time), 6 us after two sessions of 128k keys (19 parts a segment).
 constexpr int kJoin = 256;
 constexpr int kJoinRows = 4;
 constexpr int kParts = 256;
+constexpr int kFewParts = 4;
+
 
 template <typename T, int DP>
 __global__ void __launch_bounds__(kJoin) attend_join_kernel(const AttendParams P) {
@@ -380,6 +385,53 @@ __global__ void __launch_bounds__(kJoin) attend_join_kernel(const AttendParams P
   auto part = [&](int p) { return p ? rest + p * stride : first; };
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (parts <= kFewParts) {
+    constexpr int kPer = DP / 32;  // elements of a lane
+    const int col = lane * kPer;
+    for (int row = blockIdx.y * (kJoin / 32) + warp; row < rows; row += gridDim.y * (kJoin / 32)) {
+      float m = -INFINITY, l = 0.f, x[kFewParts][kPer], sum[kPer];
+      if (lane < parts) {
+        const float *q = part(lane) + R * DP + row;
+        m = q[0], l = q[R];
+      }
+#pragma unroll
+      for (int p = 0; p < kFewParts; p++) {
+        const float2 *q = reinterpret_cast<const float2 *>(part(min(p, parts - 1)) + row * DP + col);
+#pragma unroll
+        for (int i = 0; i < kPer; i += 2) {
+          const float2 y = p < parts && col < D ? q[i / 2] : make_float2(0.f, 0.f);
+          x[p][i] = y.x, x[p][i + 1] = y.y;
+        }
+      }
+      float top = m;
+#pragma unroll
+      for (int d = kFewParts / 2; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+      top = __shfl_sync(~0u, top, 0);
+      const float f = exp2_fast(m - (top == -INFINITY ? 0.f : top));
+      l *= f;
+#pragma unroll
+      for (int d = kFewParts / 2; d; d >>= 1) l += __shfl_xor_sync(~0u, l, d);
+      l = __shfl_sync(~0u, l, 0);
+#pragma unroll
+      for (int i = 0; i < kPer; i++) sum[i] = 0.f;
+#pragma unroll
+      for (int p = 0; p < kFewParts; p++) {
+        const float w = __shfl_sync(~0u, f, p);
+#pragma unroll
+        for (int i = 0; i < kPer; i++) sum[i] += x[p][i] * w;
+      }
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      const int at = seg.first_row + row, head = seg.head * G + at % G;
+      const int64_t token = seg.token + at / G;
+      T *dst = static_cast<T *>(P.s.out) + token * P.s.out_token + head * P.s.out_head + col;
+#pragma unroll
+      for (int i = 0; i < kPer; i += 2)
+        if (col < D) reinterpret_cast<uint32_t *>(dst)[i / 2] = KvType<T>::pack(sum[i] * inv, sum[i + 1] * inv);
+      if (lane == 0 && P.s.lse)
+        P.s.lse[token * P.s.n_q_heads + head] = (top + log2f(l)) * 0.6931471805599453f;
+    }
+    return;
+  }
   const int row = threadIdx.x / kVec % kJoinRows, share = threadIdx.x / (kVec * kJoinRows),
             col = threadIdx.x % kVec * 4;
   for (int row0 = blockIdx.y * kJoinRows; row0 < rows; row0 += gridDim.y * kJoinRows) {
