@@ -20,9 +20,10 @@
 // Up to 128 rows memory bounds it (5.9 TB/s at 128 rows of that case, 185 us);
 // from 256 on the tensor cores and the two warps per scheduler that compute the
 // weights: 64 nodes x 8 heads over 32 sessions of 15k to 16k keys, 8 KV heads
-// (1.06 PFLOP), take 735 us, 1.44 PFLOP/s, 74% of what a plain matrix product
-// reaches here.  512 rows' CTAs work in pairs on the same keys, which the second
-// finds in the L2 cache.
+// (1.06 PFLOP), take 740 us, 1.43 PFLOP/s, 74% of what a plain matrix product
+// reaches here (800 us in a stream of such calls, under the power limit).  512
+// rows' CTAs work in pairs on the same keys, which the second finds in the L2
+// cache.
 //
 // A wait that runs out ends the CTA (every role sees `dead`) and reports
 // UNISON_ERR_TIMEOUT.  Every copying warp waits for every slot, also for those
