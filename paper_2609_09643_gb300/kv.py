@@ -184,10 +184,12 @@ def _path(tree, path, n_path):
     return _PATH.pack(path.data_ptr(), _dense(n_path, torch.int32, (tree.n_seqs,), "n_path", tree.device), s[0])
 
 
-def _on_gpu(cache, *others):
+def _on_gpu(cache, x, workspace=None):
     """The kernels follow pointers: none to the host, none to another device."""
-    if not cache.on_gpu and cache.n_seqs or any(x.device != cache.device for x in others if x is not None):
-        raise ValueError(f"cache, tree and workspace: on one CUDA device ({cache.device})")
+    device = cache.device
+    if not cache.on_gpu and cache.n_seqs or x is not None and x.device != device or \
+            workspace is not None and workspace.device != device:
+        raise ValueError(f"cache, tree and workspace: on one CUDA device ({device})")
 
 
 def _queue(device, stream):
