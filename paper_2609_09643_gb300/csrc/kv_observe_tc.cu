@@ -36,9 +36,12 @@ constexpr int kTile = 128;
 constexpr int kCopyWarp = 8, kIssueWarp = 12, kBoxWarp = 13;
 constexpr int kBuffers = 4, kMostSlots = 6;
 constexpr int kNodes = UNISON_KV_MAX_TOKENS;
-// Tiles whose keys' accounts are kept in shared memory: those on their way, the
-// four that may be in tensor memory, and the one that is being looked up.
-constexpr int kMoreMarks = kBuffers + 1;
+// Tiles whose keys' accounts are kept in shared memory.  The copies for tile t
+// wait for the products of tile t - slots, which wait for the scores of tile
+// t - slots - kBuffers to be read; accounts are read after that.  So of the last
+// two tiles read by then, one of each group where a tile is one chunk, the
+// accounts may still be wanted; a group has read those of its tile before.
+constexpr int kMoreMarks = kBuffers + 2;
 constexpr int kMarkBytes = kTile * 12;
 
 struct ObserveShared {
