@@ -39,6 +39,10 @@ constexpr int kThreads = 416;
 constexpr int kTile = 128;
 constexpr int kCopyWarp = 8, kIssueWarp = 12;
 constexpr float kSlack = 8.f;
+// Segments whose flags of odd values are kept.  A segment that takes one tile
+// passes the second slot's warps by, so nothing else holds the copies back until
+// these have read the flags of an earlier one: they wait for that (seg_done).
+constexpr int kOddSets = 4;
 
 template <int DP>
 constexpr int kSlots = DP == 128 ? 5 : 8;  // tiles of K or V on their way
@@ -49,9 +53,9 @@ template <int DP>
 struct TcShared {
   KvRunShared run;
   uint64_t kv_full[kSlots<DP>], kv_free[kSlots<DP>], q_full, q_free, s_full[2], p_full[2], pv_done[2], half_full,
-      half_free, idle;
+      half_free, seg_done[kOddSets], idle;
   alignas(16) uint32_t row_ok[8][4];  // which keys of a tile exist
-  bool odd[4][4];         // whether new values that a copying warp read hold infinities or NaN, of four segments
+  bool odd[kOddSets][4];  // whether new values that a copying warp read hold infinities or NaN
   float half[2][128];     // maxima and sums of a single query tile's second half of the keys
   uint32_t tmem;
   volatile int dead;
@@ -114,6 +118,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     bar_init(smem_u32(&sh.idle), 1);
     bar_init(smem_u32(&sh.half_full), 4);
     bar_init(smem_u32(&sh.half_free), 4);
+    for (int i = 0; i < kOddSets; i++) bar_init(smem_u32(&sh.seg_done[i]), kCopyWarp);  // warps that weigh
     for (int i = 0; i < 2; i++) {
       bar_init(smem_u32(&sh.s_full[i]), 2);
       bar_init(smem_u32(&sh.p_full[i]), 4);  // warps
@@ -176,6 +181,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
       const int last_tile = g.tiles - 1;
       // the query rows: when the last segment's products have read theirs
       if (seg_no > 0) ok = copier.wait(smem_u32(&sh.q_free), (seg_no - 1) & 1, &sh.dead);
+      if (ok && seg_no >= kOddSets)
+        ok = copier.wait(smem_u32(&sh.seg_done[seg_no % kOddSets]), (seg_no / kOddSets - 1) & 1, &sh.dead);
       if (!ok) break;
       for (int q = 0; q < (g.rows > 128 ? 2 : 1); q++) {
         const int r = q * 128 + w * 32 + lane, row = g.row_tile * kTcRows + r;
@@ -258,7 +265,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
           copier.issued(0);
           copier.landed();
           const bool odd = copier.zero_odd_values(dst);
-          if (lane == 0) sh.odd[seg_no & 3][w] = odd;
+          if (lane == 0) sh.odd[seg_no % kOddSets][w] = odd;
           copier.arrive(bar);
         }
       }
@@ -379,6 +386,10 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     int halves = 0;                          // segments that the slots joined
     bool owed = false;                       // slot 1: its half of the last one may still be read
     bool ok = true;
+    auto warp_arrive = [&](uint64_t &bar) {
+      __syncwarp();
+      if (lane == 0) bar_arrive(smem_u32(&bar));
+    };
     while (at < run.end && ok) {
       Segment g;
       next_segment(g);
@@ -390,7 +401,10 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
       const int n = g.kt1 - g.kt0, begin = turns ? g.kt0 + q : g.kt0, step = turns ? 2 : 1;
       const int tiles_before = tile_no;
       tile_no += n;
-      if (begin >= g.kt1) continue;
+      if (begin >= g.kt1) {
+        warp_arrive(sh.seg_done[mine % kOddSets]);
+        continue;
+      }
       const int tr = turns ? r : q * 128 + r, row = g.row_tile * kTcRows + tr, node = row / G;
       const bool used = tr < g.rows;
       const uint64_t mask = !used ? 0 : P.t.mask ? P.t.mask[g.tok.first + node] : ~0ull >> (63 - node);
@@ -508,8 +522,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
           if (!ok) break;
           owed = false;
         }
-        __syncwarp();
-        if (lane == 0) bar_arrive(smem_u32(&sh.p_full[q]));
+        warp_arrive(sh.p_full[q]);
         s_no++;
       }
       if (!ok) break;
@@ -524,8 +537,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
           sh.half[0][r] = m;
           sh.half[1][r] = l;
           tmem_before_sync();
-          __syncwarp();
-          if (lane == 0) bar_arrive(smem_u32(&sh.half_full));
+          warp_arrive(sh.half_full);
+          warp_arrive(sh.seg_done[mine % kOddSets]);
           halves++;
           owed = true;
           continue;
@@ -540,7 +553,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
         m = top;
       }
       const bool whole = g.kt0 == 0 && g.kt1 == g.tiles;
-      const bool *flags = sh.odd[mine & 3];
+      const bool *flags = sh.odd[mine % kOddSets];
       const bool odd = g.kt1 == g.tiles && (flags[0] || flags[1] || flags[2] || flags[3]);
       const float inv = l == 0.f ? 0.f : 1.f / l;
       float *part = P.partial + ((int64_t)blockIdx.x * 2 + (g.kt0 == 0 ? 1 : 0)) * (kTcRows * (DP + 2));
@@ -604,6 +617,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
       __syncwarp();
       tmem_before_sync();  // the next segment's products overwrite O
       if (join && lane == 0) bar_arrive(smem_u32(&sh.half_free));
+      if (lane == 0) bar_arrive(smem_u32(&sh.seg_done[mine % kOddSets]));
     }
     if (!ok && r == 0 && P.c.status) P.c.status[b] = UNISON_ERR_TIMEOUT;
   }

@@ -107,6 +107,17 @@ def test_attend_hidden_nodes_do_not_reach_a_row(kv, bad, group):
     check_attend(kv, m)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_attend_odd_values_of_many_short_segments(kv, d):
+    """Large trees over a context, each followed by sessions without one, many to
+    a CTA: whose new values hold infinities and NaN stays with the session."""
+    lens, counts = [130, 0, 0, 0, 0, 0] * 150, [64, 9, 12, 16, 1, 10] * 150
+    m = Made(lens, counts, hkv=1, group=4, d=d, page=32, seed=d, room=0)
+    for i, bad in zip(range(5, m.total, 29), [INF, NAN, -INF, INF] * m.total):
+        m.v_new[i, 0, i % d] = bad
+    check_attend(kv, m)
+
+
 def test_attend_visible_infinities(kv):
     m = Made([100, 100], [2, 2], seed=8)
     m.v[int(m.table[0, 1]), 1, 3, 7] = INF
