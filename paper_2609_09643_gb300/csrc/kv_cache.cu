@@ -71,6 +71,7 @@ struct EvictParams {
   const int32_t *keep;
   int32_t sink, recent;
   bool in_place;
+  bool by_pos;     // positions tell what is protected: pos and next_pos are there
   bool by_four;    // mass and pos of four neighbouring slots are 16 aligned bytes
   int hold;        // keys of a thread of the selection in shared memory
   int per_seg;     // CTAs that move one segment's slots
@@ -113,7 +114,7 @@ __device__ __forceinline__ void slot_keys(const EvictParams &P, int b, int h, in
     mass[i] = 0.f;
     if (page[i] >= 0) {
       mass[i] = P.c.mass[m];
-      if (P.c.pos) pos[i] = P.c.pos[m];
+      if (P.by_pos) pos[i] = P.c.pos[m];
     }
   }
 #pragma unroll
@@ -143,7 +144,7 @@ __device__ __forceinline__ void slot_keys_by_four(const EvictParams &P, int b, i
     mass[i] = make_float4(0.f, 0.f, 0.f, 0.f);
     if (page[i] >= 0) {
       mass[i] = *reinterpret_cast<const float4 *>(P.c.mass + m);
-      if (P.c.pos) pos[i] = *reinterpret_cast<const int4 *>(P.c.pos + m);
+      if (P.by_pos) pos[i] = *reinterpret_cast<const int4 *>(P.c.pos + m);
     }
   }
 #pragma unroll
@@ -201,7 +202,7 @@ __global__ void __launch_bounds__(kSelect, 4) evict_select_kernel(const EvictPar
   const int len = kv_length(P.c, b);
   const int n = kept_count(P, b, len);
   // positions from here on are protected
-  const int64_t from_pos = (int64_t)(P.c.pos && P.c.next_pos ? P.c.next_pos[b] : len) - P.recent;
+  const int64_t from_pos = (int64_t)(P.by_pos ? P.c.next_pos[b] : len) - P.recent;
   const int next = (int)max(min(from_pos, (int64_t)INT32_MAX), (int64_t)INT32_MIN);
   const int64_t room = (int64_t)P.c.max_pages * P.c.page_size;
   int32_t *from = P.moves + seg * room, *into = from + room / 2;
@@ -515,6 +516,7 @@ extern "C" int unison_kv_evict(const unison_kv_cache *cache, const unison_kv_cac
   p.sink = sink;
   p.recent = recent;
   p.in_place = into == nullptr;
+  p.by_pos = cache->pos && cache->next_pos;
   p.by_four = cache->m_slot == 1 && cache->page_size % 4 == 0 && (cache->m_page | cache->m_head) % 4 == 0 &&
               kv_aligned(cache->mass, 16) && kv_aligned(cache->pos, 16);
   p.moves = static_cast<int32_t *>(workspace);

@@ -478,6 +478,36 @@ def test_evict_without_positions(kv):
     check_evict(kv, m, [30, 2000], 4, 9, marks=False)
 
 
+@pytest.mark.parametrize("page", [7, 16])  # slots one by one, and by four
+@pytest.mark.parametrize("without", ["pos", "next_pos"])
+@pytest.mark.parametrize("place", ["in", "into"])
+def test_evict_with_half_of_the_positions(kv, page, without, place):
+    """Positions count only where next_pos tells the next one: without either a
+    slot's index is its position, whatever pos holds; pos moves along all the same."""
+    lens, keep, sink, recent = [100, 60, 9], [40, 30, 9], 2, 5
+    m = Made(lens, [1] * 3, page=page, seed=page, room=1)
+    m.pos += 5000  # far above the lengths, as after many evictions
+    to = m if place == "in" else Made([0] * 3, [1] * 3, page=16, room=40, seed=1)
+    mass, pos, k = f64(m.mass), m.pos.clone(), m.k.clone()
+    drop = {without: None}
+    kv.evict(m.cache(kv, **drop), torch.tensor(keep, dtype=torch.int32, device="cuda"), sink=sink, recent=recent,
+             into=None if place == "in" else to.cache(kv, **drop))
+    assert to.length.tolist() == keep
+    for b, n in enumerate(lens):
+        for h in range(m.hkv):
+            at = lambda s: (int(m.table[b, s // page]), h, s % page)  # noqa: B023, E731
+            stay = ref.kept([mass[at(s)] for s in range(n)], range(n), n, keep[b], sink, recent, n)
+            if place == "in":
+                free = [s for s in range(keep[b]) if s not in stay]
+                want = {s: s for s in stay if s < keep[b]} | dict(zip(free, [s for s in stay if s >= keep[b]]))
+            else:
+                want = dict(enumerate(stay))
+            for z, a in want.items():
+                there = (int(to.table[b, z // to.page]), h, z % to.page)
+                assert torch.equal(to.k[there], k[at(a)])
+                assert without == "pos" or int(to.pos[there]) == int(pos[at(a)])
+
+
 def test_evict_into_a_cache_without_room(kv):
     m = Made([100, 60], [1, 1], page=16, seed=8, room=1)
     _plain_marks(m)
