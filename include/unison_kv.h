@@ -145,7 +145,8 @@ int unison_kv_observe(const unison_kv_cache *cache, const unison_kv_tree *tree, 
  * position next_pos[b] + i and the weight mass_new (0 where that is NULL);
  * then length[b] and next_pos[b] grow by the number of tokens.  mass, pos and
  * next_pos of the cache may be NULL.  A session whose pages do not hold them
- * all stays as it is, and its status word receives UNISON_ERR_CAPACITY.
+ * all stays as it is, and its status word receives UNISON_ERR_CAPACITY; so does
+ * one whose path names a node that it has not, with UNISON_ERR_RANGE.
  * Reads k_new, v_new, mass_new. */
 int unison_kv_commit(const unison_kv_cache *cache, const unison_kv_tree *tree, const unison_kv_step *step,
                      const unison_kv_path *path, void *cuda_stream);

@@ -131,6 +131,18 @@ __device__ __forceinline__ int kv_length(const unison_kv_cache &c, int b) {
   if (c.status && n != len) c.status[b] = UNISON_ERR_RANGE;
   return len;
 }
+// Accepted nodes of a session of `tokens`, clamped, and the i-th of them, or -1
+// where the path names another.
+__device__ __forceinline__ int kv_path_count(const unison_kv_path &p, int b, int tokens, int32_t *status) {
+  if (!p.path) return tokens;
+  const int n = p.n_path[b], count = min(max(n, 0), tokens);
+  if (status && n != count) status[b] = UNISON_ERR_RANGE;
+  return count;
+}
+__device__ __forceinline__ int kv_path_node(const unison_kv_path &p, int b, int tokens, int i) {
+  const int node = p.path ? p.path[(int64_t)b * p.path_stride + i] : i;
+  return (unsigned)node < (unsigned)tokens ? node : -1;
+}
 // Page of a slot (below max_pages * page_size), as the table has it: to be
 // checked by kv_page_ok when it is used, so that the load may be on its way.
 constexpr int kNoSlot = INT32_MIN;

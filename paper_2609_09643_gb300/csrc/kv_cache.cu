@@ -24,26 +24,25 @@ __global__ void __launch_bounds__(256) commit_kernel(const CommitParams P) {
   const int b = blockIdx.x, tid = threadIdx.x;
   const int H = P.c.n_heads, chunks = P.c.head_dim / 8;
   const KvRange tok = kv_tokens(P.t, b, P.c.status);
-  const int n = P.path.path ? min(max(P.path.n_path[b], 0), tok.count) : tok.count;
+  const int n = kv_path_count(P.path, b, tok.count, P.c.status);
   const int len = kv_length(P.c, b);
   const int pos = P.c.next_pos ? P.c.next_pos[b] : len;
   bool full = len + n > P.c.max_pages * P.c.page_size;
   int off;
   if (!full && tid < n) full = kv_page(P.c, b, len + tid, off) < 0;
+  const bool strange = tid < n && kv_path_node(P.path, b, tok.count, tid) < 0;
   // (every thread has also read what the first one will change)
-  if (__syncthreads_or(full)) {
-    if (tid == 0 && P.c.status) P.c.status[b] = UNISON_ERR_CAPACITY;
+  const bool no_room = __syncthreads_or(full), no_node = __syncthreads_or(strange);
+  if (no_room || no_node) {
+    if (tid == 0 && P.c.status) P.c.status[b] = no_room ? UNISON_ERR_CAPACITY : UNISON_ERR_RANGE;
     return;
   }
   const int per_row = H * chunks;
   for (int i = tid; i < n * per_row; i += blockDim.x) {
     const int row = i / per_row, h = i % per_row / chunks, c = i % chunks;
-    const int node = P.path.path ? P.path.path[(int64_t)b * P.path.path_stride + row] : row;
+    const int node = kv_path_node(P.path, b, tok.count, row);
     const int page = kv_page(P.c, b, len + row, off);
-    if (page < 0 || (unsigned)node >= (unsigned)tok.count) {
-      if (P.c.status) P.c.status[b] = UNISON_ERR_RANGE;
-      continue;
-    }
+    if (page < 0 || node < 0) continue;  // (asked above)
     const int64_t from = tok.first + node;
     const int4 k = *reinterpret_cast<const int4 *>(static_cast<const T *>(P.s.k_new) + from * P.s.k_token +
                                                    h * P.s.k_head + c * 8);

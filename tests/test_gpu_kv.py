@@ -386,6 +386,38 @@ def test_commit_without_path_marks_or_room(kv):
             assert torch.equal(m.k[int(page)].nan_to_num(-9.0), before[int(page)].nan_to_num(-9.0))
 
 
+def _bad_paths():
+    """(paths, lengths of paths) of five sessions of four tokens, the good one in the middle: a node behind the last
+    one, a node below 0, a good path, more nodes than tokens, fewer than none."""
+    path = torch.tensor([[0, 2, 4, -1], [0, -1, 2, -1], [0, 1, 3, -1], [0, 1, 2, 3], [0, 1, 2, 3]], dtype=torch.int32)
+    return path.cuda(), torch.tensor([3, 3, 3, 7, -2], dtype=torch.int32, device="cuda")
+
+
+@pytest.mark.parametrize("page", [1, 8])
+def test_commit_refuses_paths_with_other_nodes(kv, page):
+    """No slot counts that holds nothing: a session whose path names a node that
+    it has not stays as it is; path lengths are clamped.  Both are reported."""
+    lens = [10, 20, 5, 6, 7]
+    m = Made(lens, [4] * 5, page=page, seed=2)
+    path, n_path = _bad_paths()
+    before = {x: getattr(m, x).clone() for x in ("k", "v", "mass", "pos")}
+    kv.commit(m.cache(kv), m.tree(kv), m.k_new, m.v_new, path=path, n_path=n_path)
+    assert m.length.tolist() == [10, 20, 8, 10, 7]
+    assert m.next_pos.tolist() == [17, 27, 15, 17, 14]
+    assert m.status.tolist() == [-4, -4, 0, -4, -4]
+    for b, nodes in ((2, [0, 1, 3]), (3, [0, 1, 2, 3])):
+        for i, node in enumerate(nodes):
+            s = lens[b] + i
+            at = (int(m.table[b, s // page]), slice(None), s % page)
+            for x, new in (("k", m.k_new), ("v", m.v_new)):
+                assert torch.equal(getattr(m, x)[at], new[m.off[b] + node])
+            for x in before:
+                before[x][at] = getattr(m, x)[at]
+    for x, old in before.items():  # nothing else was written
+        assert torch.equal(getattr(m, x).nan_to_num(-9.0), old.nan_to_num(-9.0)) if old.is_floating_point() else \
+            torch.equal(getattr(m, x), old), x
+
+
 # ------------------------------------------------------------------ evict --
 def check_evict(kv, m, keep, sink, recent, into=None, marks=True):
     """Both forms against a sort of every session's and head's slots."""
