@@ -136,8 +136,9 @@ int unison_kv_attend(const unison_kv_cache *cache, const unison_kv_tree *tree, c
  * weight sum exp(S - lse) that the accepted tokens give it, over the query
  * heads of that KV head; lse is what unison_kv_attend returned.  mass_new
  * receives the same of the new tokens themselves (0 for a node that no
- * accepted one sees).  Rows with lse = -inf give nothing.  Reads q, k_new, lse;
- * writes mass and mass_new (NULL: not wanted; k_new is not read then). */
+ * accepted one sees).  Rows with lse = -inf give nothing, nor do nodes of the
+ * path that the session has not (UNISON_ERR_RANGE).  Reads q, k_new, lse; writes
+ * mass and mass_new (NULL: not wanted; k_new is not read then). */
 int unison_kv_observe(const unison_kv_cache *cache, const unison_kv_tree *tree, const unison_kv_step *step,
                       const unison_kv_path *path, void *cuda_stream);
 

@@ -51,7 +51,7 @@ __global__ void __launch_bounds__(kThreads) observe_kernel(const ObserveParams P
     }
     const KvRange tok = kv_tokens(P.t, b, nullptr);
     const int len = kv_length(P.c, b);
-    const int rows = path_count(P, b, tok.count) * G;
+    const int rows = kv_path_count(P.path, b, tok.count, nullptr) * G;
     const int key_tiles = key_tiles_of(b);
     const int last_tile = key_tiles - 1;
     const int head = (int)((at - seq_begin) / key_tiles);

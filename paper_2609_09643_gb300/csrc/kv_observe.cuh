@@ -14,22 +14,18 @@ struct ObserveParams {
   int q_rows, q_buffers, slots;  // tensor cores: query rows that fit, how often, key tiles on their way
 };
 
-// Accepted nodes of a session.
-__device__ __forceinline__ int path_count(const ObserveParams &P, int b, int tokens) {
-  return P.path.path ? min(max(P.path.n_path[b], 0), tokens) : tokens;
-}
 // Key tiles of a session; the last one holds its new tokens, the only one
 // where no token was accepted.
 __device__ __forceinline__ int observe_key_tiles(const ObserveParams &P, int b, int tile) {
   const int tokens = kv_tokens(P.t, b, P.c.status).count;
   if (!tokens) return 0;
-  return path_count(P, b, tokens) ? (kv_length(P.c, b) + tile - 1) / tile + 1 : 1;
+  return kv_path_count(P.path, b, tokens, P.c.status) ? (kv_length(P.c, b) + tile - 1) / tile + 1 : 1;
 }
-
-// Query row r of a session's accepted path, as a token of the session, or -1.
+// Node i of a session's accepted path, or -1, which is reported.
 __device__ __forceinline__ int observe_node(const ObserveParams &P, int b, int tokens, int i) {
-  const int node = P.path.path ? P.path.path[(int64_t)b * P.path.path_stride + i] : i;
-  return (unsigned)node < (unsigned)tokens ? node : -1;
+  const int node = kv_path_node(P.path, b, tokens, i);
+  if (node < 0 && P.c.status) P.c.status[b] = UNISON_ERR_RANGE;
+  return node;
 }
 
 constexpr int kObserveTcRows = 512;  // most query rows per KV head on the tensor cores

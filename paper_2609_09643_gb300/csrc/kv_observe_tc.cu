@@ -97,7 +97,7 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
   if (!kv_find_run(run, sh.run, P.c.n_seqs, gridDim.x, blockIdx.x, [&](int b) {
         const int tiles = observe_key_tiles(P, b, kTile);
         if (!tiles) return (int64_t)0;
-        const int rows = path_count(P, b, kv_tokens(P.t, b, nullptr).count) * G;
+        const int rows = kv_path_count(P.path, b, kv_tokens(P.t, b, nullptr).count, nullptr) * G;
         return (int64_t)(tiles + setup(rows)) * H * share(rows);
       }))
     return;
@@ -135,7 +135,7 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
     while (at < run.end) {
       g.tok = kv_tokens(P.t, b, nullptr);
       g.tiles = observe_key_tiles(P, b, kTile);
-      g.rows = path_count(P, b, g.tok.count) * G;
+      g.rows = kv_path_count(P.path, b, g.tok.count, nullptr) * G;
       const int each = share(g.rows), before = setup(g.rows);
       const int64_t per_head = g.tiles ? g.tiles + before : 0;
       const int64_t all = per_head * H;

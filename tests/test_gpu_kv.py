@@ -343,6 +343,25 @@ def test_observe_same_bits_again(kv):
     assert torch.equal(a, b) and torch.equal(first, m.mass)
 
 
+@pytest.mark.parametrize("group,d", [(4, 64), (2, 256)])
+def test_observe_reports_paths_with_other_nodes(kv, group, d):
+    """Nodes that a session has not give no weight; they and clamped lengths are reported."""
+    m = Made([150, 20, 5, 6, 7], [4] * 5, group=group, d=d, seed=2)
+    path, n_path = _bad_paths()
+    good = [[0, 2], [0, 2], [0, 1, 3], [0, 1, 2, 3], []]
+    lse = torch.from_numpy(ref.attend(m)[1]).float().cuda()
+    before = f64(m.mass)
+    new = kv.observe(m.cache(kv), m.tree(kv), m.q, lse, m.k_new, path=path, n_path=n_path)
+    assert m.status.tolist() == [-4, -4, 0, -4, -4]
+    added, bound, want_new, bound_new = ref.observe(m, lse, good)
+    for b, n in enumerate(m.lens):
+        s = np.arange(n)
+        at = (m.table[b, s // m.page], slice(None), s % m.page)
+        got = f64(m.mass)[at]
+        assert np.all(np.abs(got - before[at] - added[b]) <= bound[b] + 2.0 ** -23 * np.abs(got))
+    assert np.all(np.abs(f64(new) - want_new) <= bound_new)
+
+
 # ----------------------------------------------------------------- commit --
 @pytest.mark.parametrize("page,layout", [(1, "hnd"), (7, "nhd"), (16, "hnd"), (64, "nhd")])
 @pytest.mark.parametrize("d", [8, 96, 128])
