@@ -6,12 +6,15 @@
 namespace unison {
 
 // What a CTA leaves to be joined: the segment (one session, KV head and row
-// tile) that begins in its run and goes on in the runs up to `last`.
-struct AttendPart {
+// tile) that begins in its run and goes on in the runs up to `last`.  Whole
+// pieces of 16 bytes: the sums follow [grid] of them in the workspace, and are
+// read and written 16 bytes at a time.
+struct alignas(16) AttendPart {
   int last;                      // < 0: nothing
   int head, first_row, rows;     // of the row tile: its first row, its rows
   int64_t token;                 // the session's first token
 };
+static_assert(sizeof(AttendPart) % 16 == 0, "an odd number of CTAs leaves the sums aligned");
 
 struct AttendParams {
   KvCacheArg c;

@@ -56,6 +56,14 @@ def test_attend_rows(kv, group, counts, d):
     check_attend(kv, Made([70, 300, 129], counts, group=group, hkv=2, d=d, seed=group))
 
 
+@pytest.mark.parametrize("group,counts", [(12, [64, 43, 1]), (9, [64, 57, 22]), (16, [33, 48, 40])])
+@pytest.mark.parametrize("d", [64, 128])
+def test_attend_three_row_groups(kv, group, counts, d):
+    """513 to 768 rows per KV head: three CTAs share a run's keys, and the
+    sessions' segments are split."""
+    check_attend(kv, Made([2000, 300, 129], counts, group=group, hkv=2, d=d, seed=group))
+
+
 @pytest.mark.parametrize("group", [1, 16])
 @pytest.mark.parametrize("page", [1, 7, 16, 24, 64, 100, 256])
 def test_attend_pages_and_lengths(kv, page, group):

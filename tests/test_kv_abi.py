@@ -194,6 +194,16 @@ def test_room_of_a_page_table_is_limited(kv):
         assert (kv.lib().unison_kv_evict_workspace(cache.address) > 0) == fits
 
 
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("group,tokens", [(1, 1), (2, 16), (4, 64), (12, 64)])
+def test_scratch_is_whole_pieces_of_16_bytes(kv, d, group, tokens):
+    """For any number of multiprocessors (without a GPU: one), so that what lies
+    behind the first records is aligned where their number is odd, too."""
+    m = _made(d=d, group=group)
+    tree = kv.Tree(m.offsets, tokens, mask=m.mask)
+    assert kv.attend_workspace(m.cache(kv), tree, m.q.shape[1]) % 16 == 0
+
+
 def test_binding_refuses_the_host_and_other_devices(kv):
     """Kernels follow pointers, so a tensor elsewhere is refused before any launch."""
     m = _made()
