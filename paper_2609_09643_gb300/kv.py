@@ -192,10 +192,16 @@ def _on_gpu(cache, x, workspace=None):
         raise ValueError(f"cache, tree and workspace: on one CUDA device ({device})")
 
 
-def _queue(device, stream):
-    """The raw handle of a call's stream."""
+def _elsewhere(device):
+    """The library launches on the current device: whether that is another one."""
+    return device.index != torch._C._cuda_getDevice()
+
+
+def _queue(device, stream=None):
+    """The raw handle of a call's stream, of its device: the given one, or the current one."""
     if stream is None:
-        return torch._C._cuda_getCurrentRawStream(device.index)
+        return 0 if device.index is None else torch._C._cuda_getCurrentRawStream(device.index)
+    _need(getattr(stream, "device", device) == device, f"stream: of the tensors' device ({device})")
     return getattr(stream, "cuda_stream", stream)
 
 
@@ -211,10 +217,15 @@ def _workspace(cache, n, handle):
 
 
 def _on(device, stream, call, *args):
-    """A call with a given stream (torch's, or a raw handle): what it allocates belongs to that stream."""
+    """A call with its device current, on a given stream (torch's, or a raw handle; None: the device's current one):
+    what it allocates belongs to that stream."""
+    if stream is None:
+        with torch.cuda.device(device):
+            return call(*args)
     if not isinstance(stream, torch.cuda.Stream):
         raw = getattr(stream, "cuda_stream", stream)
         stream = torch.cuda.ExternalStream(raw, device=device) if raw else torch.cuda.default_stream(device)
+    _queue(device, stream)
     with torch.cuda.stream(stream):
         return call(*args)
 
@@ -223,7 +234,7 @@ def attend(cache: Cache, tree: Tree, q, k_new, v_new, scale=None, out=None, lse=
     """unison_kv_attend: (out [token, q head, head_dim], lse float32 [token, q
     head]).  scale defaults to head_dim ** -0.5; workspace: a uint8 tensor of
     at least ``attend_workspace`` bytes, else the cache keeps one."""
-    if stream is not None and cache.on_gpu:
+    if cache.on_gpu and (stream is not None or _elsewhere(cache.device)):
         return _on(cache.device, stream, attend, cache, tree, q, k_new, v_new, scale, out, lse, workspace)
     n, heads = tree.n_tokens, q.shape[1]
     qp, qs = _rows(cache, q, n, heads)
@@ -238,7 +249,7 @@ def attend(cache: Cache, tree: Tree, q, k_new, v_new, scale=None, out=None, lse=
     else:
         lp = _dense(lse, torch.float32, (n, heads), "lse", cache.device)
     _on_gpu(cache, tree, workspace)
-    handle = _queue(cache.device, stream)
+    handle = _queue(cache.device)
     if workspace is None:
         workspace = _workspace(cache, attend_workspace(cache, tree, heads), handle)
     rc = lib().unison_kv_attend(
@@ -252,7 +263,9 @@ def attend(cache: Cache, tree: Tree, q, k_new, v_new, scale=None, out=None, lse=
 
 
 def attend_workspace(cache: Cache, tree: Tree, n_q_heads: int) -> int:
-    """Bytes of scratch that attend takes (a function of the sizes alone)."""
+    """Bytes of scratch that attend takes (a function of the sizes and the device alone)."""
+    if cache.on_gpu and _elsewhere(cache.device):
+        return _on(cache.device, None, attend_workspace, cache, tree, n_q_heads)
     key = tree.max_tokens, n_q_heads
     n = cache.sizes.get(key)
     if n is None:
@@ -263,7 +276,7 @@ def attend_workspace(cache: Cache, tree: Tree, n_q_heads: int) -> int:
 def observe(cache: Cache, tree: Tree, q, lse, k_new, scale=None, path=None, n_path=None, mass_new=None, stream=None):
     """unison_kv_observe: adds to cache.mass; returns mass_new, float32 [token,
     head], the weight of the new tokens themselves."""
-    if stream is not None and cache.on_gpu:
+    if cache.on_gpu and (stream is not None or _elsewhere(cache.device)):
         return _on(cache.device, stream, observe, cache, tree, q, lse, k_new, scale, path, n_path, mass_new)
     n, heads = tree.n_tokens, q.shape[1]
     qp, qs = _rows(cache, q, n, heads)
@@ -276,7 +289,7 @@ def observe(cache: Cache, tree: Tree, q, lse, k_new, scale=None, path=None, n_pa
         cache.address, tree.address,
         _STEP.pack(qp, kp, 0, 0, lp, _dense(mass_new, torch.float32, (n, cache.n_heads), "mass_new", cache.device),
                    qs[0], qs[1], ks[0], ks[1], 0, 0, 0, 0, heads, cache.scale if scale is None else scale),
-        _path(tree, path, n_path), _queue(cache.device, stream))
+        _path(tree, path, n_path), _queue(cache.device))
     if rc:
         binding._check("unison_kv_observe", rc)
     return mass_new
@@ -285,6 +298,8 @@ def observe(cache: Cache, tree: Tree, q, lse, k_new, scale=None, path=None, n_pa
 def commit(cache: Cache, tree: Tree, k_new, v_new, mass_new=None, path=None, n_path=None, stream=None) -> None:
     """unison_kv_commit: the accepted tokens go into the pages, length and
     next_pos grow.  Without path every new token is accepted."""
+    if cache.on_gpu and _elsewhere(cache.device):
+        return _on(cache.device, stream, commit, cache, tree, k_new, v_new, mass_new, path, n_path)
     n = tree.n_tokens
     kp, ks = _rows(cache, k_new, n, cache.n_heads)
     vp, vs = _rows(cache, v_new, n, cache.n_heads)
@@ -309,11 +324,11 @@ def evict_workspace(cache: Cache) -> int:
 def evict(cache: Cache, keep, sink=0, recent=0, into: Cache | None = None, workspace=None, stream=None) -> None:
     """unison_kv_evict: at most keep[b] (int32 tensor) slots of each session
     stay, in place or, with ``into``, in another cache."""
-    if stream is not None and cache.on_gpu:
+    if cache.on_gpu and (stream is not None or _elsewhere(cache.device)):
         return _on(cache.device, stream, evict, cache, keep, sink, recent, into, workspace)
     kp = _dense(keep, torch.int32, (cache.n_seqs,), "keep", cache.device)
     _on_gpu(cache, into, workspace)
-    handle = _queue(cache.device, stream)
+    handle = _queue(cache.device)
     if workspace is None:
         workspace = _workspace(cache, evict_workspace(cache), handle)
     rc = lib().unison_kv_evict(cache.address, None if into is None else into.address, kp, sink, recent,
@@ -327,7 +342,7 @@ def verify(tree: Tree, token, p, q, u, u_sample, path=None, n_path=None, next_to
     next_token [session]), all int32.  p, q: [token, vocab] probabilities of
     one type (q None: certain drafts); token int32 [token]; u float32 [token];
     u_sample float32 [session]."""
-    if stream is not None and p.is_cuda:
+    if p.is_cuda and (stream is not None or _elsewhere(p.device)):
         return _on(p.device, stream, verify, tree, token, p, q, u, u_sample, path, n_path, next_token)
     n, t, total, device = tree.n_seqs, tree.max_tokens, tree.n_tokens, p.device
     dtype, vocab, ps, qs = p.dtype, p.shape[-1], p.stride(), _NO_STRIDES
@@ -355,7 +370,7 @@ def verify(tree: Tree, token, p, q, u, u_sample, path=None, n_path=None, next_to
                      _dense(u_sample, torch.float32, (n,), "u_sample", device), path.data_ptr(),
                      _dense(n_path, torch.int32, (n,), "n_path", device),
                      _dense(next_token, torch.int32, (n,), "next_token", device), s[0], vocab, DTYPE[dtype]),
-        _queue(device, stream))
+        _queue(device))
     if rc:
         binding._check("unison_kv_verify", rc)
     return path, n_path, next_token

@@ -204,6 +204,77 @@ def test_scratch_is_whole_pieces_of_16_bytes(kv, d, group, tokens):
     assert kv.attend_workspace(m.cache(kv), tree, m.q.shape[1]) % 16 == 0
 
 
+class _There(torch.Tensor):
+    """A host tensor that says it is on the second GPU."""
+    device = property(lambda self: torch.device("cuda", 1))
+    is_cuda = property(lambda self: True)
+
+
+def _calls_there(kv):
+    """Every call on tensors of the second GPU, outputs and scratch given; the last one asks for the scratch's size."""
+    there = lambda x: x.as_subclass(_There)  # noqa: E731
+    zeros = lambda *s, dtype=torch.float32: there(torch.zeros(s, dtype=dtype))  # noqa: E731
+    ints = lambda *s: zeros(*s, dtype=torch.int32)  # noqa: E731
+    m = _made()
+    for name, x in vars(m).items():
+        if isinstance(x, torch.Tensor):
+            setattr(m, name, there(x))
+    cache, tree, n, heads = m.cache(kv), m.tree(kv), m.total, m.q.shape[1]
+    out, lse, new = there(torch.zeros_like(m.q)), zeros(n, heads), zeros(n, m.hkv)
+    work = zeros(1 << 20, dtype=torch.uint8)
+    p = zeros(n, 10)
+    return [
+        lambda **kw: kv.attend(cache, tree, m.q, m.k_new, m.v_new, out=out, lse=lse, workspace=work, **kw),
+        lambda **kw: kv.observe(cache, tree, m.q, lse, m.k_new, mass_new=new, **kw),
+        lambda **kw: kv.commit(cache, tree, m.k_new, m.v_new, **kw),
+        lambda **kw: kv.evict(cache, ints(2), workspace=work, **kw),
+        lambda **kw: kv.verify(tree, ints(n), p, p, zeros(n), zeros(2), path=ints(2, 3), n_path=ints(2),
+                               next_token=ints(2), **kw),
+        lambda: kv.attend_workspace(cache, tree, heads)]
+
+
+def test_calls_run_on_the_device_of_their_tensors(kv, monkeypatch):
+    """The library launches on the current device: with another one current, a
+    call makes its tensors' device current, and puts the other one back."""
+    current, seen = [0], []
+
+    class On:
+        def __init__(self, device):
+            self.index = torch.device(device).index
+
+        def __enter__(self):
+            self.last, current[0] = current[0], self.index
+
+        def __exit__(self, *_):
+            current[0] = self.last
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *args: seen.append((name, current[0])) or 0
+
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: current[0])
+    monkeypatch.setattr(torch.cuda, "device", On)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda index: 0)
+    monkeypatch.setattr(kv, "lib", Library)
+    for first in (0, 1):
+        current[0] = first
+        for call in _calls_there(kv):
+            call()
+            assert current == [first]
+    names = [f"unison_kv_{x}" for x in ("attend", "observe", "commit", "evict", "verify", "attend_workspace")]
+    assert seen == [(x, 1) for x in names * 2]
+
+    class Stream:  # of the first GPU
+        device, cuda_stream = torch.device("cuda", 0), 7
+
+    monkeypatch.setattr(torch.cuda, "Stream", Stream)
+    del seen[:]
+    for call in _calls_there(kv)[:-1]:
+        with pytest.raises(ValueError, match="stream"):
+            call(stream=Stream())
+    assert not seen
+
+
 def test_binding_refuses_the_host_and_other_devices(kv):
     """Kernels follow pointers, so a tensor elsewhere is refused before any launch."""
     m = _made()
