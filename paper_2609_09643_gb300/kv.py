@@ -83,11 +83,14 @@ def _need(ok, what):
 
 
 def _dense(x, dtype, shape, what, device):
-    if x is None:
-        return None
-    if x.dtype is not dtype or x.shape != shape or not x.is_contiguous() or x.device != device:
+    if x is None or x.dtype is not dtype or x.shape != shape or not x.is_contiguous() or x.device != device:
         raise ValueError(f"{what}: a contiguous {dtype} tensor of shape {shape} on {device} is wanted")
     return x.data_ptr()
+
+
+def _given(x, *wanted):
+    """The same of a tensor that may be left out."""
+    return None if x is None else _dense(x, *wanted)
 
 
 class Cache:
@@ -126,8 +129,8 @@ class Cache:
             k.data_ptr(), v.data_ptr(), ptr(mass), ptr(pos),
             _dense(page_table, torch.int32, (n, pages), "page_table", device),
             _dense(length, torch.int32, (n,), "length", device),
-            _dense(next_pos, torch.int32, (n,), "next_pos", device),
-            _dense(status, torch.int32, (n,), "status", device), *k.stride()[:3], *v.stride()[:3], *m, n, pages,
+            _given(next_pos, torch.int32, (n,), "next_pos", device),
+            _given(status, torch.int32, (n,), "status", device), *k.stride()[:3], *v.stride()[:3], *m, n, pages,
             k.shape[0], k.shape[2], k.shape[1], k.shape[3], DTYPE[k.dtype], 0)
         self.address = C.addressof(self.struct)
         self.scale = self.head_dim ** -0.5
@@ -150,8 +153,8 @@ class Tree:
         self.n_seqs, self.n_tokens, self.max_tokens = offsets.shape[0] - 1, n, max_tokens
         self.device = offsets.device
         self.struct = KvTree(_dense(offsets, torch.int32, (self.n_seqs + 1,), "offsets", self.device),
-                             _dense(mask, torch.int64, (n,), "mask", self.device),
-                             _dense(parent, torch.int32, (n,), "parent", self.device), self.n_seqs, n, max_tokens, 0)
+                             _given(mask, torch.int64, (n,), "mask", self.device),
+                             _given(parent, torch.int32, (n,), "parent", self.device), self.n_seqs, n, max_tokens, 0)
         self.address = C.addressof(self.struct)
 
 
@@ -303,7 +306,7 @@ def commit(cache: Cache, tree: Tree, k_new, v_new, mass_new=None, path=None, n_p
     n = tree.n_tokens
     kp, ks = _rows(cache, k_new, n, cache.n_heads)
     vp, vs = _rows(cache, v_new, n, cache.n_heads)
-    mp = _dense(mass_new, torch.float32, (n, cache.n_heads), "mass_new", cache.device)
+    mp = _given(mass_new, torch.float32, (n, cache.n_heads), "mass_new", cache.device)
     _on_gpu(cache, tree)
     rc = lib().unison_kv_commit(
         cache.address, tree.address,

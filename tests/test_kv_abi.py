@@ -2,6 +2,7 @@
 is exported, and every call refuses what its header excludes before anything
 is queued."""
 import ctypes as C
+import types
 
 import pytest
 import torch
@@ -273,6 +274,34 @@ def test_calls_run_on_the_device_of_their_tensors(kv, monkeypatch):
         with pytest.raises(ValueError, match="stream"):
             call(stream=Stream())
     assert not seen
+
+
+def test_binding_refuses_calls_without_a_wanted_tensor(kv, monkeypatch):
+    there = lambda x: x.as_subclass(_There)  # noqa: E731
+    zeros = lambda *s, dtype=torch.float32: there(torch.zeros(s, dtype=dtype))  # noqa: E731
+    m = _made()
+    for name, x in vars(m).items():
+        if isinstance(x, torch.Tensor):
+            setattr(m, name, there(x))
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda index: 0)
+    sizes = {"unison_kv_evict_workspace": lambda cache: 16}  # every other function is not to be called
+    monkeypatch.setattr(kv, "lib", lambda: types.SimpleNamespace(
+        **{x: lambda *_: pytest.fail("called") for x in kv.EXPORTS} | sizes))
+    cache, tree, n = m.cache(kv), m.tree(kv), m.total
+    path, lse, new = zeros(2, 3, dtype=torch.int32), zeros(n, 8), zeros(n, 2)
+    p, i, u, us, two = zeros(n, 10), zeros(n, dtype=torch.int32), zeros(n), zeros(2), zeros(2, dtype=torch.int32)
+    outs = dict(path=path, n_path=two, next_token=two)
+    for name, call in (("n_path", lambda: kv.observe(cache, tree, m.q, lse, m.k_new, path=path, mass_new=new)),
+                       ("n_path", lambda: kv.commit(cache, tree, m.k_new, m.v_new, path=path)),
+                       ("lse", lambda: kv.observe(cache, tree, m.q, None, m.k_new, mass_new=new)),
+                       ("keep", lambda: kv.evict(cache, None)),
+                       ("token", lambda: kv.verify(tree, None, p, p, u, us, **outs)),
+                       ("u", lambda: kv.verify(tree, i, p, p, None, us, **outs)),
+                       ("u_sample", lambda: kv.verify(tree, i, p, p, u, None, **outs)),
+                       ("length", lambda: kv.Cache(m.k, m.v, m.page_table, None))):
+        with pytest.raises(ValueError, match=rf"^{name}:"):
+            call()
 
 
 def test_binding_refuses_the_host_and_other_devices(kv):
