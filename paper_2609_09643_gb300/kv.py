@@ -188,8 +188,9 @@ def _path(tree, path, n_path):
 
 
 def _on_gpu(cache, x, workspace=None):
-    """The kernels follow pointers: none to the host, none to another device."""
+    """The kernels follow pointers: none to the host, none to another device, scratch as far as it says."""
     device = cache.device
+    _need(workspace is None or workspace.is_contiguous(), "workspace: contiguous")
     if not cache.on_gpu and cache.n_seqs or x is not None and x.device != device or \
             workspace is not None and workspace.device != device:
         raise ValueError(f"cache, tree and workspace: on one CUDA device ({device})")

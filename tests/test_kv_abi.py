@@ -304,6 +304,21 @@ def test_binding_refuses_calls_without_a_wanted_tensor(kv, monkeypatch):
             call()
 
 
+@pytest.mark.parametrize("bad", [lambda n: torch.zeros(1, dtype=torch.uint8).expand(n),
+                                 lambda n: torch.zeros(2 * n, dtype=torch.uint8)[::2]])
+def test_binding_refuses_scratch_with_gaps(kv, bad):
+    """Elements are not bytes in a row there: an expanded tensor's are one byte."""
+    m = _made()
+    cache, tree, n = m.cache(kv), m.tree(kv), 1 << 20
+    keep = torch.zeros(2, dtype=torch.int32)
+    for call in (lambda w: kv.attend(cache, tree, m.q, m.k_new, m.v_new, workspace=w),
+                 lambda w: kv.evict(cache, keep, workspace=w)):
+        with pytest.raises(ValueError, match="contiguous"):
+            call(bad(n))
+        with pytest.raises(ValueError, match="CUDA"):  # this one is refused for being on the host alone
+            call(torch.zeros(n, dtype=torch.uint8))
+
+
 def test_binding_refuses_the_host_and_other_devices(kv):
     """Kernels follow pointers, so a tensor elsewhere is refused before any launch."""
     m = _made()
