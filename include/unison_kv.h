@@ -122,8 +122,10 @@ typedef struct {
  * A row that sees nothing gets out = 0 and lse = -inf.  What a mask hides does
  * not reach the result, NaN and infinities included.  Products are of the
  * type's values, sums in 32 bits; the weights exp(S - max) are rounded to the
- * type before they meet v.  Reads q, k_new, v_new; writes out, lse (lse may be
- * NULL).  Tokens outside every session's range are not written.
+ * type before they meet v (in FP16 multiplied by 2^7 or more before that, so
+ * that 2^-31 still counts, unless scores are beyond 2^19).  Reads q, k_new,
+ * v_new; writes out, lse (lse may be NULL).  Tokens outside every session's
+ * range are not written.
  * The result does not depend on timing: the same call gives the same bits.
  * UNISON_ERR_ARG: null or misaligned arrays, sizes that do not fit together,
  * a workspace that is too small (or not 16-byte aligned); UNISON_ERR_RANGE:

@@ -102,6 +102,7 @@ struct KvType<__nv_bfloat16> {
   }
   static __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
   static constexpr uint32_t kExponent = 0x7F80u;  // all ones: infinity or NaN
+  static constexpr int kMostWeight = 0;  // (log2)
 };
 template <>
 struct KvType<__half> {
@@ -111,6 +112,7 @@ struct KvType<__half> {
   }
   static __device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
   static constexpr uint32_t kExponent = 0x7C00u;
+  static constexpr int kMostWeight = 15;  // the largest number is just below 2^16
 };
 
 // A session's rows of the step's arrays, clamped to what the tree allows.
@@ -209,6 +211,15 @@ __device__ __forceinline__ void mma16816<__half>(float (&c)[4], const uint32_t (
                "{%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// What the weights 2^(score - reference) of a row are relative to, from its
+// maximum: the maximum itself in bf16.  In fp16 a weight below 2^-25 would count
+// in the row's sum but not in its products, so the reference lies kLower below
+// the maximum, as far as weights may exceed 1.  (Scores beyond 2^20 have no use
+// for it, and the difference would be rounded: a weight might not be finite.)
+template <int kLower>
+__device__ __forceinline__ float reference_of(float top) {
+  return kLower > 0 && fabsf(top) < 1048576.f ? top - kLower : top;
 }
 // 2^x; results below the normal range are 0.
 __device__ __forceinline__ float exp2_fast(float x) {

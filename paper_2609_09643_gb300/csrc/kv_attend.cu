@@ -29,7 +29,8 @@ constexpr int kAttendSmem = kAttendStages<DP> *kTile *DP * 4 + MT * 16 * DP * 2;
 // tile's rows are planned two tiles ahead of their use: first the page ids (into
 // a register), then the rows' addresses (shared memory), then the copies.
 // Weights are rounded to the cache's type, as the products' operands have to be;
-// their sum l is of the weights before that.
+// their sum l is of the weights before that.  In fp16 they are relative to a
+// reference 2^15 below the row's maximum, so that 2^-40 of it still counts.
 // One token x 4 heads over 64 sessions of 512 to 32k keys (8 KV heads of 128,
 // 2.07 GB): 303 us, 6.8 TB/s; 8 tokens over two sessions of 128k keys (1.07 GB):
 // 165 us, 6.5 TB/s; one token of one session of 2,100 keys: 8 us.
@@ -40,6 +41,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) attend_kernel(con
   constexpr int kRows = MT * 16;
   constexpr int kGroups = 4 / MT;      // groups of warps with keys of their own
   constexpr int kWarpKeys = kTile / kGroups;
+  constexpr int kLower = KvType<T>::kMostWeight;
   constexpr int kChunks = DP / 8;
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ KvRunShared shared_run;
@@ -163,7 +165,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) attend_kernel(con
     float o[DP / 8][4];
 #pragma unroll
     for (int i = 0; i < DP / 8; i++) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-    float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;  // running maximum (log2 units) and sum
+    float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;  // reference (log2 units) and sum
     const float to_log2 = P.s.scale * 1.4426950408889634f;
 
     for (int kt = kt0; kt < kt1; kt++) {
@@ -226,7 +228,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) attend_kernel(con
         t0 = fmaxf(t0, __shfl_xor_sync(~0u, t0, d));
         t1 = fmaxf(t1, __shfl_xor_sync(~0u, t1, d));
       }
-      const float n0 = fmaxf(m0, t0), n1 = fmaxf(m1, t1);
+      const float n0 = fmaxf(m0, reference_of<kLower>(t0)), n1 = fmaxf(m1, reference_of<kLower>(t1));
       const float u0 = n0 == -INFINITY ? 0.f : n0, u1 = n1 == -INFINITY ? 0.f : n1;
       const float f0 = exp2_fast(m0 - u0), f1 = exp2_fast(m1 - u1);
       m0 = n0;

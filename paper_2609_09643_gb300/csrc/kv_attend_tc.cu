@@ -15,7 +15,9 @@
 // us, in one turn 197).  O is rescaled only when a row's maximum has grown by
 // more than 2^8 over the one its weights are relative to; the sums are 32 bits
 // wide, so weights up to 2^8 cost no accuracy.  They are rounded to the cache's
-// type for the second product; their sum is of the weights before that.
+// type for the second product; their sum is of the weights before that.  In fp16
+// the reference lies 2^7 below the maximum that it was taken from, as weights may
+// be up to 2^15 there: so 2^-32 of the maximum still counts.
 //
 // Up to 128 rows memory bounds it (5.9 TB/s at 128 rows of that case, 185 us);
 // from 256 on the tensor cores and the two warps per scheduler that compute the
@@ -38,7 +40,7 @@ namespace {
 constexpr int kThreads = 416;
 constexpr int kTile = 128;
 constexpr int kCopyWarp = 8, kIssueWarp = 12;
-constexpr float kSlack = 8.f;
+constexpr int kSlack = 8;
 // Segments whose flags of odd values are kept.  A segment that takes one tile
 // passes the second slot's warps by, so nothing else holds the copies back until
 // these have read the flags of an earlier one: they wait for that (seg_done).
@@ -91,6 +93,7 @@ template <typename T, int DP>
 __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_constant__ AttendTcParams P) {
   follow_last_kernel();
   constexpr uint32_t kTileBytes = kTile * DP * 2, kBlock = kTile * 128;
+  constexpr int kLower = KvType<T>::kMostWeight > kSlack ? KvType<T>::kMostWeight - kSlack : 0;
   extern __shared__ unsigned char smem_raw[];
   __shared__ TcShared<DP> sh;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -448,7 +451,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
               p[i * 16 + j / 2] = KvType<T>::pack(a, b);
             }
           }
-          done = !__any_sync(~0u, fmaxf(t[0], t[1]) * c > m + kSlack);
+          done = !__any_sync(~0u, reference_of<kLower>(fmaxf(t[0], t[1]) * c) > m + kSlack);
           if (done) {
             tmem_st32(s_addr, p);
             tmem_st32(s_addr + 32, p + 32);
@@ -474,7 +477,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
 #pragma unroll
             for (int j = 0; j < 32; j++) t = fmaxf(t, __uint_as_float(x[0][j]));
           }
-          const float to = kt == begin || t * c > m + kSlack ? t * c : m;
+          const float top = reference_of<kLower>(t * c), to = kt == begin || top > m + kSlack ? top : m;
           if (kt > begin && __any_sync(~0u, to != m)) {
             const float f = m == to ? 1.f : exp2_fast(m - to);
             ok = __all_sync(~0u, bar_wait(smem_u32(&sh.pv_done[q]), (s_no - 1) & 1, &sh.dead));

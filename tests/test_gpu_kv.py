@@ -145,6 +145,53 @@ def test_attend_large_and_equal_scores(kv):
     check_attend(kv, m)
 
 
+@pytest.mark.parametrize("group,tokens", [(1, 1), (8, 3), (1, 40), (4, 40)])
+def test_attend_many_small_weights_in_half_precision(kv, group, tokens):
+    """Each of 4,000 weights is 2^-25.2 of the largest, less than fp16's steps near 0; all of them are what the
+    output consists of.  A weight counts down to 2^-31 at least: it may be off by 2^-32 (half a step), and the
+    output by half a step of its own, 2^-25.  (The log-sum: 62 additions to about 1 in 32 bits, its own rounding.)"""
+    n, sessions = 4000, 320  # so many that a CTA has whole sessions
+    m = Made([0] * sessions, [tokens] * sessions, hkv=1, group=group, page=64, dtype="fp16", room=n + 64, seed=1)
+    m.length.fill_(n)
+    m.k.zero_()
+    m.v.fill_(1)
+    first = torch.from_numpy(m.table[:, 0]).long().cuda()
+    m.k[first, 0, 0, 0], m.v[first, 0, 0] = 17.5, 0
+    m.q.zero_()
+    m.q[..., 0] = 1
+    m.k_new.zero_()
+    m.k_new[..., 0], m.v_new[:] = -100, 0
+    out, lse = kv.attend(m.cache(kv), m.tree(kv), m.q, m.k_new, m.v_new, scale=1.0)
+    small = (n - 1) * math.exp(-17.5)
+    want = small / (1 + small)
+    assert np.max(np.abs(f64(out) - want)) <= n * 2.0 ** -32 + 2.0 ** -25 + 2.0 ** -18 * want
+    assert np.max(np.abs(f64(lse) - 17.5 - math.log1p(small))) <= 2.0 ** -17
+
+
+@pytest.mark.parametrize("group,tokens", [(1, 1), (1, 40), (4, 40)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_attend_scores_beyond_24_bits(kv, group, tokens, dtype):
+    """Scores from 2^16 to 2^26, ascending through the tiles and down again: the
+    largest key has all the weight, whose value is the output as it is."""
+    n = 900
+    m = Made([n], [tokens], hkv=1, group=group, dtype=dtype, seed=4)
+    s = torch.arange(n)
+    at = torch.from_numpy(m.table[0]).long()[s // m.page].cuda(), 0, (s % m.page).cuda()
+    size = 2.0 ** (torch.where(s < 700, s, 1399 - s).float() / 70)  # 1 .. 2^10, in steps of 1%
+    m.k[at] = 0
+    m.k[(*at, 0)] = size.to(m.k.dtype).cuda()
+    keys = m.k[(*at, 0)].float()
+    m.q.zero_()
+    m.k_new.zero_()
+    for q in (2.0 ** 13, 2.0 ** 14, 2.0 ** 15):
+        m.q[..., 0] = q
+        out, lse = kv.attend(m.cache(kv), m.tree(kv), m.q, m.k_new, m.v_new, scale=2.0)
+        best = (keys == keys.max()).nonzero()[:, 0]
+        want = m.v[at][best].double().mean(0)
+        assert float((out.double() - want).abs().max()) <= float(want.abs().max()) * ref.UNIT[dtype] * 2
+        assert float((lse / (2 * q * keys.max()) - 1).abs().max()) <= 2.0 ** -21
+
+
 @pytest.mark.parametrize("scale", [0.0, -0.3, 2.5])
 def test_attend_scale(kv, scale):
     check_attend(kv, Made([100, 3], [2, 30], group=4, seed=6), scale=scale)
