@@ -228,6 +228,25 @@ def test_scratch_and_results_belong_to_the_given_stream(kv):
     assert torch.equal(got, want) and list(cache.scratch) == [side.cuda_stream, 0]
 
 
+def test_one_cache_on_two_streams_at_once(kv):
+    """Each stream has scratch of its own: calls that overlap do not disturb each other."""
+    m = Made([9000, 17, 900, 3000], [8, 1, 30, 5], group=4, d=128, page=64, seed=24)
+    cache, tree = m.cache(kv), m.tree(kv)
+    want = kv.attend(cache, tree, m.q, m.k_new, m.v_new)
+    other = m.q.flip(0).contiguous()
+    want_other = kv.attend(cache, tree, other, m.k_new, m.v_new)
+    torch.cuda.synchronize()
+    sides, got = [torch.cuda.Stream() for _ in range(2)], [[], []]
+    for _ in range(10):
+        for i, q in enumerate((m.q, other)):
+            got[i].append(kv.attend(cache, tree, q, m.k_new, m.v_new, stream=sides[i]))
+    torch.cuda.synchronize()
+    for results, (out, lse) in zip(got, (want, want_other)):
+        assert all(torch.equal(o, out) and torch.equal(x, lse) for o, x in results)
+    work = [cache.scratch[s.cuda_stream] for s in sides]
+    assert work[0].data_ptr() != work[1].data_ptr()
+
+
 def test_attend_absent_pages_and_bad_values_are_reported(kv):
     m = Made([100, 50, 20], [2, 20, 3], group=4, page=16, seed=13)
     full = [m.slots(f64(x), 0) for x in (m.k, m.v)]
@@ -720,6 +739,27 @@ def test_verify_many_sessions_agree_with_the_target(kv):
     path, n_path, nxt = kv.verify(m.tree(kv), token.cuda(), rows(p), rows(q), torch.rand(2 * n, generator=g).cuda(),
                                   torch.rand(n, generator=g).cuda())
     first = torch.where(n_path.cpu() == 2, token[1::2], nxt.cpu())
+    freq = torch.bincount(first.long(), minlength=vocab) / n
+    assert float((freq - p).abs().max()) < 5 * math.sqrt(0.25 / n)
+
+
+@pytest.mark.parametrize("siblings", [2, 3, 5])
+def test_verify_siblings_agree_with_the_target(kv, siblings):
+    """Several children of the root, drawn from q independently: the emitted token follows p all the same."""
+    n, vocab, t = 20000, 7, siblings + 1
+    m = Made([0] * n, [t] * n, seed=1, hkv=1, group=1, d=8, page=64, room=0)
+    m.parent = torch.tensor([-1] + [0] * siblings, dtype=torch.int32).repeat(n).cuda()
+    g = torch.Generator().manual_seed(siblings)
+    p = torch.softmax(torch.randn(vocab, generator=g) * 1.5, 0)
+    q = torch.softmax(torch.randn(vocab, generator=g) * 1.5, 0)
+    token = torch.multinomial(q, n * t, replacement=True, generator=g).to(torch.int32)
+    rows = lambda x: x[None].expand(n * t, -1).contiguous().cuda()  # noqa: E731
+    path, n_path, nxt = kv.verify(m.tree(kv), token.cuda(), rows(p), rows(q), torch.rand(n * t, generator=g).cuda(),
+                                  torch.rand(n, generator=g).cuda())
+    path, n_path = path.cpu().long(), n_path.cpu()
+    taken = token.view(n, t).gather(1, path[:, 1:2].clamp(min=0))[:, 0]
+    first = torch.where(n_path == 2, taken, nxt.cpu())
+    assert bool((n_path <= 2).all()) and bool((n_path == 1).any())
     freq = torch.bincount(first.long(), minlength=vocab) / n
     assert float((freq - p).abs().max()) < 5 * math.sqrt(0.25 / n)
 
