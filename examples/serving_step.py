@@ -5,7 +5,8 @@ the GPU in between: attention over the drafted trees, verification of the
 drafts, the weight that the accepted tokens give to the cached ones, their keys
 and values into the pages, eviction down to each session's budget.  In a tool
 gap the live ranking names the sessions that should leave the fast tier; their
-most attended tokens move to the other tier's cache.
+most attended tokens are copied to the other tier's cache (their pages here are
+the program's to give away then).
 
 The model is left out: queries, keys, values and probabilities are random, of
 the shapes that a model of one layer would give.

@@ -33,7 +33,9 @@ constexpr int kAttendSmem = kAttendStages<DP> *kTile *DP * 4 + MT * 16 * DP * 2;
 // reference 2^15 below the row's maximum, so that 2^-40 of it still counts.
 // One token x 4 heads over 64 sessions of 512 to 32k keys (8 KV heads of 128,
 // 2.07 GB): 303 us, 6.8 TB/s; 8 tokens over two sessions of 128k keys (1.07 GB):
-// 165 us, 6.5 TB/s; one token of one session of 2,100 keys: 8 us.
+// 165 us, 6.5 TB/s; one token of one session of 2,100 keys: 8 us.  Heads of 256
+// (16 sessions of 16k keys, 8 KV heads, 2.15 GB): 382 us with 4 or 16 rows, 5.6
+// TB/s, 515 with 32, 720 with 64, and 720 more for every 64 rows.
 template <typename T, int DP, int MT>
 __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) attend_kernel(const AttendParams P) {
   follow_last_kernel();
@@ -502,10 +504,10 @@ struct AttendPlan {
 };
 
 // Variants, by the query rows per KV head (16 sessions of 16k keys, 8 KV heads):
-//   up to 32 the one above: 176 us for 32 rows of 128 elements (the other one:
-//            186), 114 of 64 (148)
-//   more     tensor cores with sums in tensor memory: 180 us for 48 rows of 128
-//            (342 here, row tile by row tile), 125 of 64 (158); 185 and 126 for 128
+//   up to 32 the one above: 175 us for 32 rows of 128 elements (the other one:
+//            186), 113 of 64 (148)
+//   more     tensor cores with sums in tensor memory: 182 us for 48 rows of 128
+//            (342 here, row tile by row tile), 124 of 64 (158); 187 and 126 for 128
 // Head sizes above 128 do not fit the latter's tensor memory.
 AttendPlan attend_plan(int head_dim, int max_rows) {
   AttendPlan p;

@@ -13,19 +13,19 @@
 // query tile alone takes the keys in two turns instead, each with an O of its
 // own, joined at the end (64 rows of 16 sessions of 16k keys, head size 128: 180
 // us, in one turn 197).  O is rescaled only when a row's maximum has grown by
-// more than 2^8 over the one its weights are relative to; the sums are 32 bits
+// more than 2^8 over the one that their reference was taken from; the sums are 32 bits
 // wide, so weights up to 2^8 cost no accuracy.  They are rounded to the cache's
 // type for the second product; their sum is of the weights before that.  In fp16
 // the reference lies 2^7 below the maximum that it was taken from, as weights may
 // be up to 2^15 there: so 2^-32 of the maximum still counts.
 //
-// Up to 128 rows memory bounds it (5.9 TB/s at 128 rows of that case, 185 us);
+// Up to 128 rows memory bounds it (5.8 TB/s at 128 rows of that case, 187 us);
 // from 256 on the tensor cores and the two warps per scheduler that compute the
 // weights: 64 nodes x 8 heads over 32 sessions of 15k to 16k keys, 8 KV heads
-// (1.06 PFLOP), take 740 us, 1.43 PFLOP/s, 74% of what a plain matrix product
-// reaches here (800 us in a stream of such calls, under the power limit).  512
-// rows' CTAs work in pairs on the same keys, which the second finds in the L2
-// cache.
+// (1.06 PFLOP), take 750 us, 1.41 PFLOP/s, 73% of what a plain matrix product
+// reaches here (a long stream of such calls and their joins: 820 to 830 us a
+// call, under the power limit).  512 rows' CTAs work in pairs on the same keys,
+// which the second finds in the L2 cache.
 //
 // A wait that runs out ends the CTA (every role sees `dead`) and reports
 // UNISON_ERR_TIMEOUT.  Every copying warp waits for every slot, also for those

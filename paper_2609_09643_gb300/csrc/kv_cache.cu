@@ -521,9 +521,10 @@ extern "C" int unison_kv_evict(const unison_kv_cache *cache, const unison_kv_cac
   p.moves = static_cast<int32_t *>(workspace);
   p.count = p.moves + segs * room;
   // CTAs per segment: as many as the segments leave room for (two CTAs on a
-  // multiprocessor, though four fit: clusters then wait for places; of sessions
-  // of 8k to 32k slots 64 segments take 33 us against 73, 128 take 39 against 45,
-  // and one CTA each 35 and 53), none with less than 2,048 slots.
+  // multiprocessor, though four fit: clusters then wait for places; between events
+  // around the launch, which add 4 us, 64 segments of 8k to 32k slots take 32 us
+  // against 71, 128 take 39 against 45, and one CTA each 50 and 52), none with less
+  // than 2,048 slots.
   const int64_t spare = (int64_t)kv_sm_count() * 2 / (int64_t)segs;
   int ctas = 1;
   while (ctas < kMaxCluster && ctas * 2 <= spare && (int64_t)ctas * 2048 < room) ctas *= 2;
@@ -536,9 +537,9 @@ extern "C" int unison_kv_evict(const unison_kv_cache *cache, const unison_kv_cac
                  evict_select_kernel, p);
   if (rc != UNISON_OK) return rc;
   // A CTA moves 256 slots at a time.  Enough CTAs for all at once where a cache
-  // is copied (16 sessions' 8,192 slots: 179 us, with a fifth of the CTAs 192);
-  // few where a session at its budget drops a handful (8 slots of 64 sessions:
-  // 10 us, with five times the CTAs 16).
+  // is copied (16 sessions' 8,192 slots: 179 us between events around the launch,
+  // with a fifth of the CTAs 192); few where a session at its budget drops a
+  // handful (up to 8 slots of 64 sessions: 10 us, with five times the CTAs 15).
   const int64_t most = into ? min(room, (int64_t)into->max_pages * into->page_size) : room / 2;
   const int64_t fill = ((int64_t)kv_sm_count() * (into ? 32 : 6) + segs - 1) / (int64_t)segs;
   p.per_seg = (int)max((int64_t)1, min((most + 255) / 256, fill));

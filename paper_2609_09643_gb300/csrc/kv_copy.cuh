@@ -8,11 +8,12 @@
 // single rows.  128 keys of 128 elements cost the warps about 2,000 cycles by
 // copies and next to nothing by TMA; but a box takes the hardware 90 cycles,
 // however small.  16 sessions of 16k keys, 8 KV heads, in pages of 8 / 16 / 64
-// slots: attention of 64 rows 251 / 200 / 180 us by boxes, 194 by copies (head
-// size 128), 171 / 143 / 124 and 156 (64); observation of 8 to 64 rows 168 /
-// 113 / 113 and 113 by copies.  So boxes have 16 slots or more, except where
-// query rows leave place for two tiles only: 512 rows' observation, few of them
-// accepted, takes 168 by boxes of 8 and 350 by copies, which are not early enough.
+// slots: attention of 64 rows 259 / 203 / 183 us by boxes, 198 by copies (head
+// size 128), 178 / 143 / 124 and 159 (64); observation of 8 to 64 rows 169 /
+// 112 / 101 by boxes and 120 / 113 / 108 by copies.  So boxes have 16 slots or
+// more, except where query rows leave place for two tiles only: 512 rows'
+// observation, few of them accepted, takes 168 by boxes of 8 and 343 by copies,
+// which are not early enough.
 #pragma once
 
 #include <cuda.h>

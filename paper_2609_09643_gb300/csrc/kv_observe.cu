@@ -16,7 +16,10 @@ constexpr int kObserveSmem = kStages *kTile *DP * 2 + QR *DP * 2;
 // The keys are the rows of the matrix product and the query rows its columns:
 // a thread holds two keys' products with two query rows at a time, and adds up
 // their weights without leaving its registers.  Every CTA takes an equal run of
-// the call's key tiles.  Query rows beyond QR are loaded again for every tile.
+// the call's key tiles.  Query rows beyond QR are loaded again for every tile,
+// which bounds it by far then.  16 sessions of 16k keys, 8 KV heads: head size
+// 256 with 4 rows 498 us (2.2 TB/s), 32 rows 570, 64 rows 721, 256 rows 9.3 ms;
+// 1,024 rows of 64 or 128 elements 17 ms (512 on the tensor cores: 260, 282 us).
 template <typename T, int DP, int QR>
 __global__ void __launch_bounds__(kThreads) observe_kernel(const ObserveParams P) {
   follow_last_kernel();

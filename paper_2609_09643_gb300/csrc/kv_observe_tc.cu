@@ -82,9 +82,9 @@ __global__ void __launch_bounds__(kThreads, 1) observe_tc_kernel(const __grid_co
 
   // A tile's share of the run, in units of 33 ns: its keys' way here, or the
   // products and weights of its chunks of 128 query rows, where those take
-  // longer.  (16 sessions of 16k keys, 8 KV heads, head size 128: 115 us with 8
-  // rows, 121 with 128, 154 with 136, 166 with 256, 221 with 384, 279 with 512;
-  // head size 64: 82, 88, 145, 160, 209, 258.  Beside sessions of many rows,
+  // longer.  (16 sessions of 16k keys, 8 KV heads, head size 128: 101 us with 8
+  // rows, 106 with 128, 154 with 136, 166 with 256, 222 with 384, 282 with 512;
+  // head size 64: 81, 88, 146, 161, 212, 259.  Beside sessions of many rows,
   // which leave them the memory, few rows take a fifth less.)
   const int keys_way = DP == 64 ? 20 : P.slots > 2 || P.k_boxes.rows > 8 ? 26 : P.k_boxes.rows ? 40 : 80;
   auto share = [&](int rows) {

@@ -12,7 +12,7 @@
 // left, and a session's next pass cannot begin before.  128 sessions' trees of 32
 // nodes over 128,000 entries of 32 bits (one to four passes mostly, from the L2
 // cache after the first): 63 us, while reading every row that is wanted once
-// would take 19.  One session's chain of five over 32,000 entries: 6 us.
+// would take 19; without q 78.  One session's chain of five over 32,000 entries: 6 us.
 #include <cooperative_groups.h>
 
 #include <type_traits>
@@ -267,8 +267,9 @@ template <typename T>
 int verify_run(const unison_kv_tree &t, const unison_kv_verify_args &a, void *stream) {
   // CTAs per session: as many as the sessions leave room for (two CTAs on a
   // multiprocessor, two rounds of them: a session takes one to four passes, and
-  // those that end early make room; one round takes 107 us where two take 87),
-  // none with less than 2,048 entries.
+  // those that end early make room; 128 sessions over 128,000 entries take 90 us in
+  // one round, 67 in two and 73 in four, between events around the launch, which
+  // add 4), none with less than 2,048 entries.
   const int room = 4 * kv_sm_count() / t.n_seqs, wanted = (a.vocab + 2047) / 2048;
   int ctas = 1;
   while (ctas < kMaxCluster && ctas * 2 <= max(room, 1) && ctas < wanted) ctas *= 2;
