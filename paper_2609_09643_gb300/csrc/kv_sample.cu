@@ -8,7 +8,7 @@
 // index) less what is below min-p, so it is known by its last entry: the cut.
 //   1  A bound below what may be kept.  The threads' maxima are entries, too:
 //      where their running count reaches k, or their running weight the goal of
-//      top-p, lies at or below the cut.  Entries of less than (tail that top-p
+//      top-p, lies at or below the cut.  Entries of up to (tail that top-p
 //      leaves out) / vocab cannot reach it either, nor those below min-p.
 //   2  The entries above the bound, a few dozen mostly, go into one list, are
 //      compared one by one, and give the cut, the sum of the kept weights and the
@@ -789,8 +789,10 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const unison_kv_sam
     __syncthreads();
     // (less than the slot's edge by more than its rounding)
     if (sh.slot >= 0) low = fmaxf(low, kLeast + sh.slot / scale - 0.001f);
-    // (a weight's rounding, and the logarithm's, are far below the 0.01)
-    if (!by_count) low = fmaxf(low, log2f((float)(weight - goal) / (float)V + 1.f) - 40.01f);
+    // The cut and the entries behind it sum to more than weight - goal, so the cut's
+    // weight, the largest of theirs, is above a V-th of that, and a whole number above 0.
+    // (The roundings of 2^t, the quotient and the logarithm are far below the 0.01.)
+    if (!by_count) low = fmaxf(low, log2f(fmaxf((float)(weight - goal) / (float)V, 1.f)) - 40.01f);
     // how many of them lie in whole slots above the bound
     if (min((int)((low - kLeast) * scale), kSlots - 1) == kSlots - 2 - tid) sh.count = (uint32_t)maxima;
   }
