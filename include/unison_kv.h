@@ -170,7 +170,8 @@ int unison_kv_attend_shared(const unison_kv_cache *cache, const unison_kv_prefix
  *   (a, b) -> (a cos t - b sin t, b cos t + a sin t), t = position * inv_freq[j]
  * for the pairs j < rot_dim / 2: elements j and j + rot_dim / 2, or 2 j and
  * 2 j + 1 where interleaved is set.  Elements from rot_dim on keep y.  32-bit
- * arithmetic, t to 2^-30 for any position; one rounding at the end.
+ * arithmetic; t modulo 2 pi to 1.05 pi 2^-25 (24 bits of half a turn) for any
+ * position and frequency; one rounding at the end.
  * position: of every token; or NULL: next_pos[b] of the cache plus the number
  * of earlier nodes that the node's mask names (its depth, which is what
  * unison_kv_commit will count), tokens outside every session's range are then

@@ -11,9 +11,11 @@
 // in place is as good as out of place.
 //
 // Angles in whole numbers: inv_freq / 2 pi as a 64-bit fraction of a turn, times
-// the position modulo 2^64, is the fraction of a turn that is left, to 2^-32 for
-// any position; in 32 bits of float a position of 10^6 would leave it uncertain
-// by 0.06.
+// the position modulo 2^64, is the fraction of a turn that is left, to 2^-33 for
+// any position and frequency; in 32 bits of float a position of 10^6 would leave it
+// uncertain by 0.06.  Its first 32 bits become a number of 24 (what sincospif
+// takes): half a unit of half a turn, pi 2^-25, is what the angle is known to, as
+// 32-bit cosines and sines are to 2^-25 themselves.
 //
 // Bound by memory, if the operations are few: 13,750 tokens of 32 + 8 heads of 128
 // (282 MB): 51 us, 5.5 TB/s, 0.81 of the copy rate, instructions issued in 63% of
@@ -59,21 +61,24 @@ __device__ __forceinline__ bool token_of(const RotateParams &P, int64_t item, in
   return true;
 }
 
-// f / (2 pi) modulo 1, as a fraction of 2^64.
+// f / (2 pi) modulo 1, as a fraction of 2^64, rounded towards zero: from 128 bits
+// of 1 / (2 pi), so that what a position multiplies is off by less than a unit for
+// every |f| up to 2^24.
 __device__ __forceinline__ uint64_t turn_of(float f) {
-  constexpr uint64_t kTurn = 0x28BE60DB9391054Aull;  // 2^64 / (2 pi)
+  constexpr uint64_t kTurn = 0x28BE60DB9391054Aull, kRest = 0x7F09D5F47D4D3770ull;  // 2^128 / (2 pi)
   const uint32_t bits = __float_as_uint(f);
   const int e = bits >> 23 & 255;
   const uint64_t m = (bits & 0x7FFFFFu) | (e ? 0x800000u : 0u);
   const int shift = 150 - (e ? e : 1);  // f = m 2^-shift
   const uint64_t lo = m * kTurn, hi = __umul64hi(m, kTurn);
+  const uint64_t w1 = lo + __umul64hi(m, kRest), w2 = hi + (w1 < lo);  // m 2^64 / (2 pi), whole numbers
   uint64_t t;
   if (shift <= 0)
-    t = shift > -64 ? lo << -shift : 0;
+    t = shift > -64 ? w1 << -shift : 0;
   else if (shift < 64)
-    t = lo >> shift | hi << (64 - shift);
+    t = w1 >> shift | w2 << (64 - shift);
   else
-    t = shift < 128 ? hi >> (shift - 64) : 0;
+    t = shift < 128 ? w2 >> (shift - 64) : 0;
   return bits >> 31 ? 0 - t : t;
 }
 
@@ -81,7 +86,7 @@ __device__ __forceinline__ uint64_t turn_of(float f) {
 __device__ __forceinline__ float2 turned(const RotateParams &P, int j, int position) {
   const uint64_t t = turn_of(P.a.inv_freq[j]) * (uint64_t)(int64_t)position;
   float s, c;
-  sincospif((float)(int32_t)(t >> 32) * (1.f / 2147483648.f), &s, &c);  // (a signed fraction of half a turn)
+  sincospif((float)(int32_t)(t >> 32) * (1.f / 2147483648.f), &s, &c);  // (signed, in half turns: 24 bits of it)
   return make_float2(c, s);
 }
 __device__ __forceinline__ float norm_factor(const RotateParams &P, float squares) {
