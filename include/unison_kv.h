@@ -293,8 +293,9 @@ int unison_kv_verify(const unison_kv_tree *tree, const unison_kv_verify_args *ar
  * T <= 0 or NaN: k = 1, the largest logit.  P and u count in steps of 2^-24
  * (clamped to [0, 1] and [0, 1)); the 32-bit difference, quotient and product
  * are rounded one by one, exp2f is the hardware's ex2.approx, and sums are of whole numbers, so
- * decisions do not depend on the order of summation.  A row without a logit
- * above -inf gets token -1 and p = 0.
+ * decisions do not depend on the order of summation.  p is rounded once to 32
+ * bits, and then to its type.  A row without a logit above -inf gets token -1
+ * and p = 0.
  * Each of the four settings is an array of a value for each row, or NULL and one
  * value for all.  u and token (both or neither), p: NULL where not wanted; p is
  * what unison_kv_verify takes as p or q.  Types of logits and of p: BF16, FP16 or FP32;

@@ -87,6 +87,19 @@ __device__ __forceinline__ int64_t times(float p, int64_t w) {
   return u * (w >> 24) + ((u * (w & 0xFFFFFF)) >> 24);
 }
 
+// 1 / s for a whole number s, as two numbers: the first quotient, and what its
+// remainder adds.  Each of the roundings is 2^-47 of it at most, so w times it is
+// the quotient w / s rounded once, to 2^-24 (1 + 2^-20).
+struct Inverse {
+  float high, low;
+  __device__ __forceinline__ explicit Inverse(int64_t s) {
+    const float a = (float)s, b = (float)(s - (int64_t)a);
+    high = __fdiv_rn(1.f, a);
+    low = __fmul_rn(fmaf(-high, b, fmaf(-high, a, 1.f)), high);
+  }
+  __device__ __forceinline__ float operator()(float w) const { return fmaf(w, high, __fmul_rn(w, low)); }
+};
+
 struct Shared {
   unsigned long long pushed[2][kMaxCluster];  // one number of every CTA, in two sets by turns
   unsigned long long warp[kWarps];
@@ -282,10 +295,10 @@ __device__ __noinline__ void general(const unison_kv_sample_args &a, Shared &sh)
     total += p[c];
   }
   if (a.p) {
-    const float sum = (float)max(total, (int64_t)1);
+    const Inverse of_sum(max(total, (int64_t)1));
     const int64_t at = row * a.p_row;
     each([&](float y, int i) {
-      const float v = __fdiv_rn((float)kept(y, i), sum);
+      const float v = of_sum((float)kept(y, i));
       if (a.p_dtype == UNISON_KV_FP32)
         static_cast<float *>(a.p)[at + i] = v;
       else if (a.p_dtype == UNISON_KV_BF16)
@@ -692,12 +705,12 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const unison_kv_sam
     const float d = exp2_fast(exponent(x));
     return d >= least ? d : 0.f;
   };
-  float inverse = 0.f, least_logit = -INFINITY;  // no logit below the latter is kept
-  auto share = [&](float x, int index) -> float {
+  float least_logit = -INFINITY;  // no logit below it is kept
+  auto share = [&](float x, int index, const Inverse &of_sum) -> float {
     const float d = kept(x, index);
-    return d > 0.f ? truncf(__fmul_rn(d, 1099511627776.f)) * inverse : 0.f;
+    return d > 0.f ? of_sum(truncf(__fmul_rn(d, 1099511627776.f))) : 0.f;
   };
-  auto put = [&](auto *p) {
+  auto put = [&](auto *p, const Inverse &of_sum) {
     using P = typename std::remove_pointer<decltype(p)>::type;
     p += row * a.p_row - shift;  // as the row's pieces lie
     if constexpr (sizeof(P) == sizeof(T)) {
@@ -715,7 +728,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const unison_kv_sam
           float x[kN];
           Piece<T>::get(all, x);
 #pragma unroll
-          for (int j = 0; j < kN; j++) x[j] = share(x[j], e + j - shift);
+          for (int j = 0; j < kN; j++) x[j] = share(x[j], e + j - shift, of_sum);
           if (whole) {
             uint32_t v[4];
 #pragma unroll
@@ -738,18 +751,18 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const unison_kv_sam
 #pragma unroll 4
     for (int i = lane; i < span; i += 32) {
       const int e = begin + i;
-      if (e >= shift && e < end) store_number(p + e, share(number<T>(data[i]), e - shift));
+      if (e >= shift && e < end) store_number(p + e, share(number<T>(data[i]), e - shift, of_sum));
     }
   };
   auto put_all = [&](int64_t total) {
-    inverse = __fdiv_rn(1.f, (float)total);
+    const Inverse of_sum(total);
     least_logit = cut ? of_key((uint32_t)(cut >> 32)) : least > 0.f ? low_logit : -INFINITY;
     if (a.p_dtype == UNISON_KV_FP32)
-      put(static_cast<float *>(a.p));
+      put(static_cast<float *>(a.p), of_sum);
     else if (a.p_dtype == UNISON_KV_BF16)
-      put(static_cast<__nv_bfloat16 *>(a.p));
+      put(static_cast<__nv_bfloat16 *>(a.p), of_sum);
     else
-      put(static_cast<__half *>(a.p));
+      put(static_cast<__half *>(a.p), of_sum);
   };
 
   // ---- a bound below what may be kept
