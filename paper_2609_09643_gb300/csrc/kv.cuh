@@ -165,13 +165,9 @@ __device__ __forceinline__ int kv_page(const KvCacheArg &c, int b, int slot, int
 
 // The kernel before this one is complete and its results are seen; the next one
 // may be set up from here on (it waits in the same way).
-__device__ __forceinline__ void wait_for_last_kernel() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-__device__ __forceinline__ void next_kernel_may_begin() {
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-}
 __device__ __forceinline__ void follow_last_kernel() {
-  wait_for_last_kernel();
-  next_kernel_may_begin();
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
 __device__ __forceinline__ uint32_t smem_u32(const void *p) {

@@ -38,11 +38,7 @@ constexpr int kAttendSmem = kAttendStages<DP> *kTile *DP * 4 + MT * 16 * DP * 2;
 // TB/s, 515 with 32, 720 with 64, and 720 more for every 64 rows.
 template <typename T, int DP, int MT, int kUse>
 __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) attend_kernel(const __grid_constant__ AttendParams P) {
-  const bool beside = kUse == kList && P.beside;
-  if (beside)
-    next_kernel_may_begin();
-  else
-    follow_last_kernel();
+  follow_last_kernel();
   constexpr int kStages = kAttendStages<DP>;
   constexpr int kRows = MT * 16;
   constexpr int kGroups = 4 / MT;      // groups of warps with keys of their own
@@ -65,7 +61,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) attend_kernel(con
   auto seq_tiles = [&](int b) -> int64_t {
     if constexpr (kUse == kList) {
       const bool prefix = b < P.n_prefixes;
-      return attend_places(P, prefix, prefix ? b : b - P.n_prefixes, kTile, kRows, 1, true);
+      return attend_places(P, prefix, prefix ? b : b - P.n_prefixes, kTile, kRows, 1);
     }
     const int tokens = kv_tokens(P.t, b, P.c.status).count;
     const int row_tiles = (tokens * G + kRows - 1) / kRows;
@@ -73,12 +69,8 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) attend_kernel(con
   };
   KvRun run;
   if (!kv_find_run(run, shared_run, kUse == kList ? P.n_prefixes + P.n_sessions : P.c.n_seqs, gridDim.x, blockIdx.x,
-                   seq_tiles, [&](int64_t total) {
-                     return kUse == kList ? attend_most_runs(P, total, shared_run.part) : total;
-                   })) {
-    if (beside && blockIdx.x == 0) wait_for_last_kernel();
+                   seq_tiles, [](int64_t total) { return kUse == kList ? attend_most_runs(total) : total; }))
     return;
-  }
   int b = run.b;
   int64_t at = run.at, seq_begin = run.begin;
   const int64_t end = run.end;
@@ -377,7 +369,6 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) attend_kernel(con
       P.part[blockIdx.x] = {kv_run_of(run, span.begin + kSetup + key_tiles - 1), head, row_tile * kRows, rows,
                             tok.first};
   }
-  if (beside && blockIdx.x == 0) wait_for_last_kernel();  // this kernel's end is the other one's, too
 }
 
 // Joins the parts of the segments that lie in several runs, each by the CTAs of

@@ -45,14 +45,8 @@ struct AttendParams {
   const int32_t *first;        // sessions of a prefix
   int n_prefixes, n_sessions;  // of this launch's list
   AttendRows prefix_rows, own_rows;
-  int beside;  // the kernel before this one is another part of the same call: only its end is waited for
-  // Where prefixes and sessions have kernels of their own: the tiles of the other one's list (attend_most_runs).
-  int other_tile, other_rows, other_groups, sms;
 };
 
-// A run of a list with prefixes has that many places at least, on average: what is
-// split has to be joined, row by row.
-constexpr int kLeastPlaces = 4;
 // A segment's tiles come in the list of tiles behind kSetup places that stand
 // for its beginning (statistics, query rows, an empty pipeline), so that runs
 // of many short sessions take as long as runs of few long ones.  (64 sessions of
@@ -74,43 +68,20 @@ __device__ __forceinline__ KvRange attend_prefix_tokens(const AttendParams &P, i
 }
 // A prefix's, or a session's, places in the list of tiles.
 __device__ __forceinline__ int64_t attend_places(const AttendParams &P, bool prefix, int b, int tile, int rows,
-                                                 int groups, bool report) {
+                                                 int groups) {
   const KvCacheArg &c = prefix ? P.prefixes : P.c;
-  int32_t *status = report ? c.status : nullptr;
-  const int tokens = (prefix ? attend_prefix_tokens(P, b, status) : kv_tokens(P.t, b, status)).count;
+  const int tokens = (prefix ? attend_prefix_tokens(P, b, c.status) : kv_tokens(P.t, b, c.status)).count;
   const int tiles = attend_key_tiles(kv_length(c, b), tokens, tile, prefix);
   if (tiles == 0) return 0;
   const int row_tiles = (tokens * P.group + rows - 1) / rows;
   return (int64_t)(tiles + kSetup) * ((row_tiles + groups - 1) / groups) * c.n_heads;
 }
 
-// Runs of a list with prefixes, of `total` places.  Where prefixes (on the tensor
-// cores, a CTA on a multiprocessor) and sessions (bound by memory, two) have
-// kernels of their own, the prefixes' leaves multiprocessors to the sessions', so
-// that both end together, the rest of its CTAs end at once, and the
-// sessions' runs are finer, as they begin one by one.  The shares are those of the
-// multiprocessors' time: about 2.1 us for a prefix's tile (and 20 for beginning and
-// end) and 0.72 for a session's, at a head size of 128.  64 sessions of 512 to 8k
-// keys behind 32k shared ones: 170 us; one kernel after the other: 192.
-// By all threads of a CTA; part: 33 words of shared memory.
-__device__ __forceinline__ int64_t attend_most_runs(const AttendParams &P, int64_t total, int64_t *part) {
-  const int64_t most = (total + kLeastPlaces - 1) / kLeastPlaces;
-  if (!P.other_tile) return most;
-  const bool prefixes = P.n_prefixes > 0;
-  const int others = prefixes ? P.t.n_seqs : P.prefixes.n_seqs;
-  int64_t mine = 0, other;
-  for (int i = threadIdx.x; i < others; i += blockDim.x)
-    mine += attend_places(P, !prefixes, i, P.other_tile, P.other_rows, P.other_groups, false);
-  block_scan(mine, part, other);
-  const int groups = prefixes ? P.row_groups : P.other_groups;
-  const float size = P.c.head_dim <= 64 ? 0.5f : 1.f, sms = (float)P.sms;
-  const float of_prefixes = (float)(prefixes ? total : other) * groups * (2.1f * size);
-  const float of_sessions = (float)(prefixes ? other : total) * (0.72f * size);
-  const float all = (of_prefixes + of_sessions) / sms + 12.f;  // until both have ended
-  const float ctas = of_prefixes / fmaxf(all - 20.f, 1.f);
-  const bool together = ctas < 0.75f * sms;
-  if (prefixes) return together ? min(most, max((int64_t)(ctas / groups + 0.5f), (int64_t)1)) : most;
-  return together ? most : min(most, (int64_t)P.sms * 2);
+// Runs of a list with prefixes, of `total` places: a run has kLeastPlaces of them
+// at least, on average, as what is split has to be joined, row by row.
+constexpr int kLeastPlaces = 4;
+__device__ __forceinline__ int64_t attend_most_runs(int64_t total) {
+  return (total + kLeastPlaces - 1) / kLeastPlaces;
 }
 
 struct AttendSpan {

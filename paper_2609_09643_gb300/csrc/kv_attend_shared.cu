@@ -9,15 +9,17 @@
 //
 // Where prefixes and sessions suit the same kernel, both are one list of tiles
 // and one launch.  Else (a batch that decodes: hundreds of rows for a prefix, a
-// few for a session) the sessions' kernel is queued behind the prefixes' and may
-// begin on multiprocessors that the latter leaves (attend_most_runs).
+// few for a session) the sessions' kernel follows the prefixes'.
 //
 // 64 sessions of 512 to 8k keys behind 32k shared ones, 8 KV heads of 128 (0.87
-// GB, 128 us at the copy rate): 175 us, of which 8 join; one kernel after the
-// other: 192.  Trees of 32 nodes x 8 heads of 32 sessions behind two prompts of
-// 12k and 24k (0.68 TFLOP): 550 us, 440 of them the prefixes' products at 1.37
-// PFLOP/s, 30 the join of 65,536 rows.  45 sessions of 0 to 2.5k behind six
-// prefixes: 39 us (78 with a kernel and a join for each half).
+// GB, 128 us at the copy rate): 195 us, of which 8 join; all of it on the tensor
+// cores as one list: 225.  (Sessions' runs beside the prefixes' on other
+// multiprocessors took 174, but such a kernel begins without a wait of its own, and
+// what earlier kernels wrote is promised to be seen only behind one.)  Trees of 32
+// nodes x 8 heads of 32 sessions behind two prompts of 12k and 24k (0.68 TFLOP): 567
+// us, 440 of them the prefixes' products at 1.37 PFLOP/s, 30 the join of 65,536
+// rows.  45 sessions of 0 to 2.5k behind six prefixes: 38 us (78 with a kernel and a
+// join for each half).
 #include "kv_attend.cuh"
 
 namespace unison {
@@ -258,7 +260,6 @@ uint64_t parts_bytes(const AttendPlan &p) { return (uint64_t)p.grid * 2 * p.rows
 struct SharedPlan {
   AttendPlan prefix, own;
   bool together;  // one list
-  bool beside;    // two kernels at a time
   uint64_t own_partial, rows, own_rows, bytes;  // offsets: parts, AttendRows of prefixes and of sessions
 };
 
@@ -276,8 +277,6 @@ AttendPlan prefix_plan(int head_dim, int64_t rows, int prefixes) {
   }
   return p;
 }
-
-constexpr int kFiner = 3;  // runs of sessions for each place of their CTAs, where they begin one by one
 
 int shared_plan(SharedPlan &s, const unison_kv_cache *c, const unison_kv_prefix *x, const unison_kv_tree *t,
                 int n_q_heads) {
@@ -301,8 +300,6 @@ int shared_plan(SharedPlan &s, const unison_kv_cache *c, const unison_kv_prefix 
     if (s.own.rows < s.prefix.rows) s.own = s.prefix;
     s.prefix = s.own;
   }
-  s.beside = !s.together && s.prefix.tc && !s.own.tc;
-  if (s.beside) s.own.grid = kv_sm_count() * 2 * kFiner;
   const uint64_t rows = (uint64_t)t->n_tokens * n_q_heads;
   auto whole = [](uint64_t n) { return (n + 31) / 32 * 32; };  // stores take 32 bytes
   s.own_partial = s.together ? 0 : whole(parts_bytes(s.prefix));
@@ -360,18 +357,9 @@ extern "C" int unison_kv_attend_shared(const unison_kv_cache *cache, const uniso
   p.n_prefixes = prefix->cache->n_seqs;
   if (!s.together) {
     p.partial = prefix_partial;
-    p.sms = kv_sm_count();
-    auto others = [&](const AttendPlan &other) {
-      p.other_tile = !s.beside ? 0 : other.tc ? 128 : 64;
-      p.other_rows = other.rows;
-      p.other_groups = other.row_groups;
-    };
-    others(s.own);
     rc = attend_list(p, s.prefix, cuda_stream);
     if (rc != UNISON_OK) return rc;
-    others(s.prefix);
     p.n_prefixes = 0;
-    p.beside = 1;
   }
   p.n_sessions = tree->n_seqs;
   p.partial = own_partial;

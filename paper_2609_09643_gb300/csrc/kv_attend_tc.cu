@@ -93,10 +93,7 @@ struct AttendTcParams : AttendParams {
 
 template <typename T, int DP, int kUse>
 __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_constant__ AttendTcParams P) {
-  if (kUse == kList && P.beside)
-    next_kernel_may_begin();
-  else
-    follow_last_kernel();
+  follow_last_kernel();
   constexpr uint32_t kTileBytes = kTile * DP * 2, kBlock = kTile * 128;
   constexpr int kLower = KvType<T>::kMostWeight > kSlack ? KvType<T>::kMostWeight - kSlack : 0;
   extern __shared__ unsigned char smem_raw[];
@@ -110,7 +107,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
   auto seq_tiles = [&](int b) -> int64_t {
     if constexpr (kUse == kList) {
       const bool prefix = b < P.n_prefixes;
-      return attend_places(P, prefix, prefix ? b : b - P.n_prefixes, kTile, kTcRows, groups, true);
+      return attend_places(P, prefix, prefix ? b : b - P.n_prefixes, kTile, kTcRows, groups);
     }
     const int tokens = kv_tokens(P.t, b, P.c.status).count;
     const int row_tiles = (tokens * G + kTcRows - 1) / kTcRows;
@@ -119,12 +116,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
   };
   KvRun run;
   if (!kv_find_run(run, sh.run, kUse == kList ? P.n_prefixes + P.n_sessions : P.c.n_seqs, gridDim.x / groups,
-                   blockIdx.x / groups, seq_tiles, [&](int64_t total) {
-                     return kUse == kList ? attend_most_runs(P, total, sh.run.part) : total;
-                   })) {
-    if (kUse == kList && P.beside && blockIdx.x == 0) wait_for_last_kernel();
+                   blockIdx.x / groups, seq_tiles,
+                   [](int64_t total) { return kUse == kList ? attend_most_runs(total) : total; }))
     return;
-  }
 
   if (tid == 0) {
     for (int i = 0; i < kSlots<DP>; i++) {
@@ -677,8 +671,6 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     tmem_after_sync();
     tmem_free(tmem, 512);
   }
-  // (this kernel's end is the other one's, too)
-  if (kUse == kList && P.beside && blockIdx.x == 0) wait_for_last_kernel();
 }
 
 }  // namespace

@@ -176,3 +176,22 @@ def test_binding_refuses_other_types_shapes_and_places(kv):
         with pytest.raises(ValueError):
             call()
             print("not refused:", i)
+
+
+def test_every_kernel_waits_before_anything_else():
+    """A kernel is set up while the one before it on the stream ends.  What that one wrote, and what those before it
+    wrote, is promised to be seen only behind a wait of the kernel's own: it comes first in all of them."""
+    import os
+    import re
+    from paper_2609_09643_gb300 import native
+    seen = 0
+    for name in native.SOURCES:
+        if not name.startswith("kv_"):
+            continue
+        with open(os.path.join(native.CSRC, name)) as f:
+            text = re.sub(r"//[^\n]*", "", f.read())
+        for at in re.finditer(r"__global__", text):
+            body = text[text.index("{", at.start()) + 1:]
+            assert body.split(None, 1)[0] == "follow_last_kernel();", (name, body[:80])
+            seen += 1
+    assert seen >= 12
