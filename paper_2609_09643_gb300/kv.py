@@ -355,6 +355,9 @@ def attend_shared(cache: Cache, prefix: Prefix, tree: Tree, q, k_new, v_new, sca
     return out, lse
 
 
+_MOST_SIZES = 256  # that a cache keeps; to ask again takes a microsecond
+
+
 def attend_shared_workspace(cache: Cache, prefix: Prefix, tree: Tree, n_q_heads: int) -> int:
     """Bytes of scratch that attend_shared takes (a function of the sizes and the device alone)."""
     if cache.on_gpu and _elsewhere(cache.device):
@@ -364,6 +367,8 @@ def attend_shared_workspace(cache: Cache, prefix: Prefix, tree: Tree, n_q_heads:
     if n is None:
         n = int(lib().unison_kv_attend_shared_workspace(cache.address, prefix.address, tree.address, n_q_heads))
         if n:
+            if len(cache.sizes) >= _MOST_SIZES:  # (every count of tokens is a size of its own)
+                cache.sizes.clear()
             cache.sizes[key] = n
     return n
 

@@ -195,3 +195,14 @@ def test_every_kernel_waits_before_anything_else():
             assert body.split(None, 1)[0] == "follow_last_kernel();", (name, body[:80])
             seen += 1
     assert seen >= 12
+
+
+def test_a_cache_keeps_a_bounded_list_of_sizes(kv):
+    m, pm = Made([5, 40], [3, 2], device="cpu"), Made([100], [0], device="cpu")
+    cache, prefix = m.cache(kv), kv.Prefix(pm.cache(kv), torch.tensor([0, 2], dtype=torch.int32))
+    offsets = torch.zeros(3, dtype=torch.int32)
+    for n in range(1, 2000):  # drafts of differing size: every step has another number of tokens
+        tree = kv.Tree(offsets, 64, n_tokens=n)
+        size = kv.attend_shared_workspace(cache, prefix, tree, 8)
+        assert size > 0 and size == kv.attend_shared_workspace(cache, prefix, tree, 8)
+    assert len(cache.sizes) <= 256
