@@ -127,12 +127,6 @@ __device__ __forceinline__ void store_n(T *p, const float (&x)[N]) {
     *reinterpret_cast<uint2 *>(p) = make_uint2(KvType<T>::pack(x[0], x[1]), KvType<T>::pack(x[2], x[3]));
 }
 
-__device__ __forceinline__ uint64_t mul_pair(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-
 // V: elements of either half of a lane's unit: 4 or 8.
 template <typename T, int V>
 __global__ void __launch_bounds__(kThreads, 8) rotate_kernel(const RotateParams P) {

@@ -353,11 +353,6 @@ struct FastShared {
   uint32_t count;
 };
 
-__device__ __forceinline__ uint64_t mul_pair(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
 __device__ __forceinline__ uint64_t fma_pair_rz(uint64_t a, uint64_t b, uint64_t c) {
   uint64_t r;
   asm("fma.rz.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
