@@ -92,7 +92,8 @@ struct RowParts {
 // Four rows at a time where there are many: eight parts of each at most, and
 // rows with more go one by one, 32 parts at a time.  Bound by four or five loads
 // one after the other: 8 us for 2,048 rows of 20 parts, 30 for 65,536 rows of
-// two to four (one row of a warp at a time: 76).
+// two to four (one row of a warp at a time: 76), with 60 bytes of a thread's 64
+// registers' worth in local memory at a head size of 128.
 constexpr int kJoin = 256;
 template <typename T, int DP, int kRows>
 __global__ void __launch_bounds__(kJoin, DP <= 128 ? 4 : 2)

@@ -18,9 +18,11 @@
 // 32-bit cosines and sines are to 2^-25 themselves.
 //
 // Bound by memory, if the operations are few: 13,750 tokens of 32 + 8 heads of 128
-// (282 MB): 51 us, 5.5 TB/s, 0.81 of the copy rate, instructions issued in 63% of
+// (282 MB): 52 us, 5.4 TB/s, 0.80 of the copy rate, instructions issued in 63% of
 // the cycles.  A CTA a token, one element an operation: 71; rows fetched two or
-// three steps ahead: 55 to 60, as fewer warps fit.  One token: 3.4 us.
+// three steps ahead: 55 to 60, as fewer warps fit (eight CTAs on a multiprocessor
+// leave 64 registers, and 80 bytes of a thread's are kept in local memory as it is).
+// One token: 3.4 us.
 #include <type_traits>
 
 #include "kv_tc.cuh"
