@@ -591,6 +591,22 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const unison_kv_sam
   auto exponent = [&](float x) -> float { return __fmul_rn(__fsub_rn(x, top), factor); };
   auto weigh = [&](float x) -> int64_t { return (int64_t)__fmul_rn(exp2_fast(exponent(x)), 1099511627776.f); };
 
+  // f(how many CTAs, known when it is compiled), so that every CTA's words can be
+  // asked for at once and none of the loads has a condition.  (With loads of c < ctas
+  // and zeros else, the compiler's code for rows of one CTA added another register to
+  // the sums of a warp now and then: 2% of such rows with a histogram.)
+  auto by_ctas = [&](auto f) {
+    static_assert(kMaxCluster == 8, "powers of two up to it");
+    if (ctas == 1)
+      f(std::integral_constant<int, 1>());
+    else if (ctas == 2)
+      f(std::integral_constant<int, 2>());
+    else if (ctas == 4)
+      f(std::integral_constant<int, 4>());
+    else
+      f(std::integral_constant<int, 8>());
+  };
+
   // ---- lists: every CTA's own entries, read by those that want them all.  A list
   // is written again when a barrier has told that everyone has read the last one
   // (of one that was too long nobody has).
@@ -603,9 +619,17 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const unison_kv_sam
   int counts[kMaxCluster];
   auto gather = [&](int which) -> int {  // the length of all, and of each in `counts`
     cluster_sync(warp);
-#pragma unroll
-    for (int c = 0; c < kMaxCluster; c++) counts[c] = c < ctas ? *cluster.map_shared_rank(&sh.own_count[which], c) : 0;
     int all = 0;
+#pragma unroll
+    for (int c = 0; c < kMaxCluster; c++) counts[c] = 0;
+    by_ctas([&](auto n) {
+      if constexpr (n.value == 1) {
+        counts[0] = sh.own_count[which];
+      } else {
+#pragma unroll
+        for (int c = 0; c < n.value; c++) counts[c] = *cluster.map_shared_rank(&sh.own_count[which], c);
+      }
+    });
 #pragma unroll
     for (int c = 0; c < kMaxCluster; c++) all += min(counts[c], kList + 1);
     return all;
@@ -618,7 +642,9 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const unison_kv_sam
       at -= on ? counts[i] : 0;
       c += on;
     }
-    return tid < count ? cluster.map_shared_rank(sh.own, c)[at] : 0;
+    if (ctas == 1) return tid < count ? sh.own[tid] : 0;
+    const unsigned long long one = cluster.map_shared_rank(sh.own, min(c, ctas - 1))[min(at, kList - 1)];
+    return tid < count ? one : 0;
   };
 
   // The list's entries, each compared with all others, by as many threads as there
@@ -680,16 +706,22 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const unison_kv_sam
   };
   // This thread's slot, from the top, in all CTAs.
   auto totals = [&](int64_t &n, int64_t &w) {
-    uint4 v[kMaxCluster];
-#pragma unroll
-    for (int c = 0; c < kMaxCluster; c++)
-      v[c] = c < ctas ? *cluster.map_shared_rank(&sh.g.slots[kSlots - 1 - tid], c) : make_uint4(0, 0, 0, 0);
     n = w = 0;
+    by_ctas([&](auto count) {
+      uint4 v[count.value];
+      const uint4 *const mine = &sh.g.slots[kSlots - 1 - tid];
+      if constexpr (count.value == 1) {
+        v[0] = *mine;
+      } else {
 #pragma unroll
-    for (int c = 0; c < kMaxCluster; c++) {
-      n += v[c].x;
-      w += ((int64_t)v[c].y << 28) + ((int64_t)v[c].z << 14) + v[c].w;
-    }
+        for (int c = 0; c < count.value; c++) v[c] = *cluster.map_shared_rank(mine, c);
+      }
+#pragma unroll
+      for (int c = 0; c < count.value; c++) {
+        n += v[c].x;
+        w += ((int64_t)v[c].y << 28) + ((int64_t)v[c].z << 14) + v[c].w;
+      }
+    });
   };
 
   // ---- what is kept, and the distribution
