@@ -27,7 +27,7 @@
 // Bound by latency: the loads of a row take 4 us, each exchange between the
 // cluster's CTAs 1 to 2, and a row three to five of them, while one row's 64 KB a CTA
 // leave room for three CTAs on a multiprocessor.  One row of 32,000: 9 us.  128
-// rows of 128,000 in 32 bits (65 MB, 10 us at the copy rate), 57 at a time: 59 to 64 us, 13
+// rows of 128,000 in 32 bits (65 MB, 10 us at the copy rate), 57 at a time: 58 to 66 us, 13
 // for a row with a short list and 38 with a histogram (6 of them).  512 rows of
 // 64,000 in bf16 to distributions (131 MB, 19 us at the copy rate): 41 to 46 us.  A row
 // that stays in the L2 cache instead, all rows at a time: 112 and 66 us, because
