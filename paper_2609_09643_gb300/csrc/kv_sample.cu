@@ -593,8 +593,8 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const unison_kv_sam
 
   // f(how many CTAs, known when it is compiled), so that every CTA's words can be
   // asked for at once and none of the loads has a condition.  (With loads of c < ctas
-  // and zeros else, the compiler's code for rows of one CTA added another register to
-  // the sums of a warp now and then: 2% of such rows with a histogram.)
+  // and zeros else, what was loaded was right, but in 2% of the rows of one CTA with a
+  // histogram the sums of some warps came out larger by their slots' counts.)
   auto by_ctas = [&](auto f) {
     static_assert(kMaxCluster == 8, "powers of two up to it");
     if (ctas == 1)
